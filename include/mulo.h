@@ -315,6 +315,124 @@ MULO_API mulo_status mulo_resample_islands(mulo_ctx *ctx, mulo_kv *kv, int32_t B
                                   const int32_t *prev_tokens, const uint8_t *mask, const int32_t *rank,
                                   int32_t *tokens, float *logits, int32_t *overflow);
 
+/* ---- a prefix that sequences share, a window, and filtered draws ---------------------------------------------------
+ * Operators next to the verification step, for batches of images of one prompt. */
+
+/* Attention of a block of L queries per sequence over a prefix that the sequences of a group share (read once for all of
+ * them where that pays) and over the rows that each sequence has of its own, optionally through a window with sinks.
+ *   Sequence b belongs to group b / (B / n_prefix) and its keys are the rows 0 .. prefix_len-1 of that group's prefix, then
+ *   its own rows.  Query j sits at own row P_b + j, position p = prefix_len + P_b + j, and sees key position t iff t <= p and
+ *   (window == 0, or t < sinks, or p - t < window).  out = sum_t softmax_t(scale q . k_t) v_t; scores, statistics and sums
+ *   in float32, and for MULO_BF16 the exponentials are rounded to bf16 in front of the product with v.
+ * All strides are in elements; heads of q and out are n_heads, of k and v n_kv_heads (head h reads n_kv_heads * h / n_heads).
+ *   dtype        mulo_dtype of q, out, k, v and the prefix
+ *   q            element (b, h, j, c) at q_batch b + q_head h + q_row j + c; out likewise
+ *   k            own keys, element (b, h, t, c) at k_batch b + k_head h + k_row t + c, `rows` rows allocated
+ *   v            own values, transposed: element (b, h, c, t) at v_batch b + v_head h + v_chan c + t, t < rows
+ *                (the layouts of mulo_kv are k_row == head_dim, v_chan == rows)
+ *   P, P_seq     own rows in front of the block: P for every sequence, or, when P_seq (device int32 [B]) is given, P_seq[b]
+ *                of sequence b; P is then the largest of them (it sizes the launch).  An entry above rows - L counts as
+ *                rows - L; a negative one says that the sequence is absent: its outputs are zeros.  Rows P_b .. P_b + L-1
+ *                hold the block's own keys and values.
+ *   prefix_k, prefix_v  the prefixes, laid out as k and v with a group in the place of a sequence; prefix_rows rows allocated,
+ *                prefix_len in use.  prefix_len == 0: no prefix (the pointers are not read)
+ *   sinks, window   window == 0: every earlier key is seen, and sinks is not read
+ *   scale        0: 1 / sqrt(head_dim)
+ * Rows that no query of the call sees may hold anything, NaN included; what some query sees has to be finite.  q and out must
+ * not overlap.
+ * Limits: head_dim 64 or 128; n_heads a multiple of n_kv_heads, B of n_prefix; rows, prefix_rows and every stride a multiple
+ * of 16 bytes, pointers 16-byte aligned; rows, prefix_rows <= 2^24, k rows at most 2^22 and v channels 2^26 elements apart;
+ * B * n_heads * L < 2^30. */
+typedef struct {
+    int32_t dtype, B, L, n_heads, n_kv_heads, head_dim;
+    const void *q;
+    int64_t q_batch, q_head, q_row;
+    void *out;
+    int64_t out_batch, out_head, out_row;
+    const void *k, *v;
+    int64_t k_batch, k_head, k_row, v_batch, v_head, v_chan;
+    int32_t rows, P;
+    const int32_t *P_seq;
+    const void *prefix_k, *prefix_v;
+    int64_t prefix_k_group, prefix_k_head, prefix_k_row, prefix_v_group, prefix_v_head, prefix_v_chan;
+    int32_t n_prefix, prefix_len, prefix_rows;
+    int32_t sinks, window;
+    float scale;
+} mulo_attention_args;
+
+/* Host-side check of the arguments (no GPU needed), also run by mulo_attention. */
+MULO_API mulo_status mulo_check_attention(const mulo_attention_args *a);
+
+/* Device bytes of scratch with which mulo_attention runs fastest (partial results of keys that are dealt to several
+ * workgroups); 0 when it needs none or the arguments are bad. */
+MULO_API uint64_t mulo_attention_workspace_bytes(const mulo_attention_args *a);
+
+/* Runs on the current HIP device and allocates nothing.  workspace: device memory, 16-byte aligned, used until the call's
+ * stream work has finished (calls that may overlap need one each, and so do graphs that may replay at the same time), or
+ * NULL; with fewer bytes than mulo_attention_workspace_bytes says the keys are dealt to fewer workgroups.  The
+ * number of shares follows from the sizes alone, so equal calls give equal bits.
+ * Errors: as mulo_check_attention; a workspace that is not 16-byte aligned -> MULO_ERR_UNSUPPORTED. */
+MULO_API mulo_status mulo_attention(void *hip_stream, const mulo_attention_args *a, void *workspace, uint64_t workspace_bytes);
+
+/* A prefix that the sequences of a context share.
+ *   kv         the prefixes, as a mulo_kv of max_prefix sequences of `rows` rows: what mulo_verify_forward of another context
+ *              (max_batch = max_prefix, max_seq = rows, same model) leaves
+ *   n_prefix   groups: sequence b of a call of B sequences reads prefix b / (B / n_prefix).  Guidance: 2, the prompt's
+ *              and the empty prompt's
+ *   len        rows in use, 1 <= len <= rows
+ *   rope_cos, rope_sin  float32 [max_seq, head_dim / 2] that take the place of the context's tables while the prefix is
+ *              attached: row i belongs to the context's cache row i, which is position len + i */
+typedef struct {
+    mulo_kv kv;
+    int32_t n_prefix, max_prefix, rows, len;
+    const float *rope_cos, *rope_sin;
+} mulo_prefix;
+
+/* From the next call on every forward pass of the context (mulo_verify_forward, mulo_verify_step, mulo_resample_sequential,
+ * mulo_resample_islands) attends to the attached prefix in front of its cache rows, as mulo_attention does: P counts the
+ * context's own rows, and its cache row i is position len + i.  The struct is copied; the memory must stay valid and unchanged
+ * while attached.  NULL detaches.  A call whose number of sequences (2 B with guidance) is not a multiple of
+ * n_prefix is MULO_ERR_SHAPE.
+ * Errors: head_dim other than 64 or 128, or rows (or the context's max_seq) not a multiple of 16 bytes -> MULO_ERR_UNSUPPORTED. */
+MULO_API mulo_status mulo_attach_prefix(mulo_ctx *ctx, const mulo_prefix *prefix);
+
+/* From the next call on every forward pass of the context attends through a window: position p sees t <= p with t < sinks or
+ * p - t < window (positions count an attached prefix).  window == 0 (the state after mulo_create): everything.
+ * Errors: negative -> MULO_ERR_RANGE; the limits of mulo_attach_prefix. */
+MULO_API mulo_status mulo_set_window(mulo_ctx *ctx, int32_t sinks, int32_t window);
+
+/* Filter of a distribution, in this order (host struct):
+ *   cfg_scale    0: off.  s > 0: the row is z_u + s (z_c - z_u), as in mulo_step_params (float32, every operation rounded)
+ *   temperature  w_x = exp((z_x - max z) / temperature); 0: only the first largest entry stays
+ *   top_k        the top_k largest entries stay, of equal ones those with the lowest index; 0: all
+ *   top_p        of those an entry stays iff the mass in front of it (larger ones, equal ones of lower index) is below top_p
+ *                times the mass of all of them; in (0, 1], 1: all
+ *   min_p        of those an entry stays iff w_x >= min_p; in [0, 1] */
+typedef struct {
+    double temperature, top_p, min_p;
+    int32_t top_k;
+    float cfg_scale;
+} mulo_sample_params;
+
+/* Filters rows of logits and draws from what stays, without a context (allocates nothing, runs on the current HIP device).
+ *   logits      device, dtype (mulo_dtype) [rows, vocab], row r at r * row_stride elements; with guidance [2 rows, vocab],
+ *               row r conditional and row `rows` + r its unconditional twin.  Aligned to its element; 16-byte aligned rows
+ *               are read faster.  NaN counts as -inf; +inf takes all the mass, shared by all that are +inf
+ *   u           device float32 [rows] in [0, 1) (what lies outside counts as the nearest in it, NaN as 0); NULL allowed
+ *               without tokens
+ *   tokens      device int32 [rows] (out) or NULL: the first entry, by index, up to which the mass that stays exceeds u times
+ *               all of it (64-bit weights: the draw does not depend on an order of summation); -1 for a row without an
+ *               entry above -inf
+ *   probs       device float32 [rows, vocab] (out) or NULL: the filtered distribution (a row of zeros if there is none):
+ *               what mulo_upsample_draft and the accept test take as a draft's
+ *   logits_out  device float32 [rows, vocab] (out) or NULL: z / temperature where the entry stays (z with temperature 0;
+ *               kept within float32's finite range), -inf elsewhere: what the accept test takes as the target's.  May be `logits` itself for float32 rows
+ *               that lie next to each other
+ * Errors: no output -> MULO_ERR_NULL; vocab > 262144 -> MULO_ERR_UNSUPPORTED; row_stride < vocab -> MULO_ERR_SHAPE. */
+MULO_API mulo_status mulo_sample_filtered(void *hip_stream, const mulo_sample_params *p, int32_t rows, int32_t vocab,
+                                 int32_t dtype, const void *logits, int64_t row_stride, const float *u,
+                                 int32_t *tokens, float *probs, float *logits_out);
+
 /* Test and debugging aid (not part of the method): copies the first `bytes` bytes of one of the context's
  * workspace buffers, as the last mulo_verify_forward (or step) left it, to dst on the context's stream.  With a
  * one-layer model these are that layer's intermediate tensors, which is how the tests compare every stage of a

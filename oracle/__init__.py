@@ -17,6 +17,9 @@ Modules (each function cites the passage of the paper it follows):
   resample  residual resampling (Eq. 2) through an integer CDF
   step      the whole verification step (Alg. 1 Steps 2-5 + one-shot resample); sequential re-sampling
             (Alg. 1 Step 6); island-parallel re-sampling (Sec. 3.4)
+  context   attention over a shared prefix and own rows with a window and sinks, query by query, and the
+            rounding bounds of its float32 and bf16 forms
+  sampling  temperature, top-k, top-p and min-p, and a draw from a uniform, entry by entry
 
 Pin status (see tests/test_oracle_*.py):
   upsample, accept, local, resample, step : pinned (invariants, closed forms,

@@ -73,6 +73,7 @@ class DecoderOracle:
         self.cfg = dict(cfg)
         self.w = weights
         self.rb = round_to_bf16 if round_bf16 else (lambda t: t)
+        self.sinks = self.window = 0     # window > 0: query p of a forward sees s <= p with s < sinks or p - s < window
         self.cos = torch.as_tensor(np.asarray(rope_cos)).to(torch.float64)
         self.sin = torch.as_tensor(np.asarray(rope_sin)).to(torch.float64)
         nl, nh, dh = cfg["n_layers"], cfg["n_heads"], cfg["head_dim"]
@@ -108,6 +109,9 @@ class DecoderOracle:
         cos, sin = self.cos[P:S], self.sin[P:S]
         pos_q = torch.arange(P, S)[:, None]
         visible = torch.arange(S)[None, :] <= pos_q                  # key s visible to query j iff s <= P + j
+        if self.window:
+            rows = torch.arange(S)[None, :]
+            visible = visible & ((rows < self.sinks) | (pos_q - rows < self.window))
         for l in range(nl):
             if taps is not None:
                 taps.append(x.clone())

@@ -18,7 +18,8 @@ STATUS_NAMES = {0: "MULO_OK", 1: "MULO_ERR_NULL", 2: "MULO_ERR_SHAPE", 3: "MULO_
 EXPORTS = ["mulo_status_string", "mulo_check_model_cfg", "mulo_check_step_params", "mulo_workspace_bytes",
            "mulo_create", "mulo_destroy", "mulo_upsample_draft", "mulo_verify_forward",
            "mulo_accept_local_resample", "mulo_accept_local_resample_static", "mulo_verify_step", "mulo_resample_sequential", "mulo_rejection_islands", "mulo_resample_islands", "mulo_workspace_read", "mulo_profile",
-           "mulo_profile_read"]
+           "mulo_profile_read", "mulo_check_attention", "mulo_attention_workspace_bytes", "mulo_attention",
+           "mulo_attach_prefix", "mulo_set_window", "mulo_sample_filtered"]
 
 
 class MuloError(RuntimeError):
@@ -48,6 +49,27 @@ class StepParams(C.Structure):
                 ("nbr", C.c_void_p), ("resample_mode", C.c_int32),
                 ("seed", C.c_uint64), ("rng_counter", C.c_uint64),
                 ("accept_mode", C.c_int32), ("tau", C.c_float), ("cfg_scale", C.c_float)]
+
+
+class AttentionArgs(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("dtype", "B", "L", "n_heads", "n_kv_heads", "head_dim")] + [("q", C.c_void_p)] +
+                [(n, C.c_int64) for n in ("q_batch", "q_head", "q_row")] + [("out", C.c_void_p)] +
+                [(n, C.c_int64) for n in ("out_batch", "out_head", "out_row")] + [("k", C.c_void_p), ("v", C.c_void_p)] +
+                [(n, C.c_int64) for n in ("k_batch", "k_head", "k_row", "v_batch", "v_head", "v_chan")] +
+                [("rows", C.c_int32), ("P", C.c_int32), ("P_seq", C.c_void_p), ("prefix_k", C.c_void_p), ("prefix_v", C.c_void_p)] +
+                [(n, C.c_int64) for n in ("prefix_k_group", "prefix_k_head", "prefix_k_row", "prefix_v_group", "prefix_v_head",
+                                          "prefix_v_chan")] +
+                [(n, C.c_int32) for n in ("n_prefix", "prefix_len", "prefix_rows", "sinks", "window")] + [("scale", C.c_float)])
+
+
+class Prefix(C.Structure):
+    _fields_ = ([("kv", KV)] + [(n, C.c_int32) for n in ("n_prefix", "max_prefix", "rows", "len")] +
+                [("rope_cos", C.c_void_p), ("rope_sin", C.c_void_p)])
+
+
+class SampleParams(C.Structure):
+    _fields_ = [("temperature", C.c_double), ("top_p", C.c_double), ("min_p", C.c_double), ("top_k", C.c_int32),
+                ("cfg_scale", C.c_float)]
 
 
 _lib = None
@@ -84,8 +106,15 @@ def load_library():
     lib.mulo_workspace_read.argtypes = [P, I32, P, C.c_uint64]
     lib.mulo_profile.argtypes = [P, I32]
     lib.mulo_profile_read.argtypes = [P, C.POINTER(C.c_float), C.POINTER(I32)]
+    lib.mulo_check_attention.argtypes = [C.POINTER(AttentionArgs)]
+    lib.mulo_attention_workspace_bytes.restype = C.c_uint64
+    lib.mulo_attention_workspace_bytes.argtypes = [C.POINTER(AttentionArgs)]
+    lib.mulo_attention.argtypes = [P, C.POINTER(AttentionArgs), P, C.c_uint64]
+    lib.mulo_attach_prefix.argtypes = [P, C.POINTER(Prefix)]
+    lib.mulo_set_window.argtypes = [P, I32, I32]
+    lib.mulo_sample_filtered.argtypes = [P, C.POINTER(SampleParams), I32, I32, I32, P, I64, P, P, P, P]
     for n in EXPORTS:
-        if n not in ("mulo_status_string", "mulo_workspace_bytes", "mulo_destroy"):
+        if n not in ("mulo_status_string", "mulo_workspace_bytes", "mulo_destroy", "mulo_attention_workspace_bytes"):
             getattr(lib, n).restype = C.c_int
     _lib = lib
     return lib
@@ -250,6 +279,127 @@ def mulo_workspace_read(ctx, which, dst):
     """Copy a workspace buffer of the last forward pass into the (contiguous, device) tensor dst."""
     _check(load_library().mulo_workspace_read(ctx.handle, which, _ptr(dst), dst.numel() * dst.element_size()),
            "mulo_workspace_read")
+
+
+def _strided(t, dtype, name, dims):
+    """Pointer and strides (elements; 0 where there is only one) of a tensor whose last dimension is contiguous."""
+    if t.dim() != dims or not t.is_cuda or t.dtype != dtype or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError("%s: expected a device tensor of %d dimensions, %s, contiguous in the last" % (name, dims, dtype))
+    return t.data_ptr(), [t.stride(i) if t.shape[i] > 1 else 0 for i in range(dims - 1)]
+
+
+def _on_device(device, stream):
+    """The device of a call without a context, and its stream: a raw hipStream_t, or torch's current stream of that device."""
+    return torch.cuda.device(device), C.c_void_p(torch.cuda.current_stream(device).cuda_stream if stream is None else stream)
+
+
+class Attention:
+    """Arguments of mulo_attention, checked, with the tensors they point into."""
+
+    def __init__(self, args, keep, device):
+        self.args, self._keep, self.device = args, keep, device
+        self.ref = C.byref(args)
+
+
+def make_attention(q, out, k, v, P, P_seq=None, prefix_k=None, prefix_v=None, prefix_len=0, sinks=0, window=0, scale=0.0):
+    """q, out [B, n_heads, L, head_dim]; k [B, n_kv_heads, rows, head_dim]; v [B, n_kv_heads, head_dim, rows]; P_seq int32 [B]
+    or None; prefix_k [groups, n_kv_heads, prefix_rows, head_dim], prefix_v [groups, n_kv_heads, head_dim, prefix_rows]: any
+    strides with a contiguous last dimension."""
+    if q.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("expected bfloat16 or float32, got %s" % q.dtype)
+    B, nh, L, dh = q.shape
+    nkv, rows = k.shape[1], k.shape[2]
+    if out.shape != q.shape or k.shape != (B, nkv, rows, dh) or v.shape != (B, nkv, dh, rows):
+        raise ValueError("q, out, k and v do not fit together")
+    tensors = [q, out, k, v]
+    a = AttentionArgs(dtype=MULO_BF16 if q.dtype == torch.bfloat16 else MULO_F32, B=B, L=L, n_heads=nh, n_kv_heads=nkv, head_dim=dh,
+                      rows=rows, P=P, n_prefix=1, prefix_len=prefix_len, sinks=sinks, window=window, scale=scale)
+    a.q, (a.q_batch, a.q_head, a.q_row) = _strided(q, q.dtype, "q", 4)
+    a.out, (a.out_batch, a.out_head, a.out_row) = _strided(out, q.dtype, "out", 4)
+    a.k, (a.k_batch, a.k_head, a.k_row) = _strided(k, q.dtype, "k", 4)
+    a.v, (a.v_batch, a.v_head, a.v_chan) = _strided(v, q.dtype, "v", 4)
+    if P_seq is not None:
+        if P_seq.shape != (B,):
+            raise ValueError("P_seq has one entry per sequence")
+        a.P_seq = _ptr(P_seq, torch.int32)
+        tensors.append(P_seq)
+    if prefix_len:
+        G, prows = prefix_k.shape[0], prefix_k.shape[2]
+        if prefix_k.shape != (G, nkv, prows, dh) or prefix_v.shape != (G, nkv, dh, prows):
+            raise ValueError("the prefix does not fit the cache")
+        a.n_prefix, a.prefix_rows = G, prows
+        a.prefix_k, (a.prefix_k_group, a.prefix_k_head, a.prefix_k_row) = _strided(prefix_k, q.dtype, "prefix_k", 4)
+        a.prefix_v, (a.prefix_v_group, a.prefix_v_head, a.prefix_v_chan) = _strided(prefix_v, q.dtype, "prefix_v", 4)
+        tensors += [prefix_k, prefix_v]
+    if any(t.device != q.device for t in tensors):
+        raise ValueError("the tensors of a call lie on one device")
+    _check(load_library().mulo_check_attention(C.byref(a)), "mulo_check_attention")
+    return Attention(a, tensors, q.device)
+
+
+def mulo_attention_workspace_bytes(attention):
+    with torch.cuda.device(attention.device):
+        return load_library().mulo_attention_workspace_bytes(attention.ref)
+
+
+def mulo_attention(attention, workspace=None, stream=None):
+    """Writes `out` of make_attention; workspace: a contiguous device tensor or None."""
+    ptr, n = (None, 0) if workspace is None else (_ptr(workspace), workspace.numel() * workspace.element_size())
+    if workspace is not None and workspace.device != attention.device:
+        raise ValueError("the workspace lies on another device")
+    dev, st = _on_device(attention.device, stream)
+    with dev:
+        _check(load_library().mulo_attention(st, attention.ref, ptr, n), "mulo_attention")
+
+
+def mulo_attach_prefix(ctx, kv=None, length=0, rope_cos=None, rope_sin=None, n_prefix=None):
+    """kv: the (k, v) tensors of a cache whose max_batch sequences are the prefixes (alloc_kv of the context that made them);
+    rope_cos, rope_sin: float32 [max_seq, head_dim / 2] of ctx, row i for position length + i.  kv None detaches."""
+    if kv is None:
+        _check(load_library().mulo_attach_prefix(ctx.handle, None), "mulo_attach_prefix")
+        ctx._prefix = None
+        return
+    c = ctx.cfg
+    k, v = kv
+    n, rows = k.shape[1], k.shape[3]
+    if k.shape != (c.n_layers, n, c.n_heads, rows, c.head_dim) or v.shape != (c.n_layers, n, c.n_heads, c.head_dim, rows):
+        raise ValueError("the prefix is not a cache of this model")
+    if any(t.shape != (c.max_seq, c.head_dim // 2) for t in (rope_cos, rope_sin)):
+        raise ValueError("the rotary tables of the prefix have a row for every cache row of the context")
+    p = Prefix(KV(_ptr(k, ctx.tdtype), _ptr(v, ctx.tdtype)), n if n_prefix is None else n_prefix, n, rows, length,
+               _ptr(rope_cos, torch.float32), _ptr(rope_sin, torch.float32))
+    _check(load_library().mulo_attach_prefix(ctx.handle, C.byref(p)), "mulo_attach_prefix")
+    ctx._prefix = [k, v, rope_cos, rope_sin]
+
+
+def mulo_set_window(ctx, sinks, window):
+    _check(load_library().mulo_set_window(ctx.handle, sinks, window), "mulo_set_window")
+
+
+def make_sample_params(temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, cfg_scale=0.0):
+    return SampleParams(temperature, top_p, min_p, top_k, cfg_scale)
+
+
+def mulo_sample_filtered(params, logits, u=None, tokens=None, probs=None, logits_out=None, stream=None):
+    """logits [rows, vocab] (2 rows conditional, then unconditional, with params.cfg_scale), float32 or bfloat16, rows at any
+    stride; u float32 [rows]; tokens int32 [rows], probs and logits_out float32 [rows, vocab], each or None."""
+    if logits.dim() != 2 or logits.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("logits: expected a matrix of float32 or bfloat16")
+    ptr, (stride,) = _strided(logits, logits.dtype, "logits", 2)
+    n, V = logits.shape
+    rows = n // 2 if params.cfg_scale > 0 else n
+    if params.cfg_scale > 0 and n % 2:
+        raise ValueError("guidance takes a conditional and an unconditional row each")
+    for t, shape in ((u, (rows,)), (tokens, (rows,)), (probs, (rows, V)), (logits_out, (rows, V))):
+        if t is not None and (tuple(t.shape) != shape or t.device != logits.device):
+            raise ValueError("expected %s on the logits' device" % (shape,))
+    f32 = torch.float32
+    dev, st = _on_device(logits.device, stream)
+    with dev:
+        _check(load_library().mulo_sample_filtered(
+            st, C.byref(params), rows, V, MULO_BF16 if logits.dtype == torch.bfloat16 else MULO_F32, ptr, stride if n > 1 else V,
+            _ptr(u, f32, True), _ptr(tokens, torch.int32, True), _ptr(probs, f32, True), _ptr(logits_out, f32, True)),
+            "mulo_sample_filtered")
 
 
 PROF_CLASSES = ["gemm_qkv", "gemm_out", "gemm_gate_up", "gemm_down", "gemm_lm_head", "attention", "norm_embed",

@@ -3,6 +3,7 @@
 // enqueued (Alg. 1 Steps 2-5 + residual re-draw).  Nothing here computes.
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <new>
 #include <vector>
 
@@ -67,6 +68,8 @@ struct mulo_ctx {
     int32_t tile = -1;   // mulo_internal_tiles
     int32_t tiles_ran[5] = {-1, -1, -1, -1, -1};
     void* base;      // single allocation
+    mulo_prefix prefix{};   // len == 0: none attached
+    int sinks = 0, window = 0;
     // optional per-launch timing (mulo_profile)
     bool prof_on = false;
     uint32_t prof_mask = 0;   // classes that are bracketed
@@ -172,6 +175,7 @@ mulo_status check_forward_args(const mulo_ctx* ctx, const mulo_kv* kv, int B, in
     if (B < 1 || L < 1 || P < 0) return MULO_ERR_RANGE;
     if (B > ctx->cfg.max_batch || L > ctx->cfg.max_block || (int64_t)P + L > ctx->cfg.max_seq)
         return MULO_ERR_SHAPE;
+    if (ctx->prefix.len > 0 && B % ctx->prefix.n_prefix) return MULO_ERR_SHAPE;
     return MULO_OK;
 }
 
@@ -183,6 +187,38 @@ struct Scatter {
     const uint8_t* hide;
     int P0, Lblk;
 };
+
+// attention of a layer where a prefix is attached or a window is set
+void enqueue_context_attention(mulo_ctx* c, const mulo_kv* kv, int B, int L, int P, int layer, const Scatter* sc, bool frag) {
+    const mulo_model_cfg& m = c->cfg;
+    const int64_t nh = m.n_heads, dh = m.head_dim, slab = nh * m.max_seq * dh;   // a sequence's keys, or values, of a layer
+    const size_t e = c->esz;
+    ContextAttn a{};
+    a.dtype = m.dtype; a.B = B; a.L = L; a.nh = a.nkv = m.n_heads; a.dh = m.head_dim;
+    a.q = c->qbuf; a.q_batch = nh * L * dh; a.q_head = L * dh; a.q_row = dh;
+    a.out = c->att; a.out_batch = L * nh * dh; a.out_head = dh; a.out_row = nh * dh; a.frag = frag;
+    a.k = (const char*)kv->k + (size_t)layer * m.max_batch * slab * e;
+    a.v = (const char*)kv->v + (size_t)layer * m.max_batch * slab * e;
+    a.k_batch = a.v_batch = slab; a.k_head = a.v_head = m.max_seq * dh; a.k_row = dh; a.v_chan = m.max_seq;
+    a.rows = m.max_seq; a.P = P;
+    a.G = 1;
+    if (c->prefix.len > 0) {
+        const mulo_prefix& p = c->prefix;
+        const int64_t pslab = nh * p.rows * dh;
+        a.pk = (const char*)p.kv.k + (size_t)layer * p.max_prefix * pslab * e;
+        a.pv = (const char*)p.kv.v + (size_t)layer * p.max_prefix * pslab * e;
+        a.pk_group = a.pv_group = pslab; a.pk_head = a.pv_head = p.rows * dh; a.pk_row = dh; a.pv_chan = p.rows;
+        a.G = p.n_prefix; a.S = p.len; a.srows = p.rows;
+    }
+    a.sinks = c->sinks; a.window = c->window;
+    a.scale_log2 = 1.4426950408889634f / sqrtf((float)m.head_dim);
+    if (sc) { a.pos_tab = sc->pos_tab; a.hide = sc->hide; a.P0 = sc->P0; a.Lblk = sc->Lblk; }
+    if (m.dtype == MULO_BF16) {
+        a.part = c->attn_part;
+        a.part_floats = (int64_t)(attention_scratch_bytes(m.max_batch, m.n_heads, m.head_dim) / sizeof(float));
+    }
+    launch_context_attention(a, c->st);
+}
 
 // want_parts: also leave the softmax statistics of every 128-column part of every logit row in c->row_parts
 // (returns whether the lm-head kernel that ran produces them).  up: the inputs are a step's, from its draft tokens.
@@ -204,10 +240,13 @@ bool enqueue_forward(mulo_ctx* c, mulo_kv* kv, int B, int L, int P, const int32_
     float* const sums = shared ? c->ksums : c->attn_part;
     const int64_t sum_floats = shared ? c->ksum_floats : (int64_t)(attention_scratch_bytes(m.max_batch, m.n_heads, m.head_dim) / sizeof(float));
     auto sm = [&](int projection) { return StreamMode{frag, wfrag, sums, sum_floats, c->tile, &c->tiles_ran[projection]}; };
+    const bool own_rows = c->prefix.len == 0 && c->window == 0;   // plain causal attention over the sequence's own rows
+    const float* const rope_cos = c->prefix.len ? c->prefix.rope_cos : c->w.rope_cos;
+    const float* const rope_sin = c->prefix.len ? c->prefix.rope_sin : c->w.rope_sin;
     Slices add{nullptr, 0};   // what the last residual projection left for the norm behind it to add
     { PROF(MULO_PROF_NORM_EMBED); launch_embed(c->w.embed, dt, tok, emb, up ? *up : StepTokens{}, c->x, M, d, V, st); }
     for (int l = 0; l < m.n_layers; ++l) {
-        RopeArgs ra{c->w.rope_cos, c->w.rope_sin, L, P, m.n_heads, m.head_dim, m.max_seq, m.max_batch, l};
+        RopeArgs ra{rope_cos, rope_sin, L, P, m.n_heads, m.head_dim, m.max_seq, m.max_batch, l};
         if (sc) ra.pos_tab = sc->pos_tab;
         // launches that stream the weights read the context's copy in fragment order when it has one (same strides)
         const char* wq = (wfrag ? c->pk_wq : (const char*)c->w.wq) + (size_t)l * d * d * e;
@@ -223,7 +262,8 @@ bool enqueue_forward(mulo_ctx* c, mulo_kv* kv, int B, int L, int P, const int32_
             { PROF(MULO_PROF_NORM_EMBED); launch_rmsnorm(c->x, g_attn, dt, c->xh, M, d, m.rms_eps, frag, add, st); }
             { PROF(MULO_PROF_GEMM_QKV); launch_gemm_qkv_bf16(c->xh, wq, wk, wv, c->qbuf, kv->k, kv->v, M, d, ra, sm(0), st); }
             { PROF(MULO_PROF_ATTENTION);
-              if (sc) launch_attention_scattered_bf16(c->qbuf, kv->k, kv->v, c->att, c->attn_part, B, sc->pos_tab, L, sc->hide,
+              if (!own_rows) enqueue_context_attention(c, kv, B, L, P, l, sc, frag);
+              else if (sc) launch_attention_scattered_bf16(c->qbuf, kv->k, kv->v, c->att, c->attn_part, B, sc->pos_tab, L, sc->hide,
                                                       sc->P0, sc->Lblk, m.n_heads, m.head_dim, m.max_seq, m.max_batch, l, frag, st);
               else launch_attention_bf16(c->qbuf, kv->k, kv->v, c->att, c->attn_part, B, L, P, m.n_heads, m.head_dim,
                                          m.max_seq, m.max_batch, l, frag, st); }
@@ -236,7 +276,8 @@ bool enqueue_forward(mulo_ctx* c, mulo_kv* kv, int B, int L, int P, const int32_
               launch_qkv_f32(c->x, (const float*)g_attn, m.rms_eps, (const float*)wq, (const float*)wk, (const float*)wv,
                              (float*)c->qbuf, (float*)kv->k, (float*)kv->v, M, d, ra, st); }
             { PROF(MULO_PROF_ATTENTION);
-              launch_attention_f32((const float*)c->qbuf, (const float*)kv->k, (const float*)kv->v, (float*)c->att, B, L, P,
+              if (!own_rows) enqueue_context_attention(c, kv, B, L, P, l, nullptr, false);
+              else launch_attention_f32((const float*)c->qbuf, (const float*)kv->k, (const float*)kv->v, (float*)c->att, B, L, P,
                                    m.n_heads, m.head_dim, m.max_seq, m.max_batch, l, st); }
             { PROF(MULO_PROF_GEMM_OUT); launch_resid_f32((const float*)c->att, (const float*)wo, c->x, M, d, d, st); }
             { PROF(MULO_PROF_GEMM_GATE_UP);
@@ -469,6 +510,147 @@ MULO_API mulo_status mulo_internal_tiles(mulo_ctx* ctx, int32_t tile, int32_t* r
     ctx->tile = tile;
     for (int i = 0; ran && i < 5; ++i) ran[i] = ctx->tiles_ran[i];
     return MULO_OK;
+}
+
+namespace {
+// what the attention over prefix and own rows takes of the caches it is given
+bool context_sizes_ok(const mulo_ctx* ctx, int rows) {
+    return (ctx->cfg.head_dim == 64 || ctx->cfg.head_dim == 128) && rows % (int)(16 / ctx->esz) == 0 &&
+           ctx->cfg.max_seq % (int)(16 / ctx->esz) == 0 && rows <= (1 << 24) && ctx->cfg.max_seq <= (1 << 24);
+}
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+}  // namespace
+
+mulo_status mulo_attach_prefix(mulo_ctx* ctx, const mulo_prefix* p) {
+    if (!ctx) return MULO_ERR_NULL;
+    if (!p) {
+        ctx->prefix = mulo_prefix{};
+        return MULO_OK;
+    }
+    if (!p->kv.k || !p->kv.v || !p->rope_cos || !p->rope_sin) return MULO_ERR_NULL;
+    if (p->n_prefix < 1 || p->max_prefix < 1 || p->rows < 1 || p->len < 1) return MULO_ERR_RANGE;
+    if (p->n_prefix > p->max_prefix || p->len > p->rows) return MULO_ERR_SHAPE;
+    if (!context_sizes_ok(ctx, p->rows) || !aligned16(p->kv.k) || !aligned16(p->kv.v)) return MULO_ERR_UNSUPPORTED;
+    ctx->prefix = *p;
+    return MULO_OK;
+}
+
+mulo_status mulo_set_window(mulo_ctx* ctx, int32_t sinks, int32_t window) {
+    if (!ctx) return MULO_ERR_NULL;
+    if (sinks < 0 || window < 0) return MULO_ERR_RANGE;
+    if (window > 0 && !context_sizes_ok(ctx, ctx->cfg.max_seq)) return MULO_ERR_UNSUPPORTED;
+    ctx->sinks = sinks;
+    ctx->window = window;
+    return MULO_OK;
+}
+
+mulo_status mulo_check_attention(const mulo_attention_args* a) {
+    if (!a || !a->q || !a->out || !a->k || !a->v) return MULO_ERR_NULL;
+    if (a->dtype != MULO_F32 && a->dtype != MULO_BF16) return MULO_ERR_RANGE;
+    if (a->B < 1 || a->L < 1 || a->n_heads < 1 || a->n_kv_heads < 1 || a->head_dim < 1 || a->rows < 1 || a->P < 0 ||
+        a->prefix_len < 0 || a->sinks < 0 || a->window < 0 || !(a->scale >= 0.f && a->scale <= 3.0e38f))
+        return MULO_ERR_RANGE;
+    const bool prefix = a->prefix_len > 0;
+    if (prefix && (!a->prefix_k || !a->prefix_v)) return MULO_ERR_NULL;
+    if (prefix && a->n_prefix < 1) return MULO_ERR_RANGE;
+    const int64_t strides[] = {a->q_batch, a->q_head, a->q_row, a->out_batch, a->out_head, a->out_row, a->k_batch, a->k_head, a->k_row,
+                               a->v_batch, a->v_head, a->v_chan, a->prefix_k_group, a->prefix_k_head, a->prefix_k_row,
+                               a->prefix_v_group, a->prefix_v_head, a->prefix_v_chan};
+    const int n_strides = prefix ? 18 : 12;
+    for (int i = 0; i < n_strides; ++i)
+        if (strides[i] < 0 || strides[i] > ((int64_t)1 << 40)) return MULO_ERR_RANGE;
+    if ((int64_t)a->P + a->L > a->rows || a->n_heads % a->n_kv_heads) return MULO_ERR_SHAPE;
+    if (prefix && (a->prefix_len > a->prefix_rows || a->B % a->n_prefix)) return MULO_ERR_SHAPE;
+    if (a->k_row < a->head_dim || a->v_chan < a->rows ||
+        (prefix && (a->prefix_k_row < a->head_dim || a->prefix_v_chan < a->prefix_rows)))
+        return MULO_ERR_SHAPE;
+    // no two outputs at one place: every dimension steps over what lies inside it, in one order or another
+    {
+        struct Dim { int64_t n, step; } d[3] = {{a->B, a->out_batch}, {a->n_heads, a->out_head}, {a->L, a->out_row}};
+        for (int i = 0; i < 3; ++i)      // innermost first
+            for (int j = i + 1; j < 3; ++j)
+                if (d[j].n > 1 && (d[i].n == 1 || d[j].step < d[i].step)) { const Dim t = d[i]; d[i] = d[j]; d[j] = t; }
+        int64_t extent = a->head_dim;
+        for (int i = 0; i < 3; ++i) {
+            if (d[i].n == 1) continue;
+            if (d[i].step < extent) return MULO_ERR_SHAPE;
+            extent += (d[i].n - 1) * d[i].step;
+        }
+    }
+    if (a->head_dim != 64 && a->head_dim != 128) return MULO_ERR_UNSUPPORTED;
+    const int unit = a->dtype == MULO_BF16 ? 8 : 4;      // elements of 16 bytes
+    for (int i = 0; i < n_strides; ++i)
+        if (strides[i] % unit) return MULO_ERR_UNSUPPORTED;
+    if (a->rows % unit || a->rows > (1 << 24) || a->k_row > (1 << 22) || a->v_chan > (1 << 26)) return MULO_ERR_UNSUPPORTED;
+    if (prefix && (a->prefix_rows % unit || a->prefix_rows > (1 << 24) || a->prefix_k_row > (1 << 22) || a->prefix_v_chan > (1 << 26)))
+        return MULO_ERR_UNSUPPORTED;
+    if (!aligned16(a->q) || !aligned16(a->out) || !aligned16(a->k) || !aligned16(a->v) ||
+        (prefix && (!aligned16(a->prefix_k) || !aligned16(a->prefix_v))))
+        return MULO_ERR_UNSUPPORTED;
+    if ((int64_t)a->B * a->n_heads >= (1 << 30) || (int64_t)a->B * a->n_heads * a->L >= (1 << 30)) return MULO_ERR_UNSUPPORTED;
+    return MULO_OK;
+}
+
+namespace {
+ContextAttn context_attn(const mulo_attention_args* p) {
+    ContextAttn a{};
+    a.dtype = p->dtype; a.B = p->B; a.L = p->L; a.nh = p->n_heads; a.nkv = p->n_kv_heads; a.dh = p->head_dim;
+    a.q = p->q; a.q_batch = p->q_batch; a.q_head = p->q_head; a.q_row = p->q_row;
+    a.out = p->out; a.out_batch = p->out_batch; a.out_head = p->out_head; a.out_row = p->out_row;
+    a.k = p->k; a.v = p->v;
+    a.k_batch = p->k_batch; a.k_head = p->k_head; a.k_row = p->k_row;
+    a.v_batch = p->v_batch; a.v_head = p->v_head; a.v_chan = p->v_chan;
+    a.rows = p->rows; a.P = p->P; a.P_seq = p->P_seq;
+    a.G = 1;
+    if (p->prefix_len > 0) {
+        a.pk = p->prefix_k; a.pv = p->prefix_v;
+        a.pk_group = p->prefix_k_group; a.pk_head = p->prefix_k_head; a.pk_row = p->prefix_k_row;
+        a.pv_group = p->prefix_v_group; a.pv_head = p->prefix_v_head; a.pv_chan = p->prefix_v_chan;
+        a.G = p->n_prefix; a.S = p->prefix_len; a.srows = p->prefix_rows;
+    }
+    a.sinks = p->sinks; a.window = p->window;
+    a.scale_log2 = 1.4426950408889634f * (p->scale > 0.f ? p->scale : 1.0f / sqrtf((float)p->head_dim));
+    return a;
+}
+}  // namespace
+
+uint64_t mulo_attention_workspace_bytes(const mulo_attention_args* p) {
+    if (mulo_check_attention(p) != MULO_OK) return 0;
+    return (uint64_t)context_attention_floats(context_attn(p)) * sizeof(float);
+}
+
+mulo_status mulo_attention(void* hip_stream, const mulo_attention_args* p, void* workspace, uint64_t workspace_bytes) {
+    const mulo_status s = mulo_check_attention(p);
+    if (s != MULO_OK) return s;
+    if (!aligned16(workspace)) return MULO_ERR_UNSUPPORTED;
+    ContextAttn a = context_attn(p);
+    a.part = (float*)workspace;
+    a.part_floats = workspace ? (int64_t)((workspace_bytes < ((uint64_t)1 << 40) ? workspace_bytes : (uint64_t)1 << 40) / sizeof(float)) : 0;
+    launch_context_attention(a, (hipStream_t)hip_stream);
+    return check_launch();
+}
+
+mulo_status mulo_sample_filtered(void* hip_stream, const mulo_sample_params* p, int32_t rows, int32_t vocab, int32_t dtype,
+                                 const void* logits, int64_t row_stride, const float* u, int32_t* tokens, float* probs,
+                                 float* logits_out) {
+    if (!p || !logits || (tokens && !u) || (!tokens && !probs && !logits_out)) return MULO_ERR_NULL;
+    if (rows < 1 || vocab < 1 || (dtype != MULO_F32 && dtype != MULO_BF16) || p->top_k < 0 ||
+        !(p->temperature >= 0.0 && p->temperature <= 1e30) || (p->temperature > 0.0 && p->temperature < 1e-30) ||
+        !(p->top_p > 0.0 && p->top_p <= 1.0) || !(p->min_p >= 0.0 && p->min_p <= 1.0) || !(p->cfg_scale >= 0.f && p->cfg_scale <= 1.0e6f))
+        return MULO_ERR_RANGE;
+    if (vocab > 262144) return MULO_ERR_UNSUPPORTED;
+    if (row_stride < vocab || row_stride > ((int64_t)1 << 40)) return MULO_ERR_SHAPE;
+    const size_t e = dtype == MULO_BF16 ? 2 : 4;
+    if (((uintptr_t)logits & (e - 1)) || ((uintptr_t)probs & 3) || ((uintptr_t)logits_out & 3)) return MULO_ERR_UNSUPPORTED;
+    if (logits_out == logits && (dtype != MULO_F32 || row_stride != vocab)) return MULO_ERR_SHAPE;
+    SampleArgs a{};
+    a.logits = logits;
+    a.logits_u = p->cfg_scale > 0.f ? (const char*)logits + (size_t)rows * row_stride * e : nullptr;
+    a.dtype = dtype; a.row_stride = row_stride; a.cfg_scale = p->cfg_scale; a.rows = rows; a.V = vocab;
+    a.temperature = p->temperature; a.top_p = p->top_p; a.min_p = p->min_p; a.top_k = p->top_k;
+    a.u = u; a.tokens = tokens; a.probs = probs; a.kept = logits_out;
+    launch_sample_filtered(a, (hipStream_t)hip_stream);
+    return check_launch();
 }
 
 mulo_status mulo_profile(mulo_ctx* ctx, int32_t enable) {

@@ -200,4 +200,47 @@ void launch_logits_f32(const float* xh, const float* w, float* logits, int M, in
 void launch_attention_f32(const float* q, const float* k_cache, const float* v_cache, float* out, int B, int L, int P,
                           int n_heads, int head_dim, int max_seq, int max_batch, int layer, hipStream_t st);
 
+// ---- attention over a shared prefix and own rows, window and sinks (context_attention.hip) ----
+// Strides in elements; sizes checked by the caller.  Logical positions: prefix rows, then own rows.
+struct ContextAttn {
+    int dtype, B, L, nh, nkv, dh;
+    const void* q;
+    int64_t q_batch, q_head, q_row;
+    void* out;
+    int64_t out_batch, out_head, out_row;
+    bool frag;   // out [B * L, nh * dh] in fragment order (frag_index), bf16
+    const void *k, *v;
+    int64_t k_batch, k_head, k_row, v_batch, v_head, v_chan;
+    int rows, P;
+    const int32_t* P_seq;   // [B] or nullptr; < 0: absent
+    const void *pk, *pv;
+    int64_t pk_group, pk_head, pk_row, pv_group, pv_head, pv_chan;
+    int G, S, srows;   // S == 0: no prefix
+    int sinks, window;
+    float scale_log2;
+    // scattered queries (island passes), as launch_attention_scattered_bf16; nullptr: a block behind P own rows
+    const int32_t* pos_tab;
+    const uint8_t* hide;
+    int P0, Lblk;
+    float* part;          // scratch of part_floats floats (0: none)
+    int64_t part_floats;
+};
+size_t context_attention_floats(const ContextAttn& a);   // scratch it runs fastest with
+void launch_context_attention(const ContextAttn& a, hipStream_t st);
+
+// ---- filtered draws (sample.hip) ----
+struct SampleArgs {
+    const void *logits, *logits_u;   // rows of V entries row_stride apart; logits_u: the unconditional twins or nullptr
+    int dtype;
+    int64_t row_stride;
+    float cfg_scale;
+    int rows, V;
+    double temperature, top_p, min_p;
+    int top_k;
+    const float* u;
+    int32_t* tokens;
+    float *probs, *kept;   // [rows, V] or nullptr
+};
+void launch_sample_filtered(const SampleArgs& a, hipStream_t st);
+
 }  // namespace mulo

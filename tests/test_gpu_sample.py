@@ -1,0 +1,207 @@
+"""mulo_sample_filtered through the C ABI against its definition in float64 (oracle/sampling.py)."""
+import itertools
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2601_05149_amd as mulo
+from oracle import sampling as OS
+from tests.gpu_util import DEV, say
+
+pytestmark = pytest.mark.gpu
+INF = float("inf")
+
+
+def run(z, u, in_place=False, **kw):
+    """tokens, probs, logits of one call on z (a device tensor, any row stride)."""
+    p = mulo.make_sample_params(**kw)
+    R = z.shape[0] // 2 if kw.get("cfg_scale") else z.shape[0]
+    V = z.shape[1]
+    tokens = torch.full((R,), -7, dtype=torch.int32, device=DEV)
+    probs = torch.full((R, V), 9.0, device=DEV)
+    out = z[:R] if in_place else torch.full((R, V), 9.0, device=DEV)
+    mulo.mulo_sample_filtered(p, z, u, tokens, probs, out)
+    torch.cuda.synchronize()
+    return tokens.cpu().numpy(), probs.cpu().numpy(), out.cpu().numpy()
+
+
+def check(z, u, **kw):
+    cfg = kw.get("cfg_scale", 0.0)
+    rows = OS.row_logits(z.float().cpu().numpy(), cfg)
+    tokens, probs, out = run(z, u, **kw)
+    f = {k: v for k, v in kw.items() if k != "cfg_scale"}
+    T = kw.get("temperature", 1.0)
+    for r, row in enumerate(rows):
+        w = OS.kept(row, **f)
+        at = sorted(w)
+        assert np.array_equal(np.nonzero(np.isfinite(out[r]))[0], at), "row %d: another set stays" % r
+        # the quotient is rounded once, half a step of float32 (of its smallest numbers 2^-150), and kept finite
+        most = float(np.finfo(np.float32).max)
+        assert np.allclose(out[r][at], np.clip(row[at].astype(np.float64) / (T or 1.0), -most, most), rtol=2.0 ** -24, atol=2.0 ** -150)
+        total = sum(w.values())
+        want = np.zeros(len(row))
+        for i in at:
+            want[i] = w[i] / total
+        # a weight is an integer multiple of 2^-44 of the largest one, half a step off; the result is rounded to float32
+        assert np.all(np.abs(probs[r] - want) <= 2.0 ** -24 * want + 2.0 ** -44 + 1e-45), "row %d: probabilities" % r
+        tok, far = OS.draw(w, float(u[r]))
+        if tokens[r] != tok:                     # sums of up to 262144 weights, each half a step of 2^-44 off
+            assert far < len(row) * 2.0 ** -45, "row %d: token %d, not %d (%.3g from a border)" % (r, tokens[r], tok, far)
+    return tokens
+
+
+def rows_of(R, V, seed=0, spread=1.5, dtype=torch.float32):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(R, V, generator=g) * spread).to(dtype).to(DEV), torch.rand(R, generator=g).to(DEV)
+
+
+@pytest.mark.parametrize("V", [1, 2, 3, 5, 64, 255, 256, 257, 1000, 1024, 4097, 16384, 20001])
+def test_vocabularies(V):
+    z, u = rows_of(3, V, seed=V)
+    check(z, u)
+    check(z, u, temperature=0.7, top_k=max(1, V // 3), top_p=0.8, min_p=0.01)
+
+
+@pytest.mark.parametrize("V", [70000, 131072, 262144])
+def test_large_vocabularies(V):
+    z, u = rows_of(2, V, seed=V, spread=3.0)
+    check(z, u, top_k=500, top_p=0.9)
+    check(z, u, top_p=0.9, min_p=1e-3)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("cfg", [0.0, 4.0])
+def test_filters_and_types(dtype, cfg):
+    z, u = rows_of(8, 1500, seed=5, dtype=dtype)
+    u = u[:4].contiguous() if cfg else u
+    for T, k, p, m in itertools.product((0.0, 0.3, 1.0), (0, 1, 40, 1499, 1500, 5000), (1.0, 0.5, 1e-9), (0.0, 0.05, 1.0)):
+        check(z, u, temperature=T, top_k=k, top_p=p, min_p=m, cfg_scale=cfg)
+
+
+def test_ties_go_to_the_lowest_index():
+    g = torch.Generator().manual_seed(1)
+    z = torch.randint(0, 4, (6, 3000), generator=g).float().to(DEV)          # about 750 entries of each value
+    z[0] = 0.0                                                               # all alike
+    z[1, 100:] = -0.0
+    z[1, :100] = 0.0                                                         # the two zeros are one value
+    u = torch.rand(6, generator=g).to(DEV)
+    for k, p in ((1, 1.0), (10, 1.0), (800, 1.0), (0, 0.1), (0, 0.7), (900, 0.95), (900, 0.999), (751, 0.5), (2999, 0.9999)):
+        check(z, u, top_k=k, top_p=p)
+    tokens, _, out = run(z, u, temperature=0.0)
+    assert tokens[0] == 0 and all((out[r] > -INF).sum() == 1 for r in range(6))
+
+
+def test_masked_entries():
+    z, u = rows_of(8, 700, seed=2)
+    z[0] = -INF                                   # nothing to draw
+    z[1, 1:] = -INF                               # one entry
+    z[2, 5:] = float("nan")                       # NaN is masked
+    z[3] = float("nan")
+    z[4, 100:600] = torch.finfo(torch.float32).min
+    z[5] = torch.finfo(torch.float32).min         # a mask of the type's lowest value over the whole row: a flat distribution
+    z[6, ::2] = -INF
+    z[7, 3:] = -3.0e38
+    for kw in (dict(), dict(top_k=20), dict(top_p=0.6), dict(min_p=0.2), dict(top_k=300, top_p=0.9, min_p=0.01), dict(temperature=0.0), dict(temperature=1e-3)):
+        tokens = check(z, u, **kw)
+        assert tokens[0] == -1 and tokens[3] == -1 and tokens[1] == 0
+
+
+def test_infinite_entries_share_the_mass():
+    z, u = rows_of(2, 300, seed=3)
+    z[0, [7, 200]] = INF
+    u[0] = 0.75
+    z[1, 9] = INF
+    tokens, probs, out = run(z, u)
+    assert np.isfinite(out).all()
+    assert tokens[0] == 200 and tokens[1] == 9
+    assert probs[0, 7] == 0.5 and probs[0, 200] == 0.5 and probs[1, 9] == 1.0 and probs.sum() == 2.0
+
+
+def test_uniforms_at_and_beyond_the_ends():
+    z, _ = rows_of(1, 100, seed=4)
+    z = z.repeat(6, 1)
+    u = torch.tensor([0.0, 1.0 - 2.0 ** -24, 1.0, -1.0, float("nan"), INF], device=DEV)
+    tokens = check(z, u)
+    assert tokens[0] == 0 and tokens[3] == 0 and tokens[4] == 0 and tokens[1] == tokens[2] == tokens[5]
+
+
+def test_strides_alignment_and_outputs_in_place():
+    z, u = rows_of(5, 1001, seed=6)
+    kw = dict(temperature=0.8, top_k=300, top_p=0.9)
+    want = run(z, u, **kw)
+    wide = torch.full((5, 1301), 50.0, device=DEV)
+    for first in (0, 1, 3):
+        wide.fill_(50.0)
+        wide[:, first:first + 1001] = z
+        got = run(wide[:, first:first + 1001], u, **kw)
+        assert all(np.array_equal(a, b) for a, b in zip(want, got))
+    got = run(z.clone(), u, in_place=True, **kw)
+    assert all(np.array_equal(a, b) for a, b in zip(want, got))
+    zz, uu = rows_of(6, 1000, seed=7)
+    want = run(zz, uu[:3].contiguous(), cfg_scale=4.0, **kw)
+    got = run(zz, uu[:3].contiguous(), in_place=True, cfg_scale=4.0, **kw)
+    assert all(np.array_equal(a, b) for a, b in zip(want, got))
+    # outputs one at a time
+    p = mulo.make_sample_params(**kw)
+    want = run(z, u, **kw)
+    t, pr, lo = torch.empty(5, dtype=torch.int32, device=DEV), torch.empty(5, 1001, device=DEV), torch.empty(5, 1001, device=DEV)
+    mulo.mulo_sample_filtered(p, z, u, tokens=t)
+    mulo.mulo_sample_filtered(p, z, probs=pr)
+    mulo.mulo_sample_filtered(p, z, logits_out=lo)
+    torch.cuda.synchronize()
+    assert np.array_equal(t.cpu().numpy(), want[0]) and np.array_equal(pr.cpu().numpy(), want[1]) and np.array_equal(lo.cpu().numpy(), want[2])
+
+
+def test_skewed_values():
+    """Values far apart, a few large outliers over a dense bulk, and a bulk that float32 hardly tells apart: the search for the
+    border may not rely on how values are spread."""
+    g = torch.Generator().manual_seed(8)
+    V = 5000
+    z = torch.empty(6, V)
+    z[0] = torch.randn(V, generator=g) * 1e4
+    z[1] = torch.randn(V, generator=g) * 1e-5
+    z[1, 17] = 1000.0
+    z[2] = 1.0 + torch.randint(0, 3, (V,), generator=g) * 2.0 ** -23
+    z[3] = torch.randn(V, generator=g) * 1e30
+    z[4] = torch.randn(V, generator=g) * 1e-38
+    z[5] = -torch.rand(V, generator=g).pow(8) * 100
+    z, u = z.to(DEV), torch.rand(6, generator=g).to(DEV)
+    for kw in (dict(), dict(top_k=1), dict(top_k=37), dict(top_k=2500), dict(top_p=0.3), dict(top_p=0.999), dict(top_k=1000, top_p=0.9), dict(min_p=0.1)):
+        check(z, u, **kw)
+
+
+def test_distribution_of_draws():
+    """Uniforms on a grid land on every entry in proportion to its probability."""
+    z, _ = rows_of(1, 50, seed=9)
+    n = 4096
+    u = (torch.arange(n, dtype=torch.float32) / n).to(DEV)
+    p = mulo.make_sample_params(top_k=30, top_p=0.95)
+    tokens, probs = torch.empty(n, dtype=torch.int32, device=DEV), torch.empty(n, 50, device=DEV)
+    mulo.mulo_sample_filtered(p, z.repeat(n, 1), u, tokens, probs)
+    counts = torch.bincount(tokens.long(), minlength=50).double() / n
+    assert (counts - probs[0].double()).abs().max().item() <= 1.0 / n + 1e-6      # a grid of n points: off by at most one each
+
+
+def test_captured_and_replayed():
+    z, u = rows_of(4, 3000, seed=10)
+    p = mulo.make_sample_params(temperature=0.9, top_k=500, top_p=0.9)
+    side = torch.cuda.Stream()
+    tokens = torch.empty(4, dtype=torch.int32, device=DEV)
+    with torch.cuda.stream(side):
+        mulo.mulo_sample_filtered(p, z, u, tokens)
+        side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        mulo.mulo_sample_filtered(p, z, u, tokens)
+    with torch.cuda.stream(side):
+        for seed in (11, 12, 13):
+            z2, u2 = rows_of(4, 3000, seed=seed)
+            z.copy_(z2)
+            u.copy_(u2)
+            tokens.fill_(-7)
+            graph.replay()
+            side.synchronize()
+            assert np.array_equal(tokens.cpu().numpy(), run(z2, u2, temperature=0.9, top_k=500, top_p=0.9)[0])
+    del graph
+    say("  3 replays")
