@@ -1,113 +1,647 @@
-// Attention over a prefix that sequences share and the rows each has of its own, with a window and sinks.
+// Attention over a prefix that the sequences of a group share and the rows that each sequence has of its own, with an
+// optional window and sinks: the query at position p sees t <= p with t < sinks or p - t < window.
+//
+// One pass over the keys with a running maximum m and sum l per query: of a tile of keys with scores s (in units of
+// log2), m' = max(m, max s), o = o 2^(m - m') + sum 2^(s - m') v, l = l 2^(m - m') + sum 2^(s - m'); out = o / l.  Partial
+// results (o, m, l) over disjoint sets of keys join as sum o_i 2^(m_i - M) / sum l_i 2^(m_i - M), M = max m_i.
+//
+// A wavefront owns 32 queries and computes S^T = K Q^T and O^T = V^T P^T with 32x32 matrix instructions, so that a
+// lane owns ONE query: the reductions of the softmax stay inside the lane (and its twin 32 lanes on), and the exponentials
+// are already laid out as the second operand of the second product.  Tiles of K and V^T go from memory to LDS directly,
+// double buffered, and are shared by the wavefronts of a workgroup.
+//
+// What a workgroup's queries are (`role`):
+//   whole   one sequence; its tiles are those of its prefix that it sees, then its own
+//   stacked few queries per sequence behind a shared prefix: the rows of all sequences of a group go over the prefix
+//           together (prefix workgroups), each sequence's over its own rows (own workgroups, the same launch), and
+//           k_context_join joins the partial results.  The prefix is read once per 128 stacked rows.
+// Keys of few queries are dealt to several workgroups as well, whose shares k_context_join joins.
 #include <hip/hip_bf16.h>
+
+#include <utility>
 
 #include "mulo_internal.h"
 
 namespace mulo {
 namespace {
 
-constexpr int NTH = 256;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((address_space(3))) void lds_void;
+typedef const __attribute__((address_space(1))) void glb_void;
 
-template <class T> __device__ __forceinline__ float to_f32(T v);
-template <> __device__ __forceinline__ float to_f32<float>(float v) { return v; }
-template <> __device__ __forceinline__ float to_f32<__hip_bfloat16>(__hip_bfloat16 v) { return __bfloat162float(v); }
-template <class T> __device__ __forceinline__ T from_f32(float v);
-template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
-template <> __device__ __forceinline__ __hip_bfloat16 from_f32<__hip_bfloat16>(float v) { return __float2bfloat16(v); }
-
-__device__ __forceinline__ float block_reduce(float v, float* red, bool is_max) {
-    for (int o = 32; o > 0; o >>= 1) {
-        const float n = __shfl_xor(v, o);
-        v = is_max ? fmaxf(v, n) : v + n;
-    }
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    float r = red[0];
-    for (int i = 1; i < NTH / 64; ++i) r = is_max ? fmaxf(r, red[i]) : r + red[i];
-    return r;
+template <class F, int... Is>
+__device__ __forceinline__ void static_for_impl(F&& f, std::integer_sequence<int, Is...>) {
+    (f(std::integral_constant<int, Is>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void static_for(F&& f) {
+    static_for_impl(static_cast<F&&>(f), std::make_integer_sequence<int, N>{});
 }
 
-// one workgroup per query, 256 keys at a time, running maximum and sum
+// 16 bytes of an operand per lane: 8 bf16 feed one 32x32x16 instruction, 4 float32 four 32x32x2 ones (which of the
+// contraction's indexes a lane's elements are is the same for both operands, so it does not matter)
+template <class T> struct Chunk;
+template <> struct Chunk<__bf16> {
+    typedef bf16x8 type;
+    static __device__ __forceinline__ f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Chunk<float> {
+    typedef f32x4 type;
+    static __device__ __forceinline__ f32x16 mma(f32x4 a, f32x4 b, f32x16 c) {
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x, b.x, c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.y, b.y, c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.z, b.z, c, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_32x32x2f32(a.w, b.w, c, 0, 0, 0);
+    }
+};
+
+constexpr float LAZY_EXP = 8.0f;     // the reference of the exponentials moves once the maximum has outgrown it by 2^8 (bf16; see attention.hip)
+constexpr int MAX_SLOTS = 64;        // shares of a query that k_context_join joins: a lane each
+constexpr int STACK_ROWS = 64;       // queries per sequence and key head up to which sequences are stacked over their prefix
+
+// How a launch is laid out (host).
+struct Plan {
+    bool stacked;      // prefix and own workgroups
+    bool by_kv;        // the queries of a workgroup are those of all heads of a key head (else of one head)
+    int heads;         // heads, or key heads
+    int n;             // queries of a (sequence, head)
+    int tiles;         // of them: workgroups
+    int prefix_tiles;  // stacked: tiles of the stacked rows of a (group, key head)
+    int split;         // shares of the keys (stacked: of the own rows)
+    int prefix_split;  // stacked: shares of the prefix
+    int prefix_wgs;    // workgroups of the prefix (the first ones of the grid)
+};
+struct Args : ContextAttn, Plan {
+    float* ml;         // [slots][B nh L] pairs: maximum and sum, behind the [slots][B nh L][dh] outputs in part
+};
+
+template <class T, int DH, int BQ, int BKV, int NTH>
+__global__ __launch_bounds__(NTH, DH * BKV * (int)sizeof(T) <= 16384 ? 2 : 1) void k_context(const Args a) {
+    typedef typename Chunk<T>::type chunk;
+    constexpr bool BF16 = sizeof(T) == 2;
+    constexpr int E = 16 / sizeof(T);      // elements of a chunk
+    constexpr int NKK = DH / (2 * E);      // pairs of chunks along a row of K
+    constexpr int NDB = DH / 32;           // 32-row blocks of O^T
+    constexpr int NKB = BKV / 32;          // 32-key blocks of S^T
+    constexpr int NKS = BKV / (2 * E);     // pairs of chunks along a row of V^T
+    constexpr int NW = NTH / 64;
+    constexpr int KRB = DH * sizeof(T), VRB = BKV * sizeof(T);            // bytes of a row of the K tile, of the V^T tile
+    constexpr int KT = BKV * KRB, BUF = KT + DH * VRB;
+    constexpr int LK = KT / 1024 / NW, LV = DH * VRB / 1024 / NW;         // loads of a wavefront per tile, a KB of whole rows each
+    constexpr int RK = 1024 / KRB, RV = 1024 / VRB;                       // rows of a load
+    static_assert(LK * NW * 1024 == KT && LV * NW * 1024 == DH * VRB, "whole loads per wavefront");
+
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];  // [2][BUF]
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, lh = lane >> 5;
+    const int group = a.nh / a.nkv;
+    // ---- which queries, which share of which keys
+    const bool of_prefix = a.stacked && (int)blockIdx.x < a.prefix_wgs;
+    int b = 0, hd, qt, split, nsplit, slot, n, g;
+    if (of_prefix) {      // consecutive ids: consecutive (group, head)s, one XCD each; the row tiles of one lie on one XCD
+        const int gk = a.G * a.nkv, bid = blockIdx.x;
+        const int in = bid % gk;
+        g = in / a.nkv; hd = in % a.nkv;
+        qt = bid / gk % a.prefix_tiles;
+        split = slot = bid / (gk * a.prefix_tiles);
+        nsplit = a.prefix_split;
+        n = a.B / a.G * a.n;
+    } else {              // all query tiles of a (sequence, head) on one XCD, next to each other; long tiles first
+        const int nbh = a.B * a.heads, bid = ((int)blockIdx.x - (a.stacked ? a.prefix_wgs : 0)) % (a.tiles * nbh);
+        split = ((int)blockIdx.x - (a.stacked ? a.prefix_wgs : 0)) / (a.tiles * nbh);
+        int bh;
+        if ((nbh & 7) == 0) {
+            const int s = bid >> 3;
+            qt = a.tiles - 1 - s % a.tiles;
+            bh = (s / a.tiles) * 8 + (bid & 7);
+        } else {
+            qt = a.tiles - 1 - bid % a.tiles;
+            bh = bid / a.tiles;
+        }
+        hd = bh % a.heads;
+        b = bh / a.heads;
+        g = b / (a.B / a.G);
+        slot = split + (a.stacked ? a.prefix_split : 0);
+        nsplit = a.split;
+        n = a.n;
+    }
+    const int kvh = a.by_kv ? hd : hd / group;
+    const bool scattered = a.pos_tab != nullptr;
+    // ---- this lane's query (the last one again past the end; such lanes do not store)
+    const int r0 = qt * BQ + wave * 32, r_raw = r0 + l32, r = r_raw < n ? r_raw : n - 1;
+    const int lb = of_prefix ? g * (a.B / a.G) + r / a.n : b;
+    const int in_seq = of_prefix ? r % a.n : r;
+    const int lhd = a.by_kv ? hd * group + in_seq / a.L : hd, lj = a.by_kv ? in_seq % a.L : in_seq;
+    const bool wave_live = r0 < n;
+    int P = a.P;
+    if (a.P_seq && !of_prefix) {
+        P = a.P_seq[b];
+        P = P < a.rows - a.L ? P : a.rows - a.L;
+    }
+    const bool absent = !of_prefix && P < 0;     // uniform over the workgroup
+    int pos = P + lj;                            // own row; of the prefix's workgroups only with a window (then P is everyone's)
+    bool active = true;
+    if (scattered) {
+        const int row = a.pos_tab[(int64_t)lb * a.L + lj];
+        active = row >= 0;
+        pos = active ? row : a.P0;
+    }
+    // own rows of the queries: of this wavefront, of the workgroup (bounds)
+    auto first_last = [&](int ra, int rb, int& lo, int& hi) {
+        rb = rb < n ? rb : n - 1;
+        const bool one = !a.by_kv || ra / a.L == rb / a.L;       // within a head the queries are consecutive
+        lo = P + (one ? (a.by_kv ? ra % a.L : ra) : 0);
+        hi = P + (one ? (a.by_kv ? rb % a.L : rb) : a.L - 1);
+        if (scattered) { lo = a.P0; hi = a.P0 + a.Lblk - 1; }
+    };
+    int w_min, w_max, p_min, p_max;
+    first_last(r0, r0 + 31, w_min, w_max);
+    first_last(qt * BQ, qt * BQ + BQ - 1, p_min, p_max);
+
+    // ---- which tiles: of either source the head [0, a) of the sinks and [lo, end) of the window
+    const int S = a.S, window = a.window;
+    int pre_a = 0, pre_lo = 0, own_a = 0, own_lo = 0, np1 = 0, np = 0, tp2 = 0, no1 = 0, no = 0, to2 = 0;
+    const int own_end = p_max + 1;
+    if (S > 0 && (of_prefix || !a.stacked)) {
+        if (window) {
+            const int lo = S + p_min - window + 1;       // S + p_min < 2^25
+            pre_lo = lo < 0 ? 0 : lo < S ? lo : S;
+            pre_a = a.sinks < pre_lo ? a.sinks : pre_lo;
+        }
+        np1 = (pre_a + BKV - 1) / BKV;
+        tp2 = pre_lo / BKV > np1 ? pre_lo / BKV : np1;
+        const int more = pre_lo < S ? (S + BKV - 1) / BKV - tp2 : 0;
+        np = np1 + (more > 0 ? more : 0);
+    }
+    if (!of_prefix) {
+        if (window) {
+            const int lo = p_min - window + 1, s = a.sinks - S;
+            own_lo = lo < 0 ? 0 : lo;
+            own_a = s < 0 ? 0 : s < own_lo ? s : own_lo;
+        }
+        no1 = (own_a + BKV - 1) / BKV;
+        to2 = own_lo / BKV > no1 ? own_lo / BKV : no1;
+        const int more = (own_end + BKV - 1) / BKV - to2;
+        no = no1 + (more > 0 ? more : 0);
+    }
+    const int n_tiles = absent ? 0 : np + no;
+    const int per = (n_tiles + nsplit - 1) / nsplit;
+    const int t_begin = split * per, t_end = t_begin + per < n_tiles ? t_begin + per : n_tiles;
+    const int64_t all_rows = (int64_t)a.B * a.nh * a.L;
+    const bool partial = a.stacked || a.split > 1;
+    const int64_t out_row = ((int64_t)lb * a.nh + lhd) * a.L + lj;
+    auto store_out = [&](int i, int g4, f32x4 w) {       // channels i 32 + g4 8 + lh 4 .. + 3 of this lane's query
+        const int c = i * 32 + g4 * 8 + lh * 4;
+        T* const op = reinterpret_cast<T*>(a.out) + (a.frag ? frag_index(lb * a.L + lj, lhd * DH + c, a.nh * DH)      // 4 | c: inside a run of 8
+                                                            : lb * a.out_batch + lhd * a.out_head + lj * a.out_row + c);
+        if constexpr (BF16) {
+            bf16x4 t;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t[e] = (__bf16)w[e];
+            *reinterpret_cast<bf16x4*>(op) = t;
+        } else {
+            *reinterpret_cast<f32x4*>(op) = w;
+        }
+    };
+    if (t_begin >= t_end) {    // uniform over the workgroup, before any barrier: nothing to see
+        if (r_raw < n) {
+            if (partial) {
+                if (lh == 0) *reinterpret_cast<float2*>(a.ml + 2 * (slot * all_rows + out_row)) = make_float2(-__builtin_huge_valf(), 0.f);
+            } else {
+#pragma unroll
+                for (int i = 0; i < NDB; ++i)
+#pragma unroll
+                    for (int g4 = 0; g4 < 4; ++g4) store_out(i, g4, f32x4{0.f, 0.f, 0.f, 0.f});
+            }
+        }
+        return;
+    }
+
+    chunk qf[NKK];
+    {
+        const T* qp = reinterpret_cast<const T*>(a.q) + lb * a.q_batch + lhd * a.q_head + lj * a.q_row + lh * E;
+#pragma unroll
+        for (int kk = 0; kk < NKK; ++kk) qf[kk] = *reinterpret_cast<const chunk*>(qp + kk * 2 * E);
+    }
+
+    // Tiles go from memory to LDS directly.  16-byte chunk c of row r sits at chunk position c ^ key(r): 16 lanes that read
+    // the same chunk of 16 rows touch every bank once.
+    auto key_of = [](int r, int row_bytes) { return row_bytes >= 256 ? r & 15 : (r >> 1) & 7; };
+    const int krow = wave * RK + lane / (64 / RK), vrow = wave * RV + lane / (64 / RV);
+    static_assert(NW * RV % 16 == 0, "the key of a lane's rows of V^T");
+    const int vchunk = lane % (64 / RV) ^ key_of(vrow, VRB);
+    const unsigned char* const pk = reinterpret_cast<const unsigned char*>(reinterpret_cast<const T*>(a.pk) + g * a.pk_group + kvh * a.pk_head);
+    const unsigned char* const pv = reinterpret_cast<const unsigned char*>(reinterpret_cast<const T*>(a.pv) + g * a.pv_group + kvh * a.pv_head + (int64_t)wave * RV * a.pv_chan);
+    const unsigned char* const ok = reinterpret_cast<const unsigned char*>(reinterpret_cast<const T*>(a.k) + b * a.k_batch + kvh * a.k_head);
+    const unsigned char* const ov = reinterpret_cast<const unsigned char*>(reinterpret_cast<const T*>(a.v) + b * a.v_batch + kvh * a.v_head + (int64_t)wave * RV * a.v_chan);
+    auto to_lds = [](const unsigned char* base, uint32_t off, unsigned char* lds) {
+        __builtin_amdgcn_global_load_lds((glb_void*)(base + off), (lds_void*)lds, 16, 0, 0);
+    };
+    auto tile_of = [&](int i) { return i < np ? (i < np1 ? i : tp2 + i - np1) : (i - np < no1 ? i - np : to2 + (i - np) - no1); };
+    // A tile that runs past the end of its cache takes the last row and columns again: nothing sees those keys.
+    auto load_kv = [&](int i) {
+        const bool pre = i < np;
+        const int t = tile_of(i);
+        unsigned char* const lds = smem + (i & 1) * BUF + wave * 1024;
+        const uint32_t k_row = (uint32_t)(pre ? a.pk_row : a.k_row) * sizeof(T);
+        const int64_t v_chan = (pre ? a.pv_chan : a.v_chan) * (int64_t)sizeof(T);
+        const int left = (pre ? a.srows : a.rows) - t * BKV;
+        const unsigned char* const kt = (pre ? pk : ok) + (int64_t)t * BKV * k_row;
+        const unsigned char* const vt = (pre ? pv : ov) + (int64_t)t * VRB;
+#pragma unroll
+        for (int x = 0; x < LK; ++x) {
+            const int row = krow + x * NW * RK;
+            to_lds(kt, (uint32_t)(row < left ? row : left - 1) * k_row + ((lane % (64 / RK)) ^ key_of(row, KRB)) * 16, lds + x * NW * 1024);
+        }
+        const uint32_t vo = (uint32_t)(lane / (64 / RV)) * (uint32_t)v_chan + (uint32_t)(vchunk * E < left - E ? vchunk * E : left - E) * (uint32_t)sizeof(T);
+#pragma unroll
+        for (int x = 0; x < LV; ++x) to_lds(vt + x * (NW * RV) * v_chan, vo, lds + KT + x * NW * 1024);
+    };
+    auto meet = [&]() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+    // Columns of V^T that no query of the workgroup sees may hold anything: their probabilities are 0, and 0 * NaN must not reach
+    // the accumulators.  Between the landing of a tile and the barrier that shows it to the others, every lane clears
+    // those of the bytes it has loaded itself.
+    auto clear_unseen = [&](int i) {
+        const bool pre = i < np;
+        const int k0 = tile_of(i) * BKV, end = pre ? S : own_end, lo = pre ? pre_lo : own_lo, head = pre ? pre_a : own_a;
+        if (k0 + BKV > end || (k0 < lo && k0 + BKV > head)) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            const int key = k0 + vchunk * E;
+            auto seen = [&](int e) { return key + e < end && (key + e < head || key + e >= lo); };
+            auto keep = [&](int w) -> uint32_t {
+                if constexpr (BF16) return (seen(2 * w) ? 0xFFFFu : 0u) | (seen(2 * w + 1) ? 0xFFFF0000u : 0u);
+                else return seen(w) ? 0xFFFFFFFFu : 0u;
+            };
+            const u32x4 mask = {keep(0), keep(1), keep(2), keep(3)};
+#pragma unroll
+            for (int x = 0; x < LV; ++x) {
+                u32x4* const at = reinterpret_cast<u32x4*>(smem + (i & 1) * BUF + KT + (x * NW + wave) * 1024 + lane * 16);
+                *at = *at & mask;
+            }
+        }
+    };
+
+    f32x16 o[NDB];
+#pragma unroll
+    for (int i = 0; i < NDB; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+    float m_run = -__builtin_huge_valf(), l_run = 0.f;
+
+    // bf16: row rho of a K block is fed key rho with bits 2 and 3 swapped, so that a lane's accumulators cover 8 consecutive keys
+    const int kperm = BF16 ? (l32 & 0x13) | ((l32 & 4) << 1) | ((l32 & 8) >> 1) : l32;
+    auto key_at = [&](int kb, int e) {       // accumulator e of block kb holds this key of the tile
+        return BF16 ? kb * 32 + 16 * (e >> 3) + 8 * lh + (e & 7) : kb * 32 + 8 * (e >> 2) + 4 * lh + (e & 3);
+    };
+    const int kfrag = kperm * KRB + (lh ^ key_of(kperm, KRB)) * 16, vfrag = l32 * VRB + (lh ^ key_of(l32, VRB)) * 16;
+    f32x16 s[NKB];               // the scores of a tile, then
+    float m_safe = 0.f, alpha = 1.f;   // the reference of its exponentials and the factor of what has been added up before it
+    auto score = [&](int i) {
+        const bool pre = i < np;
+        const int kv0 = tile_of(i) * BKV;
+        const unsigned char* const kt = smem + (i & 1) * BUF;
+#pragma unroll
+        for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
+        // NKB independent chains, the fragments of a step requested during the step before it
+        chunk kf[2][NKB];
+#pragma unroll
+        for (int kb = 0; kb < NKB; ++kb) kf[0][kb] = *reinterpret_cast<const chunk*>(kt + kfrag + kb * 32 * KRB);
+        static_for<NKK>([&](auto kc) {
+            constexpr int kk = decltype(kc)::value;
+            static_for<NKB>([&](auto bc) {
+                constexpr int kb = decltype(bc)::value;
+                if constexpr (kk + 1 < NKK) kf[(kk + 1) & 1][kb] = *reinterpret_cast<const chunk*>(kt + (kfrag ^ ((kk + 1) << 5)) + kb * 32 * KRB);
+                s[kb] = Chunk<T>::mma(kf[kk & 1][kb], qf[kk], s[kb]);
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        });
+        const int last = pre ? S - 1 : w_min;                            // key up to which all queries of the wavefront see
+        if (kv0 + BKV - 1 > last) {
+            const int lim = pre ? S - 1 : pos;
+#pragma unroll
+            for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[kb][e] = kv0 + key_at(kb, e) <= lim ? s[kb][e] : -__builtin_huge_valf();
+        }
+        if (window) {
+            const int shift = (pre ? S : 0) - window, sinks = a.sinks - (pre ? 0 : S);
+            if (kv0 + BKV > sinks && kv0 <= w_max + shift) {             // some key may lie between the sinks and a window
+                const int before = pos + shift;                          // the last one in front of this query's window
+#pragma unroll
+                for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int key = kv0 + key_at(kb, e);
+                        s[kb][e] = key < sinks || key > before ? s[kb][e] : -__builtin_huge_valf();
+                        if ((e & 3) == 3) __builtin_amdgcn_sched_barrier(0);
+                    }
+            }
+        }
+        if constexpr (BF16 && BKV == 64) {
+            if (a.hide && !pre) {      // scattered queries: rows of positions that are not settled yet, the query's own excepted
+                const int t = kv0 + lane - a.P0;
+                const unsigned long long hidden = __ballot(t >= 0 && t < a.Lblk && a.hide[(int64_t)b * a.Lblk + t] != 0);
+                if (hidden != 0) {
+#pragma unroll
+                    for (int kb = 0; kb < NKB; ++kb) {
+                        const uint32_t mine = (uint32_t)(hidden >> (kb * 32)) >> (8 * lh);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            if (((mine >> (16 * (e >> 3) + (e & 7))) & 1u) && kv0 + key_at(kb, e) < pos) s[kb][e] = -__builtin_huge_valf();
+                            if ((e & 3) == 3) __builtin_amdgcn_sched_barrier(0);
+                        }
+                    }
+                }
+            }
+        }
+        float mx = -__builtin_huge_valf();
+#pragma unroll
+        for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[kb][e]);
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float mxs = mx * a.scale_log2;
+        const float m_new = mxs > m_run + LAZY_EXP ? mxs : m_run;
+        // a query that has seen no key yet keeps -inf as its maximum: exponents are then taken against 0, and every
+        // term is exp2(-inf) = 0 instead of NaN
+        m_safe = m_new == -__builtin_huge_valf() ? 0.f : m_new;
+        alpha = __builtin_amdgcn_exp2f(m_run - m_safe);
+        m_run = m_new;
+    };
+    auto output = [&](int i) {
+        const unsigned char* const vt = smem + (i & 1) * BUF + KT;
+        float ps = 0.f;
+        auto rescale = [&]() {     // only when some query of the wavefront raised its maximum
+            if (!__all(alpha == 1.0f)) {
+#pragma unroll
+                for (int d = 0; d < NDB; ++d)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[d][e] *= alpha;
+            }
+        };
+        if constexpr (BF16) {
+            // keys kv0 + 16 ks .. + 15 per step ks; the exponentials of step ks + 1 and its V^T fragments go between the
+            // matrix instructions of step ks, in three stages a slot apart
+            chunk pf[2], vf[2][NDB];
+            float x[2][2], p[2][2];
+            auto arg = [&](auto gc) {
+                constexpr int g = decltype(gc)::value, ks = g / 4, e = 2 * (g % 4);
+                if constexpr (g < BKV / 4) {
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) x[g & 1][q] = __builtin_fmaf(s[ks >> 1][(ks & 1) * 8 + e + q], a.scale_log2, -m_safe);
+                }
+            };
+            auto expo = [&](auto gc) {
+                constexpr int g = decltype(gc)::value;
+                if constexpr (g < BKV / 4) {
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) p[g & 1][q] = __builtin_amdgcn_exp2f(x[g & 1][q]);
+                }
+            };
+            auto take = [&](auto gc) {
+                constexpr int g = decltype(gc)::value, ks = g / 4, e = 2 * (g % 4);
+                if constexpr (g < BKV / 4) {
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        ps += p[g & 1][q];
+                        pf[ks & 1][e + q] = (__bf16)p[g & 1][q];
+                    }
+                }
+            };
+#pragma unroll
+            for (int d = 0; d < NDB; ++d) vf[0][d] = *reinterpret_cast<const chunk*>(vt + vfrag + d * 32 * VRB);
+            static_for<4>([&](auto gc) { arg(gc); expo(gc); take(gc); });
+            arg(std::integral_constant<int, 4>{});
+            expo(std::integral_constant<int, 4>{});
+            arg(std::integral_constant<int, 5>{});
+            rescale();
+            static_for<NKS>([&](auto kc) {
+                constexpr int ks = decltype(kc)::value, nxt = ks + 1 < NKS ? ks + 1 : ks;
+                static_for<NDB>([&](auto ic) {
+                    constexpr int d = decltype(ic)::value, m = 4 / NDB;   // pairs per slot
+                    if constexpr (nxt > ks) vf[nxt & 1][d] = *reinterpret_cast<const chunk*>(vt + (vfrag ^ (nxt << 5)) + d * 32 * VRB);
+                    static_for<m>([&](auto qc) {
+                        constexpr int g = 4 * ks + d * m + decltype(qc)::value + 4;
+                        take(std::integral_constant<int, g>{});
+                        expo(std::integral_constant<int, g + 1>{});
+                        arg(std::integral_constant<int, g + 2>{});
+                    });
+                    o[d] = Chunk<T>::mma(vf[ks & 1][d], pf[ks & 1], o[d]);
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            });
+        } else {
+            rescale();
+#pragma unroll
+            for (int ks = 0; ks < NKS; ++ks) {
+                chunk p;
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[ks / (16 / E)][ks % (16 / E) * E + e], a.scale_log2, -m_safe));
+                    ps += p[e];
+                }
+#pragma unroll
+                for (int d = 0; d < NDB; ++d) o[d] = Chunk<T>::mma(*reinterpret_cast<const chunk*>(vt + (vfrag ^ (ks << 5)) + d * 32 * VRB), p, o[d]);
+            }
+        }
+        l_run = l_run * alpha + ps;
+    };
+    // does some query of the wavefront see some key of the tile?
+    auto in_sight = [&](int i) {
+        const bool pre = i < np;
+        const int kv0 = tile_of(i) * BKV;
+        if (!pre && kv0 > w_max) return false;
+        return !window || kv0 < a.sinks - (pre ? 0 : S) || kv0 + BKV - 1 > w_min + (pre ? S : 0) - window;
+    };
+    load_kv(t_begin);
+    clear_unseen(t_begin);
+#pragma unroll
+    for (int kk = 0; kk < NKK; ++kk) asm volatile("" : "+v"(qf[kk]));   // wait for the queries here: among the tiles' loads that wait is for those as well
+    meet();
+    for (int t = t_begin; t < t_end; ++t) {
+        if (t + 1 < t_end) load_kv(t + 1);   // everybody has read the buffer: the barrier at the end of the tile before
+        if (wave_live && in_sight(t)) {
+            score(t);
+            output(t);
+        }
+        if (t + 1 < t_end) {
+            clear_unseen(t + 1);
+            meet();
+        }
+    }
+
+    l_run += __shfl_xor(l_run, 32);
+    if (r_raw >= n) return;
+    if (partial) {
+        float* const pq = a.part + (slot * all_rows + out_row) * DH;
+#pragma unroll
+        for (int i = 0; i < NDB; ++i)
+#pragma unroll
+            for (int g4 = 0; g4 < 4; ++g4)
+                *reinterpret_cast<f32x4*>(pq + i * 32 + g4 * 8 + lh * 4) = f32x4{o[i][g4 * 4], o[i][g4 * 4 + 1], o[i][g4 * 4 + 2], o[i][g4 * 4 + 3]};
+        if (lh == 0) *reinterpret_cast<float2*>(a.ml + 2 * (slot * all_rows + out_row)) = make_float2(m_run, l_run);
+        return;
+    }
+    const float inv = active && l_run > 0.f ? 1.0f / l_run : 0.f;
+#pragma unroll
+    for (int i = 0; i < NDB; ++i)
+#pragma unroll
+        for (int g4 = 0; g4 < 4; ++g4)
+            store_out(i, g4, f32x4{o[i][g4 * 4] * inv, o[i][g4 * 4 + 1] * inv, o[i][g4 * 4 + 2] * inv, o[i][g4 * 4 + 3] * inv});
+}
+
+// A wavefront joins the shares of a query: lane s takes the weight of share s, then every lane DH / 64 channels.  Rows of absent
+// sequences and unused slots are zeros.
+constexpr int JOIN_WAVES = 4;
 template <class T, int DH>
-__global__ __launch_bounds__(NTH) void k_context_rows(const ContextAttn a) {
-    __shared__ float qs[DH], ps[NTH], red[NTH / 64], os[NTH];
-    const int tid = threadIdx.x;
-    const int j = blockIdx.x % a.L, h = (blockIdx.x / a.L) % a.nh, b = blockIdx.x / (a.L * a.nh);
-    const int kvh = h / (a.nh / a.nkv), g = b / (a.B / a.G);
-    int own = (a.P_seq ? a.P_seq[b] : a.P);
-    own = own < a.rows - a.L ? own : a.rows - a.L;
-    bool absent = own < 0;
-    own += j;
-    if (a.pos_tab) {
-        own = a.pos_tab[(int64_t)b * a.L + j];
-        absent = own < 0;
-    }
-    const T* q = (const T*)a.q + b * a.q_batch + h * a.q_head + j * a.q_row;
-    const T* k = (const T*)a.k + b * a.k_batch + kvh * a.k_head;
-    const T* v = (const T*)a.v + b * a.v_batch + kvh * a.v_head;
-    const T* pk = (const T*)a.pk + g * a.pk_group + kvh * a.pk_head;
-    const T* pv = (const T*)a.pv + g * a.pv_group + kvh * a.pv_head;
-    if (tid < DH) qs[tid] = to_f32<T>(q[tid]);
-    __syncthreads();
-    const int p = a.S + own;
-    float m = -__builtin_huge_valf(), l = 0.f, o = 0.f;
-    const int c = tid % DH, part = tid / DH, parts = NTH / DH;
-    for (int t0 = 0; !absent && t0 <= p; t0 += NTH) {
-        const int t = t0 + tid;
-        bool see = t <= p && (a.window == 0 || t < a.sinks || p - t < a.window);
-        if (a.hide && see && t >= a.S && t < p) {
-            const int x = t - a.S - a.P0;
-            if (x >= 0 && x < a.Lblk && a.hide[(int64_t)b * a.Lblk + x]) see = false;
+__global__ __launch_bounds__(64 * JOIN_WAVES) void k_context_join(const Args a, int slots) {
+    constexpr int C = DH / 64;
+    const int64_t all_rows = (int64_t)a.B * a.nh * a.L, row = (int64_t)blockIdx.x * JOIN_WAVES + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    if (row >= all_rows) return;
+    const int j = row % a.L, h = (row / a.L) % a.nh, b = row / ((int64_t)a.L * a.nh);
+    const bool absent = (a.P_seq && a.P_seq[b] < 0) || (a.pos_tab && a.pos_tab[(int64_t)b * a.L + j] < 0);
+    const float2 ml = lane < slots ? *reinterpret_cast<const float2*>(a.ml + 2 * (lane * all_rows + row)) : make_float2(-__builtin_huge_valf(), 0.f);
+    float M = ml.x;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
+    const float w = ml.x == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
+    float den = ml.y * w;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) den += __shfl_xor(den, o);
+    float acc[C] = {};
+    const float* const src = a.part + row * DH + lane * C;
+    for (int s0 = 0; s0 < slots; s0 += 8) {
+        float v[8][C];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float* p = src + (int64_t)(s0 + i < slots ? s0 + i : s0) * all_rows * DH;
+#pragma unroll
+            for (int c = 0; c < C; ++c) v[i][c] = p[c];
         }
-        float s = -__builtin_huge_valf();
-        if (see) {
-            const T* kr = t < a.S ? pk + t * a.pk_row : k + (t - a.S) * a.k_row;
-            s = 0.f;
-            for (int i = 0; i < DH; ++i) s += qs[i] * to_f32<T>(kr[i]);
-            s *= a.scale_log2;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float ws = __shfl(w, s0 + i < 64 ? s0 + i : 63);
+            if (s0 + i < slots && ws != 0.f) {       // an empty share has left nothing behind
+#pragma unroll
+                for (int c = 0; c < C; ++c) acc[c] = __builtin_fmaf(v[i][c], ws, acc[c]);
+            }
         }
-        const float mn = fmaxf(m, block_reduce(s, red, true));
-        const float ms = mn == -__builtin_huge_valf() ? 0.f : mn;
-        const float w = see ? exp2f(s - ms) : 0.f;
-        ps[tid] = see ? w : -1.f;
-        const float alpha = exp2f(m - ms);
-        l = l * alpha + block_reduce(w, red, false);
-        m = mn;
-        o *= alpha;
-        for (int i = part; i < NTH; i += parts) {
-            const float w_i = ps[i];
-            const int ti = t0 + i;
-            if (w_i >= 0.f) o += w_i * to_f32<T>(ti < a.S ? pv[c * a.pv_chan + ti] : v[c * a.v_chan + ti - a.S]);
-        }
-        __syncthreads();
     }
-    os[tid] = o;
-    __syncthreads();
-    if (tid < DH) {
-        float r = 0.f;
-        for (int i = 0; i < parts; ++i) r += os[i * DH + tid];
-        r = l > 0.f ? r / l : 0.f;
-        T* out = (T*)a.out;
-        const int row = b * a.L + j;
-        out[a.frag ? frag_index(row, h * DH + tid, a.nh * DH) : b * a.out_batch + h * a.out_head + j * a.out_row + tid] = from_f32<T>(r);
-    }
+    const float inv = !absent && den > 0.f ? 1.0f / den : 0.f;
+    T* const op = reinterpret_cast<T*>(a.out) + (a.frag ? frag_index(b * a.L + j, h * DH + lane * C, a.nh * DH)
+                                                        : b * a.out_batch + h * a.out_head + j * a.out_row + lane * C);
+#pragma unroll
+    for (int c = 0; c < C; ++c) op[c] = (T)(acc[c] * inv);
 }
 
-template <class T>
-void launch_rows(const ContextAttn& a, hipStream_t st) {
-    const dim3 grid((unsigned)((int64_t)a.B * a.nh * a.L));
-    if (a.dh == 128) hipLaunchKernelGGL((k_context_rows<T, 128>), grid, dim3(NTH), 0, st, a);
-    else hipLaunchKernelGGL((k_context_rows<T, 64>), grid, dim3(NTH), 0, st, a);
+// Keys per tile where queries are few (64 KB of LDS, two workgroups per CU).
+constexpr int small_tile(int esz, int dh) { return esz == 2 ? 64 : 4096 / dh; }
+
+// Key tiles that the queries see at most (host; P rows in front of the block)
+int own_tiles(const ContextAttn& a, int bkv) {
+    const int64_t end = a.pos_tab ? (int64_t)a.P0 + a.Lblk : (int64_t)a.P + a.L;
+    if (!a.window) return (int)((end + bkv - 1) / bkv);
+    const int64_t first = a.pos_tab ? a.P0 : a.P, lo = first - a.window + 1 > 0 ? first - a.window + 1 : 0;
+    int64_t head = (int64_t)a.sinks - a.S;
+    head = head < 0 ? 0 : head < lo ? head : lo;
+    return (int)((end - lo + bkv - 1) / bkv + 1 + (head + bkv - 1) / bkv);
+}
+int prefix_tiles(const ContextAttn& a, int bkv) {
+    if (!a.S) return 0;
+    if (!a.window) return (a.S + bkv - 1) / bkv;
+    const int64_t first = a.pos_tab ? a.P0 : a.P;
+    int64_t lo = a.S + first - a.window + 1;
+    lo = lo < 0 ? 0 : lo < a.S ? lo : a.S;
+    const int64_t head = a.sinks < lo ? a.sinks : lo;
+    return (int)((a.S - lo + bkv - 1) / bkv + (head + bkv - 1) / bkv);
+}
+
+int clamp_int(int64_t v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : (int)v; }
+
+// part_floats: the scratch there is (context_attention_floats asks with as much as can be wanted)
+Plan make_plan(const ContextAttn& a, int esz, int64_t part_floats) {
+    Plan p{};
+    const int group = a.nh / a.nkv, bkv = small_tile(esz, a.dh);
+    const int64_t slot_floats = (int64_t)a.B * a.nh * a.L * (a.dh + 2);
+    const int slots = clamp_int(part_floats / slot_floats, 0, MAX_SLOTS);
+    p.by_kv = (int64_t)group * a.L <= 128;
+    p.heads = p.by_kv ? a.nkv : a.nh;
+    p.n = p.by_kv ? group * a.L : a.L;
+    p.tiles = (p.n + 127) / 128;
+    p.split = 1;
+    const int TARGET = 512;           // workgroups: two per CU
+    const int64_t base = (int64_t)a.B * p.heads * p.tiles;
+    const int n_own = own_tiles(a, bkv), n_pre = prefix_tiles(a, bkv);
+    p.stacked = p.by_kv && n_pre > 0 && a.B > a.G && p.n <= STACK_ROWS && !(a.P_seq && a.window) && slots >= 2;
+    if (p.stacked) {
+        p.prefix_tiles = (int)(((int64_t)(a.B / a.G) * p.n + 127) / 128);
+        const int64_t pbase = (int64_t)a.G * a.nkv * p.prefix_tiles;
+        const int64_t work = base * n_own + pbase * n_pre;      // tiles of all workgroups
+        const int64_t per = (work + TARGET - 1) / TARGET;
+        p.split = clamp_int((n_own + per - 1) / per, 1, slots / 2 < n_own ? slots / 2 : n_own);
+        p.prefix_split = clamp_int((n_pre + per - 1) / per, 1, slots - p.split < n_pre ? slots - p.split : n_pre);
+        p.prefix_wgs = (int)(pbase * p.prefix_split);
+        return p;
+    }
+    const int n = n_own + n_pre;
+    if (slots >= 2 && a.L <= 128) p.split = clamp_int(TARGET / base, 1, slots < n ? slots : n);
+    return p;
+}
+
+template <class T, int DH, int BQ, int BKV, int NTH>
+void run_cfg(Args a, hipStream_t st) {
+    auto kern = k_context<T, DH, BQ, BKV, NTH>;
+    const int lds = 2 * 2 * BKV * DH * (int)sizeof(T);
+    static int attr_state = 0;
+    if (!ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds, &attr_state)) return;
+    a.tiles = (a.n + BQ - 1) / BQ;
+    const int64_t all_rows = (int64_t)a.B * a.nh * a.L;
+    const int slots = a.split + (a.stacked ? a.prefix_split : 0);
+    a.ml = a.part ? a.part + slots * all_rows * DH : nullptr;
+    hipLaunchKernelGGL(kern, dim3((unsigned)((int64_t)a.tiles * a.heads * a.B * a.split + a.prefix_wgs)), dim3(NTH), lds, st, a);
+    if (slots > 1) hipLaunchKernelGGL((k_context_join<T, DH>), dim3((unsigned)((all_rows + JOIN_WAVES - 1) / JOIN_WAVES)), dim3(64 * JOIN_WAVES), 0, st, a, slots);
+}
+
+template <class T, int DH>
+void run(const ContextAttn& c, hipStream_t st) {
+    Args a{};
+    static_cast<ContextAttn&>(a) = c;
+    static_cast<Plan&>(a) = make_plan(c, sizeof(T), c.part ? c.part_floats : 0);
+    constexpr int SMALL = small_tile(sizeof(T), DH);
+    if constexpr (sizeof(T) == 2) {
+        // long blocks: tiles of 128 keys, and 256 queries where 128 would not find a CU each (heads of 128), as in attention.hip
+        if (c.L > 128 && !c.pos_tab) {
+            if (DH == 128 && (int64_t)c.B * c.nh * ((c.L + 127) / 128) > cu_count()) return run_cfg<T, DH, DH == 128 ? 256 : 128, 128, DH == 128 ? 512 : 256>(a, st);
+            return run_cfg<T, DH, 128, 128, 256>(a, st);
+        }
+    }
+    run_cfg<T, DH, 128, SMALL, 256>(a, st);
 }
 
 }  // namespace
 
-size_t context_attention_floats(const ContextAttn&) { return 0; }
+size_t context_attention_floats(const ContextAttn& a) {
+    const int64_t slot_floats = (int64_t)a.B * a.nh * a.L * (a.dh + 2);
+    const Plan p = make_plan(a, a.dtype == 1 ? 2 : 4, MAX_SLOTS * slot_floats);
+    const int slots = p.split + (p.stacked ? p.prefix_split : 0);
+    return slots > 1 ? (size_t)(slots * slot_floats) : 0;
+}
 
 void launch_context_attention(const ContextAttn& a, hipStream_t st) {
-    if (a.dtype == 1) launch_rows<__hip_bfloat16>(a, st);
-    else launch_rows<float>(a, st);
+    if (a.dtype == 1) {
+        if (a.dh == 128) run<__bf16, 128>(a, st);
+        else run<__bf16, 64>(a, st);
+    } else {
+        if (a.dh == 128) run<float, 128>(a, st);
+        else run<float, 64>(a, st);
+    }
 }
 
 }  // namespace mulo
