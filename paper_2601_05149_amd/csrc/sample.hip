@@ -12,6 +12,8 @@
 // border or a draw where sums in 64-bit floating point place it.
 #include <hip/hip_bf16.h>
 
+#include <type_traits>
+
 #include "mulo_internal.h"
 
 namespace mulo {
@@ -20,7 +22,8 @@ namespace {
 typedef unsigned long long u64;
 constexpr float MOST = 3.402823466e38f;   // the largest finite float32
 constexpr float NEG = -__builtin_huge_valf();
-constexpr int BINS = 2048, CAND = 1024;   // bins of a histogram; entries of a bin that are ordered by comparing them all
+constexpr int BINS = 1024, CAND = 512;    // bins of a histogram; entries of a bin that are ordered by comparing them all
+constexpr int DIGIT = 10;                 // bits of a rank that a histogram of them tells apart
 constexpr int LDS_ENTRIES = 32768;        // of a row that is kept in LDS (128 KB)
 constexpr int ONE = 44;                   // bits of the largest weight
 
@@ -32,55 +35,76 @@ __device__ __forceinline__ uint32_t key_of(float z) {
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 __device__ __forceinline__ u64 rank_of(float z, int i) { return (u64)key_of(z) << 32 | (uint32_t)~i; }
 
-// 2^x for x <= 0 as p 2^n: x = n + f, |f| <= 1/2, p = the polynomial that interpolates 2^f in the 11 Chebyshev nodes
-// (relative error 2^-51).  About 20 instructions at full rate; a library exp takes some 40.
-struct Pow2 { double p; int n; };
-__device__ __forceinline__ Pow2 pow2(double x) {
-    const double shift = 6755399441055744.0;      // 1.5 2^52: the sum's low word is the nearest integer
-    const double xs = x + shift, f = x - (xs - shift);
-    double p = 7.072585949269223e-09;
-    p = __builtin_fma(p, f, 1.0208690299958306e-07);
-    p = __builtin_fma(p, f, 1.321544258792169e-06);
-    p = __builtin_fma(p, f, 1.5252657260200837e-05);
-    p = __builtin_fma(p, f, 0.0001540353044173605);
-    p = __builtin_fma(p, f, 0.0013333558230164974);
-    p = __builtin_fma(p, f, 0.009618129107606888);
-    p = __builtin_fma(p, f, 0.05550410866444772);
-    p = __builtin_fma(p, f, 0.24022650695910097);
-    p = __builtin_fma(p, f, 0.69314718055995);
-    p = __builtin_fma(p, f, 1.0);
-    return Pow2{p, (int)__double_as_longlong(xs)};
-}
-__device__ __forceinline__ double scaled(const Pow2& w, int bits) {     // w 2^bits, bits + w.n > -1000
-    return w.p * __longlong_as_double((long long)(1023 + bits + w.n) << 52);
-}
+// Weights, 2^x with x = (z - max z) log2(e) / T <= 0.  y = STEPS x = n + f, |f| <= 1/2:
+//   2^x = 2^(n / STEPS) e^t, t = f ln 2 / STEPS, |t| <= 1.4e-3
+// The first factor is a table's, its exponent moved.  e^t - 1 = t + t^2 (1/2 + t (1/6 + t / 24)): the sum's second part is below
+// 2^-20 and float32 is enough for it, so that 10 operations in 64 bits are left, at 8 cycles each half of the time (a
+// polynomial of 2^x over all of [-1/2, 1/2] takes 18).  Relative error: 2^-43.
+constexpr int STEPS = 256;
 struct Weights {
     float zmax;
-    double c;      // log2(e) / temperature
-    __device__ __forceinline__ double exponent(float z) const { return z == zmax ? 0.0 : ((double)z - (double)zmax) * c; }
-    __device__ __forceinline__ u64 integer(float z) const {
-        const double x = exponent(z);
-        if (!(x >= -(ONE + 2.0))) return 0;
-        return __double_as_longlong(scaled(pow2(x), ONE) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;      // + 2^52: rounds to an integer
+    double c;                  // STEPS log2(e) / temperature
+    const double* table;       // 2^(i / STEPS), in LDS
+    __device__ __forceinline__ double part(float z, int least, double bits) const {     // 2^(x + bits), 0 below 2^(least + bits)
+        const double shift = 6755399441055744.0;      // 1.5 2^52: the sum's low word is the nearest integer
+        const double d = z == zmax ? 0.0 : (double)z - (double)zmax;
+        const bool some = d * c >= STEPS * (double)least;
+        const double y = some ? d : 0.0, ys = __builtin_fma(y, c, shift), f = __builtin_fma(y, c, -(ys - shift));
+        const int n = (int)__double_as_longlong(ys);
+        const long long tb = __double_as_longlong(table[n & (STEPS - 1)]) + ((long long)((n >> 8) + (int)bits) << 52);
+        const float t = (float)f * (float)(0.6931471805599453 / STEPS);
+        const double r = __builtin_fma(f, 0.6931471805599453 / STEPS, (double)(t * t * __builtin_fmaf(t, __builtin_fmaf(t, 1.f / 24.f, 1.f / 6.f), 0.5f)));
+        const double tw = __longlong_as_double(tb);
+        return some ? __builtin_fma(tw, r, tw) : 0.0;
     }
-    __device__ __forceinline__ double value(float z) const {
-        const double x = exponent(z);
-        return x >= -900.0 ? scaled(pow2(x), 0) : 0.0;
+    __device__ __forceinline__ u64 integer(float z) const {       // + 2^52: rounds to an integer
+        return __double_as_longlong(part(z, -(ONE + 2), ONE) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
     }
+    // of the entries of four that are in: side by side, without a branch
+    __device__ __forceinline__ void integers(const float z[4], const bool in[4], u64 out[4]) const {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[e] = 0;
+        if (!__any(in[0] || in[1] || in[2] || in[3])) return;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const u64 t = integer(z[e]);
+            out[e] = in[e] ? t : 0;
+        }
+    }
+    __device__ __forceinline__ double value(float z) const { return part(z, -900, 0); }
 };
 
-__device__ __forceinline__ u64 wave_sum(u64 v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+// Sums and maxima over the lanes of a wavefront by data-parallel moves: shifts by 1, 2, 4, 8 inside a row of 16 lanes, then the
+// last lane of a row to the next row, and lane 31 to the upper half.  Lanes without a source take `none`.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t moved(uint32_t none, uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, CTRL, ROWS, 0xf, false);
+}
+template <class F>
+__device__ __forceinline__ void six_moves(F&& f) {
+    f(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});
+    f(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+    f(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+    f(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+    f(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});
+    f(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
+}
+__device__ __forceinline__ u64 wave_scan(u64 v) {      // inclusive
+    six_moves([&](auto c, auto r) {
+        const uint32_t lo = moved<decltype(c)::value, decltype(r)::value>(0, (uint32_t)v), hi = moved<decltype(c)::value, decltype(r)::value>(0, (uint32_t)(v >> 32));
+        v += (u64)hi << 32 | lo;
+    });
     return v;
 }
-__device__ __forceinline__ u64 wave_scan(u64 v, int lane) {      // inclusive
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const u64 n = __shfl_up(v, o);
-        if (lane >= o) v += n;
-    }
-    return v;
+__device__ __forceinline__ u64 last_lane(u64 v) {
+    return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), 63) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+__device__ __forceinline__ float wave_max(float v) {
+    six_moves([&](auto c, auto r) {
+        const uint32_t b = __float_as_uint(v);
+        v = fmaxf(v, __uint_as_float(moved<decltype(c)::value, decltype(r)::value>(b, b)));
+    });
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63));
 }
 
 // LDS: the row is read from memory once and kept there; else every pass reads it again.  (Kept in registers, a row of 16384
@@ -92,6 +116,7 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
     constexpr int NW = NT / 64;
     extern __shared__ __attribute__((aligned(16))) float4 kept_row[];      // [NW][runs][64]
     __shared__ __align__(16) u64 hist[BINS];       // then the entries of a bin, and their weights
+    __shared__ double table[STEPS];
     __shared__ u64 s_wave[NW], s_front, s_border;
     __shared__ float s_lo[NW], s_hi[NW];
     __shared__ int s_bin, s_n;
@@ -151,11 +176,8 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
             from_memory([&](int i, const float4 z, int) { f(i, z); });
         }
     };
-    auto each = [&](auto&& f) {
-        each4([&](int i, const float4 z) { f(i, z.x); f(i + 1, z.y); f(i + 2, z.z); f(i + 3, z.w); });
-    };
-
     for (int i = tid; i < BINS; i += NT) hist[i] = 0;
+    if (tid < STEPS) table[tid] = exp2((double)tid / STEPS);
     // ---- the largest entry, and the smallest that is not masked
     float hi = NEG, lo = -NEG;
     from_memory([&](int, const float4 z, int j) {
@@ -164,11 +186,8 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
         auto floor = [](float x) { return x > NEG ? x : -NEG; };
         lo = fminf(fminf(lo, fminf(floor(z.x), floor(z.y))), fminf(floor(z.z), floor(z.w)));
     });
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        hi = fmaxf(hi, __shfl_xor(hi, o));
-        lo = fminf(lo, __shfl_xor(lo, o));
-    }
+    hi = wave_max(hi);
+    lo = -wave_max(-lo);
     if (lane == 0) { s_hi[wave] = hi; s_lo[wave] = lo; }
     __syncthreads();
 #pragma unroll
@@ -177,25 +196,32 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
         lo = fminf(lo, s_lo[i]);
     }
     const bool none = hi == NEG, greedy = a.temperature == 0.0;
-    const Weights w{hi, greedy ? 0.0 : 1.4426950408889634 / a.temperature};
-    u64 border = 0;       // C: entries with a rank of at least this stay, so far
-    auto inside = [&](int i, float z) { return z > NEG && rank_of(z, i) >= border; };
+    const Weights w{hi, greedy ? 0.0 : STEPS * 1.4426950408889634 / a.temperature, table};
+    // the border, so far: entries above b_z stay, and those at it up to index b_i
+    float b_z = NEG;
+    int b_i = -1;
+    auto inside = [&](int i, float z) -> bool { return (z > b_z) | ((z == b_z) & (i <= b_i)); };
+    auto each = [&](auto&& f) {      // f(index of the first, the four, which of them are inside)
+        each4([&](int i, const float4 v) {
+            const float z[4] = {v.x, v.y, v.z, v.w};
+            const bool in[4] = {inside(i, v.x), inside(i + 1, v.y), inside(i + 2, v.z), inside(i + 3, v.w)};
+            f(i, z, in);
+        });
+    };
 
     // ---- the head of what is inside that ends with the entry at which the count, or the mass, reaches want(all of it)
     // Bins along the value: linear over the range of the row, or over the first 128 below the maximum (masks of very low values).
     // Float subtraction and multiplication by a positive number are monotone, so a larger value is never in a later bin.
-    const float scale = (float)BINS / fminf(hi - lo, 128.f);
-    auto bin_of = [&](float z) {
-        const float t = (hi - z) * scale;
-        return t >= (float)(BINS - 1) ? BINS - 1 : t > 0.f ? (int)t : 0;      // NaN (no range, infinities): 0
-    };
-    // where the prefix sum of the bins reaches want: s_bin, and the sum in front of it in s_front; all of it in s_total
+    // Nothing here is a NaN: with infinite entries the maximum's place takes the largest finite number.
+    const float top = fminf(hi, MOST), scale = (float)BINS / fmaxf(fminf(top - lo, 128.f), 1e-30f);
+    auto bin_of = [&](float z) { return (int)__builtin_amdgcn_fmed3f((top - z) * scale, 0.f, (float)(BINS - 1)); };
+    // where the prefix sum of the bins reaches want: s_bin, and the sum in front of it in s_front
     auto cross = [&](u64 before, auto&& want) -> u64 {
         constexpr int PER = BINS / NT;
         u64 v[PER], sum = 0;
 #pragma unroll
         for (int i = 0; i < PER; ++i) sum += v[i] = hist[tid * PER + i];
-        const u64 upto = wave_scan(sum, lane);
+        const u64 upto = wave_scan(sum);
         if (lane == 63) s_wave[wave] = upto;
         __syncthreads();
         u64 front = before + upto - sum, all = before;
@@ -217,67 +243,79 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
         __syncthreads();
         return target;
     };
-    auto find_border = [&](bool mass, auto&& want) {
-        auto amount = [&](float z) -> u64 { return mass ? w.integer(z) : 1ull; };
-        each([&](int i, float z) {
-            if (inside(i, z)) {
-                const u64 x = amount(z);
-                if (x) atomicAdd(&hist[bin_of(z)], x);
+    auto find_border = [&](auto by_mass, auto&& want) {
+        constexpr bool MASS = decltype(by_mass)::value;
+        // adds the counts, or the weights, of entries to their bins
+        auto add = [&](const float z[4], const bool in[4], auto&& bin) {
+            if constexpr (MASS) {
+                u64 x[4];
+                w.integers(z, in, x);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (x[e]) atomicAdd(&hist[bin(e)], x[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (in[e]) atomicAdd(reinterpret_cast<uint32_t*>(&hist[bin(e)]), 1u);      // at most 2^18: the low words
             }
-        });
+        };
+        each([&](int, const float z[4], const bool in[4]) { add(z, in, [&](int e) { return bin_of(z[e]); }); });
         __syncthreads();
         const u64 target = cross(0, want);
         const int bin = s_bin;
         u64 front = s_front;
-        each([&](int i, float z) {
-            if (inside(i, z) && bin_of(z) == bin) {
-                const int at = atomicAdd(&s_n, 1);
-                if (at < CAND) cand[at] = rank_of(z, i);
-            }
+        each4([&](int i, const float4 v) {
+            const float z[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if ((bin_of(z[e]) == bin) & inside(i + e, z[e])) {
+                    const int at = atomicAdd(&s_n, 1);
+                    if (at < CAND) cand[at] = rank_of(z[e], i + e);
+                }
         });
         __syncthreads();
         const int n = s_n;
         if (n <= CAND) {
-            if (mass) {
+            if (MASS) {
                 for (int t = tid; t < n; t += NT) candw[t] = w.integer(of_key((uint32_t)(cand[t] >> 32)));
                 __syncthreads();
             }
             for (int t = tid; t < n; t += NT) {
                 const u64 own = cand[t];
                 u64 before = front;
-                for (int i = 0; i < n; ++i)
-                    if (cand[i] > own) before += mass ? candw[i] : 1ull;
-                if (before < target && before + (mass ? candw[t] : 1ull) >= target) s_border = own;
+                for (int i = 0; i < n; ++i) {
+                    const u64 amount = MASS ? candw[i] : 1ull;
+                    before += cand[i] > own ? amount : 0;
+                }
+                if (before < target && before + (MASS ? candw[t] : 1ull) >= target) s_border = own;
             }
             __syncthreads();
         } else {
             // by the digits of the rank, the largest first: 32 bits of the value, and the 18 of an index that can differ
-            u64 known = 0, mask = 0;
-            const int shifts[5] = {53, 42, 32, 9, 0};
+            auto short_rank = [](float z, int i) { return (u64)key_of(z) << 18 | ((uint32_t)~i & 0x3FFFFu); };
+            u64 known = 0;
 #pragma unroll 1
-            for (int d = 0; d < 5; ++d) {
-                const int shift = shifts[d], bits = d < 2 ? 11 : d == 2 ? 10 : 9;
+            for (int shift = 4 * DIGIT; shift >= 0; shift -= DIGIT) {
                 for (int i = tid; i < BINS; i += NT) hist[i] = 0;
                 __syncthreads();
-                each([&](int i, float z) {
-                    const u64 c = rank_of(z, i);
-                    if (inside(i, z) && bin_of(z) == bin && (c & mask) == known) {
-                        const u64 x = amount(z);
-                        if (x) atomicAdd(&hist[(1 << bits) - 1 - (int)(c >> shift & ((1u << bits) - 1))], x);
-                    }
+                each([&](int i, const float z[4], const bool in[4]) {
+                    bool here[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) here[e] = in[e] && bin_of(z[e]) == bin && short_rank(z[e], i + e) >> (shift + DIGIT) == known;
+                    add(z, here, [&](int e) { return BINS - 1 - (int)(short_rank(z[e], i + e) >> shift & (BINS - 1)); });
                 });
                 __syncthreads();
                 cross(front, [&](u64) { return target; });
                 front = s_front;
-                known |= (u64)((1 << bits) - 1 - s_bin) << shift;
-                mask |= (u64)((1 << bits) - 1) << shift;
-                if (d == 2) { known |= 0xFFFC0000ull; mask |= 0xFFFC0000ull; }      // an index below 2^18, inverted
+                known = known << DIGIT | (BINS - 1 - s_bin);
             }
-            if (tid == 0) s_border = known;
+            if (tid == 0) s_border = known >> 18 << 32 | 0xFFFC0000ull | (known & 0x3FFFFu);
             __syncthreads();
         }
-        border = s_border;
+        b_z = of_key((uint32_t)(s_border >> 32));
+        b_i = (int)~(uint32_t)s_border;
     };
+    static_assert(BINS == 1 << DIGIT, "a bin for every digit");
     bool cleared = true;
     auto clear_hist = [&]() {
         if (!cleared) {
@@ -290,36 +328,40 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
         const int top_k = greedy ? 1 : a.top_k;
         if (top_k > 0 && top_k < V) {      // all of a row's entries stay where fewer than top_k are not masked
             clear_hist();
-            find_border(false, [&](u64 all) { return all < (u64)top_k ? all : (u64)top_k; });
+            find_border(std::false_type{}, [&](u64 all) { return all < (u64)top_k ? all : (u64)top_k; });
         }
         if (!greedy && a.top_p < 1.0) {
             clear_hist();
-            find_border(true, [&](u64 all) {
+            find_border(std::true_type{}, [&](u64 all) {
                 const u64 t = (u64)__builtin_ceil(a.top_p * (double)all);      // the mass in front of the next entry is below top_p of all
                 return t < 1 ? 1ull : t < all ? t : all;
             });
         }
     }
-    // min-p by the value, and by the weight itself next to the border
-    float sure = NEG, never = NEG;
-    const bool min_p = !greedy && a.min_p > 0.0 && !none;
-    if (min_p) {
-        const double d = log(a.min_p) * a.temperature, at = (double)hi + d, eps = 1e-6 * (fabs((double)hi) + fabs(d)) + 1e-40;
-        sure = (float)(at + eps);
-        never = (float)(at - eps);
+    // min-p: the least value with enough weight, from where its logarithm says, a step of float32 at a time
+    if (!greedy && a.min_p > 0.0 && !none) {
+        const uint32_t most = key_of(hi), least = key_of(-MOST);
+        auto enough = [&](uint32_t k) { return k >= most || w.value(of_key(k)) >= a.min_p; };
+        uint32_t k = key_of((float)fmax((double)hi + log(a.min_p) * a.temperature, -(double)MOST));
+        k = k < most ? k : most;
+        for (int i = 0; i < 8 && !enough(k); ++i) ++k;
+        for (int i = 0; i < 8 && k > least && enough(k - 1); ++i) --k;
+        if (of_key(k) > b_z) {
+            b_z = of_key(k);
+            b_i = V;
+        }
     }
-    auto stays = [&](int i, float z) {
-        if (!inside(i, z)) return false;
-        if (!min_p || z > sure || z == hi) return true;
-        return z >= never && w.value(z) >= a.min_p;
-    };
 
     // ---- the draw: the mass that stays, by wavefronts (in index order), then the run, the lane and the entry
     u64 total = 0;
     if (a.tokens || a.probs) {
         u64 sum = 0;
-        each([&](int i, float z) { if (stays(i, z)) sum += w.integer(z); });
-        sum = wave_sum(sum);
+        each([&](int, const float z[4], const bool in[4]) {
+            u64 x[4];
+            w.integers(z, in, x);
+            sum += (x[0] + x[1]) + (x[2] + x[3]);
+        });
+        sum = last_lane(wave_scan(sum));
         __syncthreads();                    // s_wave of the searches has been read
         if (lane == 0) s_wave[wave] = sum;
         __syncthreads();
@@ -335,14 +377,13 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
             const u64 target = (u64)((double)u * (double)total);
             if (none && tid == 0) a.tokens[r] = -1;
             if (front <= target && target < front + sum) {      // uniform over the wavefront
-                each4([&](int i, const float4 z) {
-                    const u64 w0 = stays(i, z.x) ? w.integer(z.x) : 0, w1 = stays(i + 1, z.y) ? w.integer(z.y) : 0,
-                              w2 = stays(i + 2, z.z) ? w.integer(z.z) : 0, w3 = stays(i + 3, z.w) ? w.integer(z.w) : 0;
-                    const u64 mine = w0 + w1 + w2 + w3, upto = wave_scan(mine, lane), run = __shfl(upto, 63);
-                    const u64 c0 = front + upto - mine;
-                    if (target >= c0 && target < c0 + mine)
-                        a.tokens[r] = target < c0 + w0 ? i : target < c0 + w0 + w1 ? i + 1 : target < c0 + w0 + w1 + w2 ? i + 2 : i + 3;
-                    front += run;
+                each([&](int i, const float z[4], const bool in[4]) {
+                    u64 x[4];
+                    w.integers(z, in, x);
+                    const u64 own = (x[0] + x[1]) + (x[2] + x[3]), upto = wave_scan(own), c0 = front + upto - own;
+                    if (target >= c0 && target < c0 + own)
+                        a.tokens[r] = target < c0 + x[0] ? i : target < c0 + x[0] + x[1] ? i + 1 : target < c0 + x[0] + x[1] + x[2] ? i + 2 : i + 3;
+                    front += last_lane(upto);
                 });
             }
         }
@@ -361,7 +402,7 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
             }
         };
         each4([&](int i, const float4 z) {
-            const bool s0 = stays(i, z.x), s1 = stays(i + 1, z.y), s2 = stays(i + 2, z.z), s3 = stays(i + 3, z.w);
+            const bool s0 = inside(i, z.x), s1 = inside(i + 1, z.y), s2 = inside(i + 2, z.z), s3 = inside(i + 3, z.w);
             if (a.probs) put(a.probs + r * V, i, make_float4(s0 ? (float)(w.value(z.x) * inv) : 0.f, s1 ? (float)(w.value(z.y) * inv) : 0.f,
                                                              s2 ? (float)(w.value(z.z) * inv) : 0.f, s3 ? (float)(w.value(z.w) * inv) : 0.f));
             if (a.kept) {
@@ -388,7 +429,10 @@ void run(const SampleArgs& a, hipStream_t st) {
 
 void launch_sample_filtered(const SampleArgs& a, hipStream_t st) {
     if (a.V <= 2048) run<256, true>(a, st);
-    else if (a.V <= LDS_ENTRIES) run<1024, true>(a, st);
+    else if (a.V <= LDS_ENTRIES) {
+        if (a.rows > cu_count()) run<512, true>(a, st);
+        else run<1024, true>(a, st);
+    }
     else run<1024, false>(a, st);
 }
 
