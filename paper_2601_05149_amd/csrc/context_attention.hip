@@ -98,44 +98,39 @@ __global__ __launch_bounds__(NTH, DH * BKV * (int)sizeof(T) <= 16384 ? 2 : 1) vo
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];  // [2][BUF]
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, lh = lane >> 5;
-    const int group = a.nh / a.nkv;
+    auto div = [](int x, int y) { return (int)((uint32_t)x / (uint32_t)y); };      // of numbers that are not negative: half the instructions
+    auto mod = [](int x, int y) { return (int)((uint32_t)x % (uint32_t)y); };
+    const int group = div(a.nh, a.nkv), in_group = div(a.B, a.G);      // heads of a key head, sequences of a prefix
     // ---- which queries, which share of which keys
     const bool of_prefix = a.stacked && (int)blockIdx.x < a.prefix_wgs;
     int b = 0, hd, qt, split, nsplit, slot, n, g;
     if (of_prefix) {      // consecutive ids: consecutive (group, head)s, one XCD each; the row tiles of one lie on one XCD
         const int gk = a.G * a.nkv, bid = blockIdx.x;
-        const int in = bid % gk;
-        g = in / a.nkv; hd = in % a.nkv;
-        qt = bid / gk % a.prefix_tiles;
-        split = slot = bid / (gk * a.prefix_tiles);
+        const int rest = div(bid, gk), in = bid - rest * gk;
+        g = div(in, a.nkv); hd = in - g * a.nkv;
+        split = slot = div(rest, a.prefix_tiles);
+        qt = rest - split * a.prefix_tiles;
         nsplit = a.prefix_split;
-        n = a.B / a.G * a.n;
+        n = in_group * a.n;
     } else {              // all query tiles of a (sequence, head) on one XCD, next to each other; long tiles first
-        const int nbh = a.B * a.heads, bid = ((int)blockIdx.x - (a.stacked ? a.prefix_wgs : 0)) % (a.tiles * nbh);
-        split = ((int)blockIdx.x - (a.stacked ? a.prefix_wgs : 0)) / (a.tiles * nbh);
-        int bh;
-        if ((nbh & 7) == 0) {
-            const int s = bid >> 3;
-            qt = a.tiles - 1 - s % a.tiles;
-            bh = (s / a.tiles) * 8 + (bid & 7);
-        } else {
-            qt = a.tiles - 1 - bid % a.tiles;
-            bh = bid / a.tiles;
-        }
-        hd = bh % a.heads;
-        b = bh / a.heads;
-        g = b / (a.B / a.G);
+        const int nbh = a.B * a.heads, id = (int)blockIdx.x - (a.stacked ? a.prefix_wgs : 0);
+        split = div(id, a.tiles * nbh);
+        const int bid = id - split * (a.tiles * nbh), by8 = (nbh & 7) == 0, s = by8 ? bid >> 3 : bid, s_bh = div(s, a.tiles);
+        qt = a.tiles - 1 - (s - s_bh * a.tiles);
+        const int bh = by8 ? s_bh * 8 + (bid & 7) : s_bh;
+        b = div(bh, a.heads);
+        hd = bh - b * a.heads;
+        g = div(b, in_group);
         slot = split + (a.stacked ? a.prefix_split : 0);
         nsplit = a.split;
         n = a.n;
     }
-    const int kvh = a.by_kv ? hd : hd / group;
+    const int kvh = a.by_kv ? hd : div(hd, group);
     const bool scattered = a.pos_tab != nullptr;
     // ---- this lane's query (the last one again past the end; such lanes do not store)
     const int r0 = qt * BQ + wave * 32, r_raw = r0 + l32, r = r_raw < n ? r_raw : n - 1;
-    const int lb = of_prefix ? g * (a.B / a.G) + r / a.n : b;
-    const int in_seq = of_prefix ? r % a.n : r;
-    const int lhd = a.by_kv ? hd * group + in_seq / a.L : hd, lj = a.by_kv ? in_seq % a.L : in_seq;
+    const int r_seq = of_prefix ? div(r, a.n) : 0, lb = of_prefix ? g * in_group + r_seq : b, in_seq = r - r_seq * a.n;
+    const int r_hd = a.by_kv ? div(in_seq, a.L) : 0, lhd = a.by_kv ? hd * group + r_hd : hd, lj = in_seq - r_hd * a.L;
     const bool wave_live = r0 < n;
     int P = a.P;
     if (a.P_seq && !of_prefix) {
@@ -153,9 +148,9 @@ __global__ __launch_bounds__(NTH, DH * BKV * (int)sizeof(T) <= 16384 ? 2 : 1) vo
     // own rows of the queries: of this wavefront, of the workgroup (bounds)
     auto first_last = [&](int ra, int rb, int& lo, int& hi) {
         rb = rb < n ? rb : n - 1;
-        const bool one = !a.by_kv || ra / a.L == rb / a.L;       // within a head the queries are consecutive
-        lo = P + (one ? (a.by_kv ? ra % a.L : ra) : 0);
-        hi = P + (one ? (a.by_kv ? rb % a.L : rb) : a.L - 1);
+        const bool one = !a.by_kv || div(ra, a.L) == div(rb, a.L);       // within a head the queries are consecutive
+        lo = P + (one ? (a.by_kv ? mod(ra, a.L) : ra) : 0);
+        hi = P + (one ? (a.by_kv ? mod(rb, a.L) : rb) : a.L - 1);
         if (scattered) { lo = a.P0; hi = a.P0 + a.Lblk - 1; }
     };
     int w_min, w_max, p_min, p_max;
@@ -294,9 +289,10 @@ __global__ __launch_bounds__(NTH, DH * BKV * (int)sizeof(T) <= 16384 ? 2 : 1) vo
 
     // bf16: row rho of a K block is fed key rho with bits 2 and 3 swapped, so that a lane's accumulators cover 8 consecutive keys
     const int kperm = BF16 ? (l32 & 0x13) | ((l32 & 4) << 1) | ((l32 & 8) >> 1) : l32;
-    auto key_at = [&](int kb, int e) {       // accumulator e of block kb holds this key of the tile
-        return BF16 ? kb * 32 + 16 * (e >> 3) + 8 * lh + (e & 7) : kb * 32 + 8 * (e >> 2) + 4 * lh + (e & 3);
-    };
+    // accumulator e of block kb holds key key_at(kb, e) + lane_key of the tile.  (Kept apart: the sums are the same in every
+    // tile, and 64 registers would hold them.)
+    auto key_at = [](int kb, int e) { return BF16 ? kb * 32 + 16 * (e >> 3) + (e & 7) : kb * 32 + 8 * (e >> 2) + (e & 3); };
+    const int lane_key = (BF16 ? 8 : 4) * lh;
     const int kfrag = kperm * KRB + (lh ^ key_of(kperm, KRB)) * 16, vfrag = l32 * VRB + (lh ^ key_of(l32, VRB)) * 16;
     f32x16 s[NKB];               // the scores of a tile, then
     float m_safe = 0.f, alpha = 1.f;   // the reference of its exponentials and the factor of what has been added up before it
@@ -321,26 +317,28 @@ __global__ __launch_bounds__(NTH, DH * BKV * (int)sizeof(T) <= 16384 ? 2 : 1) vo
                 __builtin_amdgcn_sched_barrier(0);
             });
         });
-        const int last = pre ? S - 1 : w_min;                            // key up to which all queries of the wavefront see
-        if (kv0 + BKV - 1 > last) {
-            const int lim = pre ? S - 1 : pos;
+        // at most 4 comparisons at once: more than that need more scalars than there are
+        auto mask = [&](auto&& seen) {
 #pragma unroll
             for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s[kb][e] = kv0 + key_at(kb, e) <= lim ? s[kb][e] : -__builtin_huge_valf();
+                for (int e = 0; e < 16; ++e) {
+                    s[kb][e] = seen(key_at(kb, e)) ? s[kb][e] : -__builtin_huge_valf();
+                    if ((e & 3) == 3) __builtin_amdgcn_sched_barrier(0);
+                }
+        };
+        const int last = pre ? S - 1 : w_min;                            // key up to which all queries of the wavefront see
+        if (kv0 + BKV - 1 > last) {
+            const int lim = (pre ? S - 1 : pos) - kv0 - lane_key;
+            mask([&](int key) { return key <= lim; });
         }
         if (window) {
             const int shift = (pre ? S : 0) - window, sinks = a.sinks - (pre ? 0 : S);
             if (kv0 + BKV > sinks && kv0 <= w_max + shift) {             // some key may lie between the sinks and a window
-                const int before = pos + shift;                          // the last one in front of this query's window
-#pragma unroll
-                for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int key = kv0 + key_at(kb, e);
-                        s[kb][e] = key < sinks || key > before ? s[kb][e] : -__builtin_huge_valf();
-                        if ((e & 3) == 3) __builtin_amdgcn_sched_barrier(0);
-                    }
+                // the last key in front of this query's window; all below head are sinks.  (One loop for tiles with and without
+                // sinks: as two branches their 64 results each take more registers than there are.)
+                const int before = pos + shift - kv0 - lane_key, head = sinks - kv0 - lane_key;
+                mask([&](int key) -> bool { return (key < head) | (key > before); });
             }
         }
         if constexpr (BF16 && BKV == 64) {
@@ -353,7 +351,7 @@ __global__ __launch_bounds__(NTH, DH * BKV * (int)sizeof(T) <= 16384 ? 2 : 1) vo
                         const uint32_t mine = (uint32_t)(hidden >> (kb * 32)) >> (8 * lh);
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
-                            if (((mine >> (16 * (e >> 3) + (e & 7))) & 1u) && kv0 + key_at(kb, e) < pos) s[kb][e] = -__builtin_huge_valf();
+                            if (((mine >> (16 * (e >> 3) + (e & 7))) & 1u) && kv0 + lane_key + key_at(kb, e) < pos) s[kb][e] = -__builtin_huge_valf();
                             if ((e & 3) == 3) __builtin_amdgcn_sched_barrier(0);
                         }
                     }
@@ -496,18 +494,30 @@ __global__ __launch_bounds__(NTH, DH * BKV * (int)sizeof(T) <= 16384 ? 2 : 1) vo
             store_out(i, g4, f32x4{o[i][g4 * 4] * inv, o[i][g4 * 4 + 1] * inv, o[i][g4 * 4 + 2] * inv, o[i][g4 * 4 + 3] * inv});
 }
 
-// A wavefront joins the shares of a query: lane s takes the weight of share s, then every lane DH / 64 channels.  Rows of absent
-// sequences and unused slots are zeros.
+// A wavefront joins the shares of a query: lane s takes the weight of share s, then every lane DH / 64 channels of all of them.
+// One memory round trip: the outputs of NS shares (those there are not re-read the first) are requested together with the weights.
+// Rows of absent sequences and unused slots are zeros.
 constexpr int JOIN_WAVES = 4;
-template <class T, int DH>
+template <class T, int DH, int NS>
 __global__ __launch_bounds__(64 * JOIN_WAVES) void k_context_join(const Args a, int slots) {
     constexpr int C = DH / 64;
-    const int64_t all_rows = (int64_t)a.B * a.nh * a.L, row = (int64_t)blockIdx.x * JOIN_WAVES + (threadIdx.x >> 6);
+    const uint32_t all_rows = (uint32_t)(a.B * a.nh * a.L), row = blockIdx.x * JOIN_WAVES + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
     if (row >= all_rows) return;
-    const int j = row % a.L, h = (row / a.L) % a.nh, b = row / ((int64_t)a.L * a.nh);
-    const bool absent = (a.P_seq && a.P_seq[b] < 0) || (a.pos_tab && a.pos_tab[(int64_t)b * a.L + j] < 0);
-    const float2 ml = lane < slots ? *reinterpret_cast<const float2*>(a.ml + 2 * (lane * all_rows + row)) : make_float2(-__builtin_huge_valf(), 0.f);
+    const float* const src = a.part + (int64_t)row * DH + lane * C;
+    float v[NS][C];
+    auto request = [&](int s0) {
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            const float* p = src + (int64_t)(s0 + i < slots ? s0 + i : 0) * all_rows * DH;
+#pragma unroll
+            for (int c = 0; c < C; ++c) v[i][c] = p[c];
+        }
+    };
+    request(0);
+    const float2 ml = lane < slots ? *reinterpret_cast<const float2*>(a.ml + 2 * ((int64_t)lane * all_rows + row)) : make_float2(-__builtin_huge_valf(), 0.f);
+    const uint32_t j = row % (uint32_t)a.L, bh = row / (uint32_t)a.L, h = bh % (uint32_t)a.nh, b = bh / (uint32_t)a.nh;
+    const bool absent = (a.P_seq && a.P_seq[b] < 0) || (a.pos_tab && a.pos_tab[b * a.L + j] < 0);
     float M = ml.x;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
@@ -516,29 +526,29 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void k_context_join(const Args a, 
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) den += __shfl_xor(den, o);
     float acc[C] = {};
-    const float* const src = a.part + row * DH + lane * C;
-    for (int s0 = 0; s0 < slots; s0 += 8) {
-        float v[8][C];
+    for (int s0 = 0;;) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float* p = src + (int64_t)(s0 + i < slots ? s0 + i : s0) * all_rows * DH;
+        for (int i = 0; i < NS; ++i) {
+            const float ws = s0 + i < slots ? __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(w), s0 + i)) : 0.f;
 #pragma unroll
-            for (int c = 0; c < C; ++c) v[i][c] = p[c];
+            for (int c = 0; c < C; ++c) acc[c] = ws != 0.f ? __builtin_fmaf(v[i][c], ws, acc[c]) : acc[c];      // an empty share has left nothing behind
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float ws = __shfl(w, s0 + i < 64 ? s0 + i : 63);
-            if (s0 + i < slots && ws != 0.f) {       // an empty share has left nothing behind
-#pragma unroll
-                for (int c = 0; c < C; ++c) acc[c] = __builtin_fmaf(v[i][c], ws, acc[c]);
-            }
-        }
+        s0 += NS;
+        if (s0 >= slots) break;
+        request(s0);
     }
     const float inv = !absent && den > 0.f ? 1.0f / den : 0.f;
     T* const op = reinterpret_cast<T*>(a.out) + (a.frag ? frag_index(b * a.L + j, h * DH + lane * C, a.nh * DH)
-                                                        : b * a.out_batch + h * a.out_head + j * a.out_row + lane * C);
+                                                        : (int64_t)b * a.out_batch + h * a.out_head + j * a.out_row + lane * C);
 #pragma unroll
     for (int c = 0; c < C; ++c) op[c] = (T)(acc[c] * inv);
+}
+template <class T, int DH>
+void join(const Args& a, int slots, hipStream_t st) {
+    const dim3 grid((unsigned)(((int64_t)a.B * a.nh * a.L + JOIN_WAVES - 1) / JOIN_WAVES)), block(64 * JOIN_WAVES);
+    if (slots <= 4) hipLaunchKernelGGL((k_context_join<T, DH, 4>), grid, block, 0, st, a, slots);
+    else if (slots <= 8) hipLaunchKernelGGL((k_context_join<T, DH, 8>), grid, block, 0, st, a, slots);
+    else hipLaunchKernelGGL((k_context_join<T, DH, 16>), grid, block, 0, st, a, slots);
 }
 
 // Keys per tile where queries are few (64 KB of LDS, two workgroups per CU).
@@ -606,7 +616,7 @@ void run_cfg(Args a, hipStream_t st) {
     const int slots = a.split + (a.stacked ? a.prefix_split : 0);
     a.ml = a.part ? a.part + slots * all_rows * DH : nullptr;
     hipLaunchKernelGGL(kern, dim3((unsigned)((int64_t)a.tiles * a.heads * a.B * a.split + a.prefix_wgs)), dim3(NTH), lds, st, a);
-    if (slots > 1) hipLaunchKernelGGL((k_context_join<T, DH>), dim3((unsigned)((all_rows + JOIN_WAVES - 1) / JOIN_WAVES)), dim3(64 * JOIN_WAVES), 0, st, a, slots);
+    if (slots > 1) join<T, DH>(a, slots, st);
 }
 
 template <class T, int DH>
