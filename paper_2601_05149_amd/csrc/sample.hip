@@ -42,23 +42,23 @@ __device__ __forceinline__ u64 rank_of(float z, int i) { return (u64)key_of(z) <
 // polynomial of 2^x over all of [-1/2, 1/2] takes 18).  Relative error: 2^-43.
 constexpr int STEPS = 256;
 struct Weights {
-    float zmax;
-    double c;                  // STEPS log2(e) / temperature
+    double zmax, c;            // the maximum (of infinite ones: the largest finite number); STEPS log2(e) / temperature
+    float least_value, least;  // smallest z with a weight that value(), and integer(), tell from 0
     const double* table;       // 2^(i / STEPS), in LDS
-    __device__ __forceinline__ double part(float z, int least, double bits) const {     // 2^(x + bits), 0 below 2^(least + bits)
+    __device__ __forceinline__ double part(float z, int bits) const {     // 2^(x + bits), for z of at least least_value
         const double shift = 6755399441055744.0;      // 1.5 2^52: the sum's low word is the nearest integer
-        const double d = z == zmax ? 0.0 : (double)z - (double)zmax;
-        const bool some = d * c >= STEPS * (double)least;
-        const double y = some ? d : 0.0, ys = __builtin_fma(y, c, shift), f = __builtin_fma(y, c, -(ys - shift));
+        const double d = (double)fminf(z, MOST) - zmax;
+        const double ys = __builtin_fma(d, c, shift), f = __builtin_fma(d, c, -(ys - shift));
         const int n = (int)__double_as_longlong(ys);
-        const long long tb = __double_as_longlong(table[n & (STEPS - 1)]) + ((long long)((n >> 8) + (int)bits) << 52);
+        const long long tb = __double_as_longlong(table[n & (STEPS - 1)]) + ((long long)((n >> 8) + bits) << 52);
         const float t = (float)f * (float)(0.6931471805599453 / STEPS);
         const double r = __builtin_fma(f, 0.6931471805599453 / STEPS, (double)(t * t * __builtin_fmaf(t, __builtin_fmaf(t, 1.f / 24.f, 1.f / 6.f), 0.5f)));
         const double tw = __longlong_as_double(tb);
-        return some ? __builtin_fma(tw, r, tw) : 0.0;
+        return __builtin_fma(tw, r, tw);
     }
-    __device__ __forceinline__ u64 integer(float z) const {       // + 2^52: rounds to an integer
-        return __double_as_longlong(part(z, -(ONE + 2), ONE) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
+    __device__ __forceinline__ u64 integer(float z, bool in) const {       // + 2^52: rounds to an integer
+        const u64 t = __double_as_longlong(part(z, ONE) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
+        return (in && z >= least) ? t : 0;
     }
     // of the entries of four that are in: side by side, without a branch
     __device__ __forceinline__ void integers(const float z[4], const bool in[4], u64 out[4]) const {
@@ -66,12 +66,9 @@ struct Weights {
         for (int e = 0; e < 4; ++e) out[e] = 0;
         if (!__any(in[0] || in[1] || in[2] || in[3])) return;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const u64 t = integer(z[e]);
-            out[e] = in[e] ? t : 0;
-        }
+        for (int e = 0; e < 4; ++e) out[e] = integer(z[e], in[e]);
     }
-    __device__ __forceinline__ double value(float z) const { return part(z, -900, 0); }
+    __device__ __forceinline__ double value(float z) const { return z >= least_value ? part(z, 0) : 0.0; }
 };
 
 // Sums and maxima over the lanes of a wavefront by data-parallel moves: shifts by 1, 2, 4, 8 inside a row of 16 lanes, then the
@@ -96,9 +93,14 @@ __device__ __forceinline__ u64 wave_scan(u64 v) {      // inclusive
     });
     return v;
 }
-__device__ __forceinline__ u64 last_lane(u64 v) {
-    return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), 63) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+    six_moves([&](auto c, auto r) { v += moved<decltype(c)::value, decltype(r)::value>(0, v); });
+    return v;
 }
+__device__ __forceinline__ u64 lane_of(u64 v, int i) {
+    return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, i);
+}
+__device__ __forceinline__ uint32_t lane_of(uint32_t v, int i) { return (uint32_t)__builtin_amdgcn_readlane((int)v, i); }
 __device__ __forceinline__ float wave_max(float v) {
     six_moves([&](auto c, auto r) {
         const uint32_t b = __float_as_uint(v);
@@ -111,15 +113,19 @@ __device__ __forceinline__ float wave_max(float v) {
 // unrolls every pass 64 times: 70000 instructions, which neither registers nor the instruction cache hold.)
 // Wavefront w has the stretch [w seg, (w + 1) seg) of the row, in runs of 256: consecutive lanes, consecutive entries.
 // A thread takes the same entries in every pass.
-template <int NT, bool LDS>
+// PER: entries of the list a thread takes.  Where top-k leaves at most PER NT entries they are listed, and everything behind it
+// (masses, top-p, the draw's sums, what is written of them) goes by the list: of 16384 entries 2000 cost an eighth.
+template <int NT, bool LDS, int PER>
 __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
     constexpr int NW = NT / 64;
     extern __shared__ __attribute__((aligned(16))) float4 kept_row[];      // [NW][runs][64]
     __shared__ __align__(16) u64 hist[BINS];       // then the entries of a bin, and their weights
     __shared__ double table[STEPS];
-    __shared__ u64 s_wave[NW], s_front, s_border;
+    __shared__ u64 s_wave[NW], s_mass[NW], s_front, s_border;
     __shared__ float s_lo[NW], s_hi[NW];
-    __shared__ int s_bin, s_n;
+    __shared__ int s_bin, s_n, s_listed;
+    __shared__ float list_z[PER * NT];
+    __shared__ uint32_t list_at[PER * NT];         // wavefront << 18 | index
     u64* const cand = hist;
     u64* const candw = hist + CAND;
 
@@ -147,12 +153,14 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
         };
         return make_float4(one(i), one(i + 1), one(i + 2), one(i + 3));
     };
-    auto row4 = [&](int i, float4 c, float4 u) -> float4 {     // guided; NaN, and what lies past the end, is masked
-        auto clean = [&](float x, float y, int k) {
-            const float z = zu ? __fadd_rn(y, __fmul_rn(a.cfg_scale, __fsub_rn(x, y))) : x;
-            return z == z && k < V ? z : NEG;
-        };
-        return make_float4(clean(c.x, u.x, i), clean(c.y, u.y, i + 1), clean(c.z, u.z, i + 2), clean(c.w, u.w, i + 3));
+    auto row4 = [&](int i, float4 c, float4 u) -> float4 {     // guided; NaN (a maximum's other operand), and what lies past the end, is masked
+        if (zu) {
+            auto guide = [&](float x, float y) { return __fadd_rn(y, __fmul_rn(a.cfg_scale, __fsub_rn(x, y))); };
+            c = make_float4(guide(c.x, u.x), guide(c.y, u.y), guide(c.z, u.z), guide(c.w, u.w));
+        }
+        c = make_float4(fmaxf(c.x, NEG), fmaxf(c.y, NEG), fmaxf(c.z, NEG), fmaxf(c.w, NEG));
+        if (i - lane * 4 + 256 > V) c = make_float4(i < V ? c.x : NEG, i + 1 < V ? c.y : NEG, i + 2 < V ? c.z : NEG, i + 3 < V ? c.w : NEG);
+        return c;
     };
     // f(index of the first, four entries, number of the run), four runs requested together
     auto from_memory = [&](auto&& f) {
@@ -176,27 +184,61 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
             from_memory([&](int i, const float4 z, int) { f(i, z); });
         }
     };
+    auto put = [&](float* row, int i, const float4 v) {
+        if ((V & 3) == 0 && ((uintptr_t)row & 15) == 0) {
+            if (i < V) *reinterpret_cast<float4*>(row + i) = v;
+        } else {
+            if (i < V) row[i] = v.x;
+            if (i + 1 < V) row[i + 1] = v.y;
+            if (i + 2 < V) row[i + 2] = v.z;
+            if (i + 3 < V) row[i + 3] = v.w;
+        }
+    };
     for (int i = tid; i < BINS; i += NT) hist[i] = 0;
     if (tid < STEPS) table[tid] = exp2((double)tid / STEPS);
-    // ---- the largest entry, and the smallest that is not masked
+    if (tid < NW) s_mass[tid] = 0;
+    if (tid == 0) s_listed = 0;
+    const bool greedy = a.temperature == 0.0;
+    const int top_k = greedy ? 1 : a.top_k;
+    // (from memory in every pass, the row has to stay as it is where the filtered logits take its place)
+    const bool by_list = top_k > 0 && top_k <= PER * NT && top_k < V && (LDS || (const void*)a.kept != a.logits);
+    float* const probs = a.probs ? a.probs + r * V : nullptr;
+    float* const kept = a.kept ? a.kept + r * V : nullptr;
+    // ---- the largest entry, and the smallest that is not masked (masked ones are left out in a pass of their own)
     float hi = NEG, lo = -NEG;
-    from_memory([&](int, const float4 z, int j) {
+    auto meet = [&]() {
+        hi = wave_max(hi);
+        lo = -wave_max(-lo);
+        if (lane == 0) { s_hi[wave] = hi; s_lo[wave] = lo; }
+        __syncthreads();
+        const float h = s_hi[lane & (NW - 1)], l = s_lo[lane & (NW - 1)];
+        hi = wave_max(h);
+        lo = -wave_max(-l);
+    };
+    from_memory([&](int i, const float4 z, int j) {
         if constexpr (LDS) mine[j * 64] = z;
         hi = fmaxf(fmaxf(hi, fmaxf(z.x, z.y)), fmaxf(z.z, z.w));
-        auto floor = [](float x) { return x > NEG ? x : -NEG; };
-        lo = fminf(fminf(lo, fminf(floor(z.x), floor(z.y))), fminf(floor(z.z), floor(z.w)));
+        lo = fminf(fminf(lo, fminf(z.x, z.y)), fminf(z.z, z.w));
+        // what the list does not hold; the list's entries are written over it, barriers later
+        if (by_list && probs) put(probs, i, make_float4(0.f, 0.f, 0.f, 0.f));
+        if (by_list && kept) put(kept, i, make_float4(NEG, NEG, NEG, NEG));
     });
-    hi = wave_max(hi);
-    lo = -wave_max(-lo);
-    if (lane == 0) { s_hi[wave] = hi; s_lo[wave] = lo; }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < NW; ++i) {
-        hi = fmaxf(hi, s_hi[i]);
-        lo = fminf(lo, s_lo[i]);
+    meet();
+    if (lo == NEG && hi > NEG) {
+        lo = -NEG;
+        each4([&](int, const float4 z) {
+            auto some = [](float x) { return x > NEG ? x : -NEG; };
+            lo = fminf(fminf(lo, fminf(some(z.x), some(z.y))), fminf(some(z.z), some(z.w)));
+        });
+        __syncthreads();         // the others have read s_hi and s_lo
+        meet();
     }
-    const bool none = hi == NEG, greedy = a.temperature == 0.0;
-    const Weights w{hi, greedy ? 0.0 : STEPS * 1.4426950408889634 / a.temperature, table};
+    const bool none = hi == NEG;
+    // with infinite entries the largest finite number takes the maximum's place
+    const float top = fminf(hi, MOST);
+    const double per_x = STEPS * 1.4426950408889634, c_w = greedy ? 0.0 : per_x / a.temperature, per_z = a.temperature * 0.6931471805599453;
+    auto at_least = [&](double bits) { return (float)fmax((double)top - bits * per_z, -(double)MOST); };
+    const Weights w{(double)top, c_w, at_least(900.0), at_least(ONE + 2.0), table};
     // the border, so far: entries above b_z stay, and those at it up to index b_i
     float b_z = NEG;
     int b_i = -1;
@@ -212,29 +254,25 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
     // ---- the head of what is inside that ends with the entry at which the count, or the mass, reaches want(all of it)
     // Bins along the value: linear over the range of the row, or over the first 128 below the maximum (masks of very low values).
     // Float subtraction and multiplication by a positive number are monotone, so a larger value is never in a later bin.
-    // Nothing here is a NaN: with infinite entries the maximum's place takes the largest finite number.
-    const float top = fminf(hi, MOST), scale = (float)BINS / fmaxf(fminf(top - lo, 128.f), 1e-30f);
+    const float scale = (float)BINS / fmaxf(fminf(top - lo, 128.f), 1e-30f);
     auto bin_of = [&](float z) { return (int)__builtin_amdgcn_fmed3f((top - z) * scale, 0.f, (float)(BINS - 1)); };
-    // where the prefix sum of the bins reaches want: s_bin, and the sum in front of it in s_front
-    auto cross = [&](u64 before, auto&& want) -> u64 {
-        constexpr int PER = BINS / NT;
-        u64 v[PER], sum = 0;
+    // where the prefix sum of the bins (of counts: their low words) reaches want: s_bin, and the sum in front of it in s_front
+    auto cross = [&](auto by_mass, u64 before, auto&& want) -> u64 {
+        typedef std::conditional_t<decltype(by_mass)::value, u64, uint32_t> X;
+        constexpr int BPT = BINS / NT;
+        X v[BPT], sum = 0;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) sum += v[i] = hist[tid * PER + i];
-        const u64 upto = wave_scan(sum);
+        for (int i = 0; i < BPT; ++i) sum += v[i] = (X)hist[tid * BPT + i];
+        const X upto = wave_scan(sum);
         if (lane == 63) s_wave[wave] = upto;
         __syncthreads();
-        u64 front = before + upto - sum, all = before;
+        const X waves = wave_scan(lane < NW ? (X)s_wave[lane] : X(0));
+        const u64 target = want(before + lane_of(waves, NW - 1));
+        u64 front = before + (wave ? lane_of(waves, wave - 1) : X(0)) + (upto - sum);
 #pragma unroll
-        for (int i = 0; i < NW; ++i) {
-            if (i < wave) front += s_wave[i];
-            all += s_wave[i];
-        }
-        const u64 target = want(all);
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
+        for (int i = 0; i < BPT; ++i) {
             if (front < target && front + v[i] >= target) {
-                s_bin = tid * PER + i;
+                s_bin = tid * BPT + i;
                 s_front = front;
             }
             front += v[i];
@@ -242,6 +280,29 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
         if (tid == 0) s_n = 0;
         __syncthreads();
         return target;
+    };
+    // the entry of the bin that was found at which target is reached, in the order of the ranks: s_border
+    auto order_bin = [&](auto by_mass, u64 front, u64 target, int n) {
+        constexpr bool MASS = decltype(by_mass)::value;
+        if (MASS) {
+            for (int t = tid; t < n; t += NT) candw[t] = w.integer(of_key((uint32_t)(cand[t] >> 32)), true);
+            __syncthreads();
+        }
+        for (int t = tid; t < n; t += NT) {
+            const u64 own = cand[t];
+            u64 before = front;
+#pragma unroll 4
+            for (int i = 0; i < n; ++i) {
+                const u64 amount = MASS ? candw[i] : 1ull;
+                before += cand[i] > own ? amount : 0;
+            }
+            if (before < target && before + (MASS ? candw[t] : 1ull) >= target) s_border = own;
+        }
+        __syncthreads();
+    };
+    auto take_border = [&]() {
+        b_z = of_key((uint32_t)(s_border >> 32));
+        b_i = (int)~(uint32_t)s_border;
     };
     auto find_border = [&](auto by_mass, auto&& want) {
         constexpr bool MASS = decltype(by_mass)::value;
@@ -255,41 +316,35 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
                     if (x[e]) atomicAdd(&hist[bin(e)], x[e]);
             } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (in[e]) atomicAdd(reinterpret_cast<uint32_t*>(&hist[bin(e)]), 1u);      // at most 2^18: the low words
+                for (int e = 0; e < 4; ++e) atomicAdd(reinterpret_cast<uint32_t*>(&hist[bin(e)]), in[e] ? 1u : 0u);      // at most 2^18: the low words
             }
         };
         each([&](int, const float z[4], const bool in[4]) { add(z, in, [&](int e) { return bin_of(z[e]); }); });
         __syncthreads();
-        const u64 target = cross(0, want);
+        const u64 target = cross(by_mass, 0, want);
         const int bin = s_bin;
         u64 front = s_front;
+        // the bin's entries lie between zl and zh, which are wider than it by more than the roundings of bin_of
+        const float width = 1.0f / scale, slack = (fabsf(top) + (bin + 1) * width) * 4.8e-7f;
+        const float zh = bin == 0 ? -NEG : top - bin * width + slack, zl = bin == BINS - 1 ? NEG : top - (bin + 1) * width - slack;
         each4([&](int i, const float4 v) {
             const float z[4] = {v.x, v.y, v.z, v.w};
+            bool near[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if ((bin_of(z[e]) == bin) & inside(i + e, z[e])) {
-                    const int at = atomicAdd(&s_n, 1);
-                    if (at < CAND) cand[at] = rank_of(z[e], i + e);
-                }
+            for (int e = 0; e < 4; ++e) near[e] = (z[e] >= zl) & (z[e] <= zh);
+            if (near[0] | near[1] | near[2] | near[3]) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (near[e] && bin_of(z[e]) == bin && inside(i + e, z[e])) {
+                        const int at = atomicAdd(&s_n, 1);
+                        if (at < CAND) cand[at] = rank_of(z[e], i + e);
+                    }
+            }
         });
         __syncthreads();
         const int n = s_n;
         if (n <= CAND) {
-            if (MASS) {
-                for (int t = tid; t < n; t += NT) candw[t] = w.integer(of_key((uint32_t)(cand[t] >> 32)));
-                __syncthreads();
-            }
-            for (int t = tid; t < n; t += NT) {
-                const u64 own = cand[t];
-                u64 before = front;
-                for (int i = 0; i < n; ++i) {
-                    const u64 amount = MASS ? candw[i] : 1ull;
-                    before += cand[i] > own ? amount : 0;
-                }
-                if (before < target && before + (MASS ? candw[t] : 1ull) >= target) s_border = own;
-            }
-            __syncthreads();
+            order_bin(by_mass, front, target, n);
         } else {
             // by the digits of the rank, the largest first: 32 bits of the value, and the 18 of an index that can differ
             auto short_rank = [](float z, int i) { return (u64)key_of(z) << 18 | ((uint32_t)~i & 0x3FFFFu); };
@@ -305,15 +360,14 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
                     add(z, here, [&](int e) { return BINS - 1 - (int)(short_rank(z[e], i + e) >> shift & (BINS - 1)); });
                 });
                 __syncthreads();
-                cross(front, [&](u64) { return target; });
+                cross(by_mass, front, [&](u64) { return target; });
                 front = s_front;
                 known = known << DIGIT | (BINS - 1 - s_bin);
             }
             if (tid == 0) s_border = known >> 18 << 32 | 0xFFFC0000ull | (known & 0x3FFFFu);
             __syncthreads();
         }
-        b_z = of_key((uint32_t)(s_border >> 32));
-        b_i = (int)~(uint32_t)s_border;
+        take_border();
     };
     static_assert(BINS == 1 << DIGIT, "a bin for every digit");
     bool cleared = true;
@@ -324,18 +378,79 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
         }
         cleared = false;
     };
+    const bool listed = by_list && !none;
+    float lz[PER];
+    uint32_t lat[PER];
     if (!none) {
-        const int top_k = greedy ? 1 : a.top_k;
-        if (top_k > 0 && top_k < V) {      // all of a row's entries stay where fewer than top_k are not masked
+        auto share = [&](u64 all) {
+            const u64 t = (u64)__builtin_ceil(a.top_p * (double)all);      // the mass in front of the next entry is below top_p of all
+            return t < 1 ? 1ull : t < all ? t : all;
+        };
+        const bool top_p = !greedy && a.top_p < 1.0;
+        if (top_k > 0 && top_k < V) {
             clear_hist();
-            find_border(std::false_type{}, [&](u64 all) { return all < (u64)top_k ? all : (u64)top_k; });
+            find_border(std::false_type{}, [&](u64 all) { return all < (u64)top_k ? all : (u64)top_k; });      // fewer are not masked: all of them
         }
-        if (!greedy && a.top_p < 1.0) {
-            clear_hist();
-            find_border(std::true_type{}, [&](u64 all) {
-                const u64 t = (u64)__builtin_ceil(a.top_p * (double)all);      // the mass in front of the next entry is below top_p of all
-                return t < 1 ? 1ull : t < all ? t : all;
+        if (listed) {
+            each([&](int i, const float z[4], const bool in[4]) {
+                u64 b[4];
+                int upto[5] = {0};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    b[e] = __ballot(in[e]);
+                    upto[e + 1] = upto[e] + __popcll(b[e]);
+                }
+                if (upto[4] == 0) return;
+                int base = 0;
+                if (lane == 0) base = atomicAdd(&s_listed, upto[4]);
+                base = __builtin_amdgcn_readfirstlane(base);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (in[e]) {
+                        const int at = base + upto[e] + __builtin_amdgcn_mbcnt_hi((uint32_t)(b[e] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)b[e], 0));
+                        list_z[at] = z[e];
+                        list_at[at] = (uint32_t)wave << 18 | (uint32_t)(i + e);
+                    }
             });
+            clear_hist();
+            __syncthreads();
+            const int n = s_listed;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int t = tid + i * NT;
+                lz[i] = t < n ? list_z[t] : NEG;
+                lat[i] = t < n ? list_at[t] : 0;
+            }
+            if (top_p) {
+#pragma unroll
+                for (int i = 0; i < PER; ++i)
+                    if (lz[i] > NEG) {
+                        const u64 x = w.integer(lz[i], true);
+                        if (x) atomicAdd(&hist[bin_of(lz[i])], x);
+                    }
+                __syncthreads();
+                const u64 target = cross(std::true_type{}, 0, share);
+                const int bin = s_bin;
+                const u64 front = s_front;
+#pragma unroll
+                for (int i = 0; i < PER; ++i)
+                    if (lz[i] > NEG && bin_of(lz[i]) == bin) {
+                        const int at = atomicAdd(&s_n, 1);
+                        if (at < CAND) cand[at] = rank_of(lz[i], (int)(lat[i] & 0x3FFFFu));
+                    }
+                __syncthreads();
+                if (s_n <= CAND) {
+                    order_bin(std::true_type{}, front, target, s_n);
+                    take_border();
+                } else {
+                    for (int i = tid; i < BINS; i += NT) hist[i] = 0;
+                    __syncthreads();
+                    find_border(std::true_type{}, share);
+                }
+            }
+        } else if (top_p) {
+            clear_hist();
+            find_border(std::true_type{}, share);
         }
     }
     // min-p: the least value with enough weight, from where its logarithm says, a step of float32 at a time
@@ -354,70 +469,74 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
 
     // ---- the draw: the mass that stays, by wavefronts (in index order), then the run, the lane and the entry
     u64 total = 0;
-    if (a.tokens || a.probs) {
-        u64 sum = 0;
-        each([&](int, const float z[4], const bool in[4]) {
-            u64 x[4];
-            w.integers(z, in, x);
-            sum += (x[0] + x[1]) + (x[2] + x[3]);
-        });
-        sum = last_lane(wave_scan(sum));
+    if (a.tokens || probs) {
         __syncthreads();                    // s_wave of the searches has been read
-        if (lane == 0) s_wave[wave] = sum;
-        __syncthreads();
-        u64 front = 0;
+        if (listed) {
 #pragma unroll
-        for (int i = 0; i < NW; ++i) {
-            if (i < wave) front += s_wave[i];
-            total += s_wave[i];
+            for (int i = 0; i < PER; ++i) {
+                const u64 x = lz[i] > NEG && inside((int)(lat[i] & 0x3FFFFu), lz[i]) ? w.integer(lz[i], true) : 0;
+                if (x) atomicAdd(&s_mass[lat[i] >> 18], x);
+            }
+        } else {
+            u64 sum = 0;
+            each([&](int, const float z[4], const bool in[4]) {
+                u64 x[4];
+                w.integers(z, in, x);
+                sum += (x[0] + x[1]) + (x[2] + x[3]);
+            });
+            sum = lane_of(wave_scan(sum), 63);
+            if (lane == 0) s_mass[wave] = sum;
         }
+        __syncthreads();
+        const u64 own = lane < NW ? s_mass[lane] : 0, waves = wave_scan(own);
+        total = lane_of(waves, NW - 1);
         if (a.tokens) {
             float u = a.u[r];
             u = u > 0.f ? (u < 1.f ? u : 0.99999994f) : 0.f;
             const u64 target = (u64)((double)u * (double)total);
             if (none && tid == 0) a.tokens[r] = -1;
-            if (front <= target && target < front + sum) {      // uniform over the wavefront
+            u64 front = wave ? lane_of(waves, wave - 1) : 0;
+            if (front <= target && target < lane_of(waves, wave)) {      // uniform over the wavefront
                 each([&](int i, const float z[4], const bool in[4]) {
                     u64 x[4];
                     w.integers(z, in, x);
                     const u64 own = (x[0] + x[1]) + (x[2] + x[3]), upto = wave_scan(own), c0 = front + upto - own;
                     if (target >= c0 && target < c0 + own)
                         a.tokens[r] = target < c0 + x[0] ? i : target < c0 + x[0] + x[1] ? i + 1 : target < c0 + x[0] + x[1] + x[2] ? i + 2 : i + 3;
-                    front += last_lane(upto);
+                    front += lane_of(upto, 63);
                 });
             }
         }
     }
     // ---- what stays
-    if (a.probs || a.kept) {
+    if (probs || kept) {
         const double inv = total ? 1.0 / scalbn((double)total, -ONE) : 0.0, inv_t = greedy ? 1.0 : 1.0 / a.temperature;
-        auto put = [&](float* row, int i, const float4 v) {
-            if ((V & 3) == 0 && ((uintptr_t)row & 15) == 0) {
-                if (i < V) *reinterpret_cast<float4*>(row + i) = v;
-            } else {
-                if (i < V) row[i] = v.x;
-                if (i + 1 < V) row[i + 1] = v.y;
-                if (i + 2 < V) row[i + 2] = v.z;
-                if (i + 3 < V) row[i + 3] = v.w;
+        auto logit = [&](bool s, float x) { return s ? fmaxf(-MOST, fminf(MOST, (float)((double)x * inv_t))) : NEG; };
+        auto prob = [&](bool s, float x) { return s ? (float)(w.value(x) * inv) : 0.f; };
+        if (listed) {
+            __syncthreads();                // what the entries are written over has been written (a barrier waits for that)
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int at = (int)(lat[i] & 0x3FFFFu);
+                if (lz[i] > NEG && inside(at, lz[i])) {
+                    if (probs) probs[at] = prob(true, lz[i]);
+                    if (kept) kept[at] = logit(true, lz[i]);
+                }
             }
-        };
-        each4([&](int i, const float4 z) {
-            const bool s0 = inside(i, z.x), s1 = inside(i + 1, z.y), s2 = inside(i + 2, z.z), s3 = inside(i + 3, z.w);
-            if (a.probs) put(a.probs + r * V, i, make_float4(s0 ? (float)(w.value(z.x) * inv) : 0.f, s1 ? (float)(w.value(z.y) * inv) : 0.f,
-                                                             s2 ? (float)(w.value(z.z) * inv) : 0.f, s3 ? (float)(w.value(z.w) * inv) : 0.f));
-            if (a.kept) {
-                auto t = [&](bool s, float x) { return s ? fmaxf(-MOST, fminf(MOST, (float)((double)x * inv_t))) : NEG; };
-                put(a.kept + r * V, i, make_float4(t(s0, z.x), t(s1, z.y), t(s2, z.z), t(s3, z.w)));
-            }
-        });
+        } else {
+            each([&](int i, const float z[4], const bool s[4]) {
+                if (probs) put(probs, i, make_float4(prob(s[0], z[0]), prob(s[1], z[1]), prob(s[2], z[2]), prob(s[3], z[3])));
+                if (kept) put(kept, i, make_float4(logit(s[0], z[0]), logit(s[1], z[1]), logit(s[2], z[2]), logit(s[3], z[3])));
+            });
+        }
     }
 }
 
-template <int NT, bool LDS>
+template <int NT, bool LDS, int PER>
 void run(const SampleArgs& a, hipStream_t st) {
     const int runs = (a.V + NT * 4 - 1) / (NT * 4);
     const int lds = LDS ? runs * NT * (int)sizeof(float4) : 0;
-    auto kern = k_sample<NT, LDS>;
+    auto kern = k_sample<NT, LDS, PER>;
     if constexpr (LDS) {
         static int attr_state = 0;
         if (!ensure_dynamic_lds(reinterpret_cast<const void*>(kern), LDS_ENTRIES * 4, &attr_state)) return;
@@ -428,12 +547,12 @@ void run(const SampleArgs& a, hipStream_t st) {
 }  // namespace
 
 void launch_sample_filtered(const SampleArgs& a, hipStream_t st) {
-    if (a.V <= 2048) run<256, true>(a, st);
+    if (a.V <= 2048) run<256, true, 2>(a, st);
     else if (a.V <= LDS_ENTRIES) {
-        if (a.rows > cu_count()) run<512, true>(a, st);
-        else run<1024, true>(a, st);
+        if (a.rows > cu_count()) run<512, true, 1>(a, st);
+        else run<1024, true, 2>(a, st);
     }
-    else run<1024, false>(a, st);
+    else run<1024, false, 2>(a, st);
 }
 
 }  // namespace mulo
