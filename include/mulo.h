@@ -417,7 +417,7 @@ typedef struct {
 /* Filters rows of logits and draws from what stays, without a context (allocates nothing, runs on the current HIP device).
  *   logits      device, dtype (mulo_dtype) [rows, vocab], row r at r * row_stride elements; with guidance [2 rows, vocab],
  *               row r conditional and row `rows` + r its unconditional twin.  Aligned to its element; 16-byte aligned rows
- *               are read faster.  NaN counts as -inf; +inf takes all the mass, shared by all that are +inf
+ *               are read faster.  NaN counts as -inf, +inf as the largest finite number
  *   u           device float32 [rows] in [0, 1) (what lies outside counts as the nearest in it, NaN as 0); NULL allowed
  *               without tokens
  *   tokens      device int32 [rows] (out) or NULL: the first entry, by index, up to which the mass that stays exceeds u times

@@ -26,6 +26,7 @@ constexpr int BINS = 1024, CAND = 512;    // bins of a histogram; entries of a b
 constexpr int DIGIT = 10;                 // bits of a rank that a histogram of them tells apart
 constexpr int LDS_ENTRIES = 32768;        // of a row that is kept in LDS (128 KB)
 constexpr int ONE = 44;                   // bits of the largest weight
+static_assert(ONE == 44, "Weights::value");
 
 // order-preserving integer of a value (not NaN); -0 and 0 are the same value
 __device__ __forceinline__ uint32_t key_of(float z) {
@@ -36,39 +37,42 @@ __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k &
 __device__ __forceinline__ u64 rank_of(float z, int i) { return (u64)key_of(z) << 32 | (uint32_t)~i; }
 
 // Weights, 2^x with x = (z - max z) log2(e) / T <= 0.  y = STEPS x = n + f, |f| <= 1/2:
-//   2^x = 2^(n / STEPS) e^t, t = f ln 2 / STEPS, |t| <= 1.4e-3
-// The first factor is a table's, its exponent moved.  e^t - 1 = t + t^2 (1/2 + t (1/6 + t / 24)): the sum's second part is below
-// 2^-20 and float32 is enough for it, so that 10 operations in 64 bits are left, at 8 cycles each half of the time (a
-// polynomial of 2^x over all of [-1/2, 1/2] takes 18).  Relative error: 2^-43.
-constexpr int STEPS = 256;
+//   2^x = 2^(n / STEPS) e^t, t = f ln 2 / STEPS, |t| <= 6.8e-4
+// The first factor is a table's, its exponent moved.  e^t - 1 = t + t^2 (1/2 + t / 6), less than t^4 / 24 = 2^-46 of it left
+// out; the sum's second part is below 2^-22 and float32 is enough for it.  18 instructions, all of which issue at the same
+// rate (a polynomial of 2^x over all of [-1/2, 1/2] takes 10 more).  Relative error: 2^-44.
+constexpr int STEPS = 512;
 struct Weights {
-    double zmax, c;            // the maximum (of infinite ones: the largest finite number); STEPS log2(e) / temperature
+    double zmax, c;            // the maximum; STEPS log2(e) / temperature
     float least_value, least;  // smallest z with a weight that value(), and integer(), tell from 0
-    const double* table;       // 2^(i / STEPS), in LDS
-    __device__ __forceinline__ double part(float z, int bits) const {     // 2^(x + bits), for z of at least least_value
-        const double shift = 6755399441055744.0;      // 1.5 2^52: the sum's low word is the nearest integer
-        const double d = (double)fminf(z, MOST) - zmax;
+    const double* table;       // 2^(ONE + i / STEPS), in LDS
+    __device__ __forceinline__ double part(float z) const {     // 2^(ONE + x), for z of at least least_value
+        constexpr double K = 0.6931471805599453 / STEPS, shift = 6755399441055744.0;      // 1.5 2^52: the sum's low word is the nearest integer
+        const double d = (double)z - zmax;
         const double ys = __builtin_fma(d, c, shift), f = __builtin_fma(d, c, -(ys - shift));
-        const int n = (int)__double_as_longlong(ys);
-        const long long tb = __double_as_longlong(table[n & (STEPS - 1)]) + ((long long)((n >> 8) + bits) << 52);
-        const float t = (float)f * (float)(0.6931471805599453 / STEPS);
-        const double r = __builtin_fma(f, 0.6931471805599453 / STEPS, (double)(t * t * __builtin_fmaf(t, __builtin_fmaf(t, 1.f / 24.f, 1.f / 6.f), 0.5f)));
-        const double tw = __longlong_as_double(tb);
+        const uint32_t n = (uint32_t)__double_as_longlong(ys);
+        const u64 tb = (u64)__double_as_longlong(table[n & (STEPS - 1)]);
+        const double tw = __longlong_as_double((long long)((u64)((uint32_t)(tb >> 32) + ((n & ~(STEPS - 1u)) << (20 - LOG_STEPS))) << 32 | (uint32_t)tb));
+        const float t = (float)f;
+        const double r = __builtin_fma(f, K, (double)(t * t * __builtin_fmaf(t, (float)(K * K * K / 6), (float)(K * K / 2))));
         return __builtin_fma(tw, r, tw);
     }
-    __device__ __forceinline__ u64 integer(float z, bool in) const {       // + 2^52: rounds to an integer
-        const u64 t = __double_as_longlong(part(z, ONE) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
-        return (in && z >= least) ? t : 0;
-    }
-    // of the entries of four that are in: side by side, without a branch
+    static constexpr int LOG_STEPS = 9;
+    static_assert(STEPS == 1 << LOG_STEPS, "the steps");
+    // + 2^52: rounds to an integer.  Of an entry below `least` the result means nothing.
+    __device__ __forceinline__ u64 integer(float z) const { return (u64)__double_as_longlong(part(z) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull; }
+    // the weights of the entries of four that are in, 0 of the others: side by side, without a branch
     __device__ __forceinline__ void integers(const float z[4], const bool in[4], u64 out[4]) const {
 #pragma unroll
         for (int e = 0; e < 4; ++e) out[e] = 0;
         if (!__any(in[0] || in[1] || in[2] || in[3])) return;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) out[e] = integer(z[e], in[e]);
+        for (int e = 0; e < 4; ++e) {
+            const u64 t = integer(z[e]);
+            out[e] = in[e] && z[e] >= least ? t : 0;
+        }
     }
-    __device__ __forceinline__ double value(float z) const { return z >= least_value ? part(z, 0) : 0.0; }
+    __device__ __forceinline__ double value(float z) const { return z >= least_value ? part(z) * 0x1p-44 : 0.0; }
 };
 
 // Sums and maxima over the lanes of a wavefront by data-parallel moves: shifts by 1, 2, 4, 8 inside a row of 16 lanes, then the
@@ -123,11 +127,12 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
     __shared__ double table[STEPS];
     __shared__ u64 s_wave[NW], s_mass[NW], s_front, s_border;
     __shared__ float s_lo[NW], s_hi[NW];
-    __shared__ int s_bin, s_n, s_listed;
-    __shared__ float list_z[PER * NT];
-    __shared__ uint32_t list_at[PER * NT];         // wavefront << 18 | index
+    __shared__ int s_bin, s_n, s_count[NW];
+    constexpr bool OWN_LIST = PER * NT > BINS;     // else the list passes through the histogram's place
+    __shared__ u64 own_list[OWN_LIST ? PER * NT : 1];
     u64* const cand = hist;
     u64* const candw = hist + CAND;
+    u64* const list = OWN_LIST ? own_list : hist;  // value << 32 | index
 
     const int64_t r = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), V = a.V;
@@ -153,12 +158,13 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
         };
         return make_float4(one(i), one(i + 1), one(i + 2), one(i + 3));
     };
-    auto row4 = [&](int i, float4 c, float4 u) -> float4 {     // guided; NaN (a maximum's other operand), and what lies past the end, is masked
+    auto row4 = [&](int i, float4 c, float4 u) -> float4 {     // guided; NaN, and what lies past the end, is masked; +inf is the largest finite number
         if (zu) {
             auto guide = [&](float x, float y) { return __fadd_rn(y, __fmul_rn(a.cfg_scale, __fsub_rn(x, y))); };
             c = make_float4(guide(c.x, u.x), guide(c.y, u.y), guide(c.z, u.z), guide(c.w, u.w));
         }
-        c = make_float4(fmaxf(c.x, NEG), fmaxf(c.y, NEG), fmaxf(c.z, NEG), fmaxf(c.w, NEG));
+        auto clean = [](float z) { return fminf(fmaxf(z, NEG), MOST); };      // of a NaN and a number the maximum is the number
+        c = make_float4(clean(c.x), clean(c.y), clean(c.z), clean(c.w));
         if (i - lane * 4 + 256 > V) c = make_float4(i < V ? c.x : NEG, i + 1 < V ? c.y : NEG, i + 2 < V ? c.z : NEG, i + 3 < V ? c.w : NEG);
         return c;
     };
@@ -195,9 +201,6 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
         }
     };
     for (int i = tid; i < BINS; i += NT) hist[i] = 0;
-    if (tid < STEPS) table[tid] = exp2((double)tid / STEPS);
-    if (tid < NW) s_mass[tid] = 0;
-    if (tid == 0) s_listed = 0;
     const bool greedy = a.temperature == 0.0;
     const int top_k = greedy ? 1 : a.top_k;
     // (from memory in every pass, the row has to stay as it is where the filtered logits take its place)
@@ -223,6 +226,7 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
         if (by_list && probs) put(probs, i, make_float4(0.f, 0.f, 0.f, 0.f));
         if (by_list && kept) put(kept, i, make_float4(NEG, NEG, NEG, NEG));
     });
+    for (int i = tid; i < STEPS; i += NT) table[i] = exp2((double)ONE + (double)i / STEPS);      // while the row is on its way
     meet();
     if (lo == NEG && hi > NEG) {
         lo = -NEG;
@@ -234,19 +238,27 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
         meet();
     }
     const bool none = hi == NEG;
-    // with infinite entries the largest finite number takes the maximum's place
-    const float top = fminf(hi, MOST);
-    const double per_x = STEPS * 1.4426950408889634, c_w = greedy ? 0.0 : per_x / a.temperature, per_z = a.temperature * 0.6931471805599453;
+    const float top = hi;
+    const double per_z = a.temperature * 0.6931471805599453;
     auto at_least = [&](double bits) { return (float)fmax((double)top - bits * per_z, -(double)MOST); };
-    const Weights w{(double)top, c_w, at_least(900.0), at_least(ONE + 2.0), table};
+    const Weights w{(double)top, greedy ? 0.0 : STEPS * 1.4426950408889634 / a.temperature, at_least(900.0), at_least(ONE + 2.0), table};
     // the border, so far: entries above b_z stay, and those at it up to index b_i
     float b_z = NEG;
     int b_i = -1;
     auto inside = [&](int i, float z) -> bool { return (z > b_z) | ((z == b_z) & (i <= b_i)); };
-    auto each = [&](auto&& f) {      // f(index of the first, the four, which of them are inside)
+    auto above = [](float z) { return of_key(key_of(z) + 1); };
+    // f(index of the first, the four, which of them are inside).  Whether an entry at b_z is inside is the same for a whole run,
+    // but for the run that holds b_i: there those that are not are masked first.
+    auto each = [&](auto&& f) {
         each4([&](int i, const float4 v) {
-            const float z[4] = {v.x, v.y, v.z, v.w};
-            const bool in[4] = {inside(i, v.x), inside(i + 1, v.y), inside(i + 2, v.z), inside(i + 3, v.w)};
+            const int r0 = __builtin_amdgcn_readfirstlane(i - lane * 4);
+            float z[4] = {v.x, v.y, v.z, v.w};
+            if (r0 <= b_i && r0 + 255 > b_i) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) z[e] = z[e] == b_z && i + e > b_i ? NEG : z[e];
+            }
+            const float t = r0 <= b_i ? b_z : above(b_z);
+            const bool in[4] = {z[0] >= t, z[1] >= t, z[2] >= t, z[3] >= t};
             f(i, z, in);
         });
     };
@@ -285,7 +297,10 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
     auto order_bin = [&](auto by_mass, u64 front, u64 target, int n) {
         constexpr bool MASS = decltype(by_mass)::value;
         if (MASS) {
-            for (int t = tid; t < n; t += NT) candw[t] = w.integer(of_key((uint32_t)(cand[t] >> 32)), true);
+            for (int t = tid; t < n; t += NT) {
+                const float z = of_key((uint32_t)(cand[t] >> 32));
+                candw[t] = z >= w.least ? w.integer(z) : 0;
+            }
             __syncthreads();
         }
         for (int t = tid; t < n; t += NT) {
@@ -309,11 +324,13 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
         // adds the counts, or the weights, of entries to their bins
         auto add = [&](const float z[4], const bool in[4], auto&& bin) {
             if constexpr (MASS) {
+                if (!__any(in[0] || in[1] || in[2] || in[3])) return;
                 u64 x[4];
-                w.integers(z, in, x);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = w.integer(z[e]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (x[e]) atomicAdd(&hist[bin(e)], x[e]);
+                    if (in[e] && z[e] >= w.least) atomicAdd(&hist[bin(e)], x[e]);
             } else {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) atomicAdd(reinterpret_cast<uint32_t*>(&hist[bin(e)]), in[e] ? 1u : 0u);      // at most 2^18: the low words
@@ -392,42 +409,47 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
             find_border(std::false_type{}, [&](u64 all) { return all < (u64)top_k ? all : (u64)top_k; });      // fewer are not masked: all of them
         }
         if (listed) {
+            // in the order of the indexes: first how many of every wavefront
+            int count = 0;
+            each([&](int, const float[4], const bool in[4]) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) count += __popcll(__ballot(in[e]));
+            });
+            if (lane == 0) s_count[wave] = count;
+            __syncthreads();
+            const uint32_t counts = wave_scan(lane < NW ? (uint32_t)s_count[lane] : 0u);
+            int base = (int)lane_of(counts, wave) - count;
             each([&](int i, const float z[4], const bool in[4]) {
                 u64 b[4];
-                int upto[5] = {0};
+                int before = base;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     b[e] = __ballot(in[e]);
-                    upto[e + 1] = upto[e] + __popcll(b[e]);
+                    base += __popcll(b[e]);
+                    before = __builtin_amdgcn_mbcnt_hi((uint32_t)(b[e] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)b[e], before));
                 }
-                if (upto[4] == 0) return;
-                int base = 0;
-                if (lane == 0) base = atomicAdd(&s_listed, upto[4]);
-                base = __builtin_amdgcn_readfirstlane(base);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (in[e]) {
-                        const int at = base + upto[e] + __builtin_amdgcn_mbcnt_hi((uint32_t)(b[e] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)b[e], 0));
-                        list_z[at] = z[e];
-                        list_at[at] = (uint32_t)wave << 18 | (uint32_t)(i + e);
+                        list[before++] = (u64)__float_as_uint(z[e]) << 32 | (uint32_t)(i + e);
                     }
             });
-            clear_hist();
             __syncthreads();
-            const int n = s_listed;
+            const int n = (int)lane_of(counts, NW - 1);
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int t = tid + i * NT;
-                lz[i] = t < n ? list_z[t] : NEG;
-                lat[i] = t < n ? list_at[t] : 0;
+                const int t = tid * PER + i;
+                lz[i] = t < n ? __uint_as_float((uint32_t)(list[t] >> 32)) : NEG;
+                lat[i] = t < n ? (uint32_t)list[t] : 0;
+            }
+            if (top_p) {
+                __syncthreads();
+                clear_hist();
             }
             if (top_p) {
 #pragma unroll
                 for (int i = 0; i < PER; ++i)
-                    if (lz[i] > NEG) {
-                        const u64 x = w.integer(lz[i], true);
-                        if (x) atomicAdd(&hist[bin_of(lz[i])], x);
-                    }
+                    if (lz[i] >= w.least) atomicAdd(&hist[bin_of(lz[i])], w.integer(lz[i]));
                 __syncthreads();
                 const u64 target = cross(std::true_type{}, 0, share);
                 const int bin = s_bin;
@@ -436,7 +458,7 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
                 for (int i = 0; i < PER; ++i)
                     if (lz[i] > NEG && bin_of(lz[i]) == bin) {
                         const int at = atomicAdd(&s_n, 1);
-                        if (at < CAND) cand[at] = rank_of(lz[i], (int)(lat[i] & 0x3FFFFu));
+                        if (at < CAND) cand[at] = rank_of(lz[i], (int)lat[i]);
                     }
                 __syncthreads();
                 if (s_n <= CAND) {
@@ -470,40 +492,43 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
     // ---- the draw: the mass that stays, by wavefronts (in index order), then the run, the lane and the entry
     u64 total = 0;
     if (a.tokens || probs) {
-        __syncthreads();                    // s_wave of the searches has been read
+        float u = a.u ? a.u[r] : 0.f;
+        u = u > 0.f ? (u < 1.f ? u : 0.99999994f) : 0.f;
+        u64 x[PER], sum = 0, upto;
         if (listed) {
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const u64 x = lz[i] > NEG && inside((int)(lat[i] & 0x3FFFFu), lz[i]) ? w.integer(lz[i], true) : 0;
-                if (x) atomicAdd(&s_mass[lat[i] >> 18], x);
-            }
+            for (int i = 0; i < PER; ++i) sum += x[i] = lz[i] >= w.least && inside((int)lat[i], lz[i]) ? w.integer(lz[i]) : 0;
         } else {
-            u64 sum = 0;
             each([&](int, const float z[4], const bool in[4]) {
                 u64 x[4];
                 w.integers(z, in, x);
                 sum += (x[0] + x[1]) + (x[2] + x[3]);
             });
-            sum = lane_of(wave_scan(sum), 63);
-            if (lane == 0) s_mass[wave] = sum;
         }
+        upto = wave_scan(sum);
+        if (lane == 63) s_mass[wave] = upto;
         __syncthreads();
-        const u64 own = lane < NW ? s_mass[lane] : 0, waves = wave_scan(own);
+        const u64 waves = wave_scan(lane < NW ? s_mass[lane] : 0);
         total = lane_of(waves, NW - 1);
-        if (a.tokens) {
-            float u = a.u[r];
-            u = u > 0.f ? (u < 1.f ? u : 0.99999994f) : 0.f;
-            const u64 target = (u64)((double)u * (double)total);
-            if (none && tid == 0) a.tokens[r] = -1;
-            u64 front = wave ? lane_of(waves, wave - 1) : 0;
-            if (front <= target && target < lane_of(waves, wave)) {      // uniform over the wavefront
+        const u64 target = (u64)((double)u * (double)total);
+        u64 front = wave ? lane_of(waves, wave - 1) : 0;
+        if (none && tid == 0 && a.tokens) a.tokens[r] = -1;
+        if (a.tokens && front <= target && target < lane_of(waves, wave)) {      // uniform over the wavefront
+            if (listed) {
+                front += upto - sum;
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    if (front <= target && target < front + x[i]) a.tokens[r] = (int)lat[i];
+                    front += x[i];
+                }
+            } else {
                 each([&](int i, const float z[4], const bool in[4]) {
                     u64 x[4];
                     w.integers(z, in, x);
-                    const u64 own = (x[0] + x[1]) + (x[2] + x[3]), upto = wave_scan(own), c0 = front + upto - own;
+                    const u64 own = (x[0] + x[1]) + (x[2] + x[3]), run = wave_scan(own), c0 = front + run - own;
                     if (target >= c0 && target < c0 + own)
                         a.tokens[r] = target < c0 + x[0] ? i : target < c0 + x[0] + x[1] ? i + 1 : target < c0 + x[0] + x[1] + x[2] ? i + 2 : i + 3;
-                    front += lane_of(upto, 63);
+                    front += lane_of(run, 63);
                 });
             }
         }
@@ -511,13 +536,16 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
     // ---- what stays
     if (probs || kept) {
         const double inv = total ? 1.0 / scalbn((double)total, -ONE) : 0.0, inv_t = greedy ? 1.0 : 1.0 / a.temperature;
-        auto logit = [&](bool s, float x) { return s ? fmaxf(-MOST, fminf(MOST, (float)((double)x * inv_t))) : NEG; };
+        auto logit = [&](bool s, float x) {
+            if (inv_t != 1.0) x = __builtin_amdgcn_fmed3f((float)((double)x * inv_t), -MOST, MOST);
+            return s ? x : NEG;
+        };
         auto prob = [&](bool s, float x) { return s ? (float)(w.value(x) * inv) : 0.f; };
         if (listed) {
             __syncthreads();                // what the entries are written over has been written (a barrier waits for that)
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int at = (int)(lat[i] & 0x3FFFFu);
+                const int at = (int)lat[i];
                 if (lz[i] > NEG && inside(at, lz[i])) {
                     if (probs) probs[at] = prob(true, lz[i]);
                     if (kept) kept[at] = logit(true, lz[i]);
