@@ -143,44 +143,53 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
     const size_t esz = bf16 ? 2 : 4;
     const char* const zc = (const char*)a.logits + r * a.row_stride * esz;
     const char* const zu = a.logits_u ? (const char*)a.logits_u + r * a.row_stride * esz : nullptr;
-    // whole vectors where rows allow it (entries past the end re-read the row's first)
-    const bool vectors = (((uintptr_t)zc | (uintptr_t)zu) & (esz * 4 - 1)) == 0 && (V & 3) == 0;
-    auto raw4 = [&](const char* p, int i) -> float4 {
-        if (vectors) {
-            const size_t at = i < V ? i : 0;
-            if (!bf16) return *reinterpret_cast<const float4*>(p + at * 4);
-            const uint2 t = *reinterpret_cast<const uint2*>(p + at * 2);
-            return make_float4(__uint_as_float(t.x << 16), __uint_as_float(t.x & 0xFFFF0000u), __uint_as_float(t.y << 16), __uint_as_float(t.y & 0xFFFF0000u));
-        }
-        auto one = [&](int k) {
-            k = k < V ? k : 0;
-            return bf16 ? __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(p)[k] << 16) : reinterpret_cast<const float*>(p)[k];
-        };
-        return make_float4(one(i), one(i + 1), one(i + 2), one(i + 3));
+    // rows whose start and length allow it are read in whole vectors; runs that lie in the row as a whole, without a test of an entry
+    const bool vectors = (((uintptr_t)zc | (uintptr_t)zu) & (esz * 4 - 1)) == 0;
+    auto wide = [](uint2 t) {
+        return make_float4(__uint_as_float(t.x << 16), __uint_as_float(t.x & 0xFFFF0000u), __uint_as_float(t.y << 16), __uint_as_float(t.y & 0xFFFF0000u));
     };
-    auto row4 = [&](int i, float4 c, float4 u) -> float4 {     // guided; NaN, and what lies past the end, is masked; +inf is the largest finite number
-        if (zu) {
-            auto guide = [&](float x, float y) { return __fadd_rn(y, __fmul_rn(a.cfg_scale, __fsub_rn(x, y))); };
-            c = make_float4(guide(c.x, u.x), guide(c.y, u.y), guide(c.z, u.z), guide(c.w, u.w));
+    auto four_runs = [&](const char* row, int i, float4 v[4]) {      // entries i .. i + 3 and 256, 512 and 768 further on
+        if (vectors && i - lane * 4 + 1024 <= V) {
+            if (bf16) {
+                uint2 t[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) t[j] = reinterpret_cast<const uint2*>(row + (size_t)i * 2)[j * 64];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = wide(t[j]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = reinterpret_cast<const float4*>(row + (size_t)i * 4)[j * 64];
+            }
+        } else {
+            auto one = [&](int k) {      // entries past the end re-read the row's first
+                k = k < V ? k : 0;
+                return bf16 ? __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(row)[k] << 16) : reinterpret_cast<const float*>(row)[k];
+            };
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = make_float4(one(i + j * 256), one(i + j * 256 + 1), one(i + j * 256 + 2), one(i + j * 256 + 3));
         }
-        auto clean = [](float z) { return fminf(fmaxf(z, NEG), MOST); };      // of a NaN and a number the maximum is the number
-        c = make_float4(clean(c.x), clean(c.y), clean(c.z), clean(c.w));
-        if (i - lane * 4 + 256 > V) c = make_float4(i < V ? c.x : NEG, i + 1 < V ? c.y : NEG, i + 2 < V ? c.z : NEG, i + 3 < V ? c.w : NEG);
-        return c;
     };
-    // f(index of the first, four entries, number of the run), four runs requested together
+    // f(index of the first, four entries, number of the run), four runs requested together; guided; NaN, and what lies past the
+    // end, is masked.  (+inf becomes the largest finite number: below where the row is kept in LDS.)
     auto from_memory = [&](auto&& f) {
         for (int j0 = 0; j0 < w_runs; j0 += 4) {
-            float4 c[4], u[4] = {};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) c[j] = raw4(zc, first + (j0 + j) * 256);
+            float4 c[4];
+            four_runs(zc, first + j0 * 256, c);
             if (zu) {
+                float4 u[4];
+                four_runs(zu, first + j0 * 256, u);
+                auto guide = [&](float x, float y) { return __fadd_rn(y, __fmul_rn(a.cfg_scale, __fsub_rn(x, y))); };
 #pragma unroll
-                for (int j = 0; j < 4; ++j) u[j] = raw4(zu, first + (j0 + j) * 256);
+                for (int j = 0; j < 4; ++j) c[j] = make_float4(guide(c[j].x, u[j].x), guide(c[j].y, u[j].y), guide(c[j].z, u[j].z), guide(c[j].w, u[j].w));
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (j0 + j < w_runs) f(first + (j0 + j) * 256, row4(first + (j0 + j) * 256, c[j], u[j]), j0 + j);
+            for (int j = 0; j < 4; ++j) {
+                const int i = first + (j0 + j) * 256;
+                auto clean = [](float z) { z = fmaxf(z, NEG); return LDS ? z : fminf(z, MOST); };      // of a NaN and a number the maximum is the number
+                float4 v = make_float4(clean(c[j].x), clean(c[j].y), clean(c[j].z), clean(c[j].w));
+                if (i - lane * 4 + 256 > V) v = make_float4(i < V ? v.x : NEG, i + 1 < V ? v.y : NEG, i + 2 < V ? v.z : NEG, i + 3 < V ? v.w : NEG);
+                if (j0 + j < w_runs) f(i, v, j0 + j);
+            }
         }
     };
     auto each4 = [&](auto&& f) {
@@ -190,8 +199,9 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
             from_memory([&](int i, const float4 z, int) { f(i, z); });
         }
     };
+    const bool out_vectors = (((uintptr_t)a.probs | (uintptr_t)a.kept) & 15) == 0 && (V & 3) == 0;
     auto put = [&](float* row, int i, const float4 v) {
-        if ((V & 3) == 0 && ((uintptr_t)row & 15) == 0) {
+        if (out_vectors) {
             if (i < V) *reinterpret_cast<float4*>(row + i) = v;
         } else {
             if (i < V) row[i] = v.x;
@@ -236,6 +246,14 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
         });
         __syncthreads();         // the others have read s_hi and s_lo
         meet();
+    }
+    if (LDS && hi > MOST) {
+        for (int j = 0; j < w_runs; ++j) {
+            const float4 z = mine[j * 64];
+            mine[j * 64] = make_float4(fminf(z.x, MOST), fminf(z.y, MOST), fminf(z.z, MOST), fminf(z.w, MOST));
+        }
+        hi = MOST;
+        lo = fminf(lo, MOST);
     }
     const bool none = hi == NEG;
     const float top = hi;
@@ -475,16 +493,15 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
             find_border(std::true_type{}, share);
         }
     }
-    // min-p: the least value with enough weight, from where its logarithm says, a step of float32 at a time
+    // min-p: the least value with enough weight.  It is within a few steps of float32 of where its logarithm says: a lane looks at each.
     if (!greedy && a.min_p > 0.0 && !none) {
-        const uint32_t most = key_of(hi), least = key_of(-MOST);
-        auto enough = [&](uint32_t k) { return k >= most || w.value(of_key(k)) >= a.min_p; };
-        uint32_t k = key_of((float)fmax((double)hi + log(a.min_p) * a.temperature, -(double)MOST));
-        k = k < most ? k : most;
-        for (int i = 0; i < 8 && !enough(k); ++i) ++k;
-        for (int i = 0; i < 8 && k > least && enough(k - 1); ++i) --k;
-        if (of_key(k) > b_z) {
-            b_z = of_key(k);
+        const int64_t most = key_of(hi), least = key_of(-MOST), guess = key_of((float)fmax((double)hi + log(a.min_p) * a.temperature, -(double)MOST));
+        const int64_t at = guess - 32 + lane, k = at < least ? least : at < most ? at : most;
+        const float z = of_key((uint32_t)k);
+        const u64 enough = __ballot(k == most || w.value(z) >= a.min_p);      // of the last lane on, at the least
+        const float least_z = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(z), enough ? __builtin_ctzll(enough) : 63));
+        if (least_z > b_z) {
+            b_z = least_z;
             b_i = V;
         }
     }
@@ -536,10 +553,7 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
     // ---- what stays
     if (probs || kept) {
         const double inv = total ? 1.0 / scalbn((double)total, -ONE) : 0.0, inv_t = greedy ? 1.0 : 1.0 / a.temperature;
-        auto logit = [&](bool s, float x) {
-            if (inv_t != 1.0) x = __builtin_amdgcn_fmed3f((float)((double)x * inv_t), -MOST, MOST);
-            return s ? x : NEG;
-        };
+        auto logit = [&](bool s, float x) { return s ? __builtin_amdgcn_fmed3f((float)((double)x * inv_t), -MOST, MOST) : NEG; };
         auto prob = [&](bool s, float x) { return s ? (float)(w.value(x) * inv) : 0.f; };
         if (listed) {
             __syncthreads();                // what the entries are written over has been written (a barrier waits for that)
@@ -552,10 +566,9 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
                 }
             }
         } else {
-            each([&](int i, const float z[4], const bool s[4]) {
-                if (probs) put(probs, i, make_float4(prob(s[0], z[0]), prob(s[1], z[1]), prob(s[2], z[2]), prob(s[3], z[3])));
-                if (kept) put(kept, i, make_float4(logit(s[0], z[0]), logit(s[1], z[1]), logit(s[2], z[2]), logit(s[3], z[3])));
-            });
+            if (probs) each([&](int i, const float z[4], const bool s[4]) { put(probs, i, make_float4(prob(s[0], z[0]), prob(s[1], z[1]), prob(s[2], z[2]), prob(s[3], z[3]))); });
+            if (kept && inv_t == 1.0) each([&](int i, const float z[4], const bool s[4]) { put(kept, i, make_float4(s[0] ? z[0] : NEG, s[1] ? z[1] : NEG, s[2] ? z[2] : NEG, s[3] ? z[3] : NEG)); });
+            else if (kept) each([&](int i, const float z[4], const bool s[4]) { put(kept, i, make_float4(logit(s[0], z[0]), logit(s[1], z[1]), logit(s[2], z[2]), logit(s[3], z[3]))); });
         }
     }
 }
