@@ -402,7 +402,7 @@ MULO_API mulo_status mulo_attach_prefix(mulo_ctx *ctx, const mulo_prefix *prefix
 MULO_API mulo_status mulo_set_window(mulo_ctx *ctx, int32_t sinks, int32_t window);
 
 /* Filter of a distribution, in this order (host struct):
- *   cfg_scale    0: off.  s > 0: the row is z_u + s (z_c - z_u), as in mulo_step_params (float32, every operation rounded)
+ *   cfg_scale    0: off.  s > 0: the row is z_u + s (z_c - z_u) (guidance; float32, every operation rounded)
  *   temperature  w_x = exp((z_x - max z) / temperature); 0: only the first largest entry stays
  *   top_k        the top_k largest entries stay, of equal ones those with the lowest index; 0: all
  *   top_p        of those an entry stays iff the mass in front of it (larger ones, equal ones of lower index) is below top_p

@@ -178,7 +178,11 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
             if (zu) {
                 float4 u[4];
                 four_runs(zu, first + j0 * 256, u);
-                auto guide = [&](float x, float y) { return __fadd_rn(y, __fmul_rn(a.cfg_scale, __fsub_rn(x, y))); };
+                auto guide = [&](float x, float y) {
+#pragma clang fp contract(off)      // every operation is rounded: a fused one gives another value
+                    const float d = x - y, m = a.cfg_scale * d;
+                    return y + m;
+                };
 #pragma unroll
                 for (int j = 0; j < 4; ++j) c[j] = make_float4(guide(c[j].x, u[j].x), guide(c[j].y, u[j].y), guide(c[j].z, u[j].z), guide(c[j].w, u[j].w));
             }

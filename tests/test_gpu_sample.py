@@ -79,6 +79,13 @@ def test_filters_and_types(dtype, cfg):
         check(z, u, temperature=T, top_k=k, top_p=p, min_p=m, cfg_scale=cfg)
 
 
+@pytest.mark.parametrize("scale", [0.3, 1.0, 2.7, 7.5])
+def test_guidance_rounds_every_operation(scale):
+    z, u = rows_of(8, 5000, seed=21)
+    check(z, u[:4].contiguous(), cfg_scale=scale)
+    check(z, u[:4].contiguous(), cfg_scale=scale, top_k=700, top_p=0.9)
+
+
 def test_ties_go_to_the_lowest_index():
     g = torch.Generator().manual_seed(1)
     z = torch.randint(0, 4, (6, 3000), generator=g).float().to(DEV)          # about 750 entries of each value
