@@ -75,8 +75,29 @@ struct Plan {
     int prefix_split;  // stacked: shares of the prefix
     int prefix_wgs;    // workgroups of the prefix (the first ones of the grid)
 };
+// Division of x < 2^32 by a number that the host knows, by multiplication: with 2^(l - 1) < d <= 2^l and
+// m = floor(2^32 (2^l - d) / d) + 1, t = the high word of m x, the quotient is (t + (x - t) / 2^min(l, 1)) / 2^max(l - 1, 0)
+// (Granlund and Montgomery, "Division by invariant integers using multiplication").  A division by a kernel argument is
+// some 30 instructions in a row, and a workgroup has eight in front of its first load.
+struct Div {
+    uint32_t d, m, s1, s2;
+    Div() = default;
+    explicit Div(uint32_t by) : d(by) {
+        uint32_t l = 0;
+        while (((uint64_t)1 << l) < d) ++l;
+        m = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << l) - d)) / d + 1);
+        s1 = l < 1 ? l : 1;
+        s2 = l < 1 ? 0 : l - 1;
+    }
+    __device__ __forceinline__ int of(int x) const {
+        const uint32_t t = __umulhi(m, (uint32_t)x);
+        return (int)((t + (((uint32_t)x - t) >> s1)) >> s2);
+    }
+};
 struct Args : ContextAttn, Plan {
     float* ml;         // [slots][B nh L] pairs: maximum and sum, behind the [slots][B nh L][dh] outputs in part
+    int group, in_group, shares;      // heads of a key head, sequences of a prefix, workgroups of a share of the keys (not of the prefix)
+    Div by_group, by_in_group, by_L, by_n, by_heads, by_tiles, by_shares, by_gk, by_nkv, by_prefix_tiles;
 };
 
 template <class T, int DH, int BQ, int BKV, int NTH>
@@ -98,39 +119,40 @@ __global__ __launch_bounds__(NTH, DH * BKV * (int)sizeof(T) <= 16384 ? 2 : 1) vo
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];  // [2][BUF]
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, lh = lane >> 5;
-    auto div = [](int x, int y) { return (int)((uint32_t)x / (uint32_t)y); };      // of numbers that are not negative: half the instructions
-    auto mod = [](int x, int y) { return (int)((uint32_t)x % (uint32_t)y); };
-    const int group = div(a.nh, a.nkv), in_group = div(a.B, a.G);      // heads of a key head, sequences of a prefix
+    // A line of arguments that is not in the scalar cache is a microsecond's way off: one of each is asked for here, together, not
+    // one after the other where they are used.
+    asm volatile("" ::"s"(a.dtype), "s"(a.k), "s"(a.rows), "s"(a.G), "s"(a.window), "s"(a.n), "s"(a.group), "s"(a.by_L.m), "s"(a.by_heads.m), "s"(a.by_gk.m), "s"(a.by_prefix_tiles.m));
+    const int group = a.group, in_group = a.in_group;
     // ---- which queries, which share of which keys
     const bool of_prefix = a.stacked && (int)blockIdx.x < a.prefix_wgs;
     int b = 0, hd, qt, split, nsplit, slot, n, g;
     if (of_prefix) {      // consecutive ids: consecutive (group, head)s, one XCD each; the row tiles of one lie on one XCD
         const int gk = a.G * a.nkv, bid = blockIdx.x;
-        const int rest = div(bid, gk), in = bid - rest * gk;
-        g = div(in, a.nkv); hd = in - g * a.nkv;
-        split = slot = div(rest, a.prefix_tiles);
+        const int rest = a.by_gk.of(bid), in = bid - rest * gk;
+        g = a.by_nkv.of(in); hd = in - g * a.nkv;
+        split = slot = a.by_prefix_tiles.of(rest);
         qt = rest - split * a.prefix_tiles;
         nsplit = a.prefix_split;
         n = in_group * a.n;
     } else {              // all query tiles of a (sequence, head) on one XCD, next to each other; long tiles first
         const int nbh = a.B * a.heads, id = (int)blockIdx.x - (a.stacked ? a.prefix_wgs : 0);
-        split = div(id, a.tiles * nbh);
-        const int bid = id - split * (a.tiles * nbh), by8 = (nbh & 7) == 0, s = by8 ? bid >> 3 : bid, s_bh = div(s, a.tiles);
+        split = a.by_shares.of(id);
+        const int bid = id - split * a.shares, by8 = (nbh & 7) == 0, s = by8 ? bid >> 3 : bid, s_bh = a.by_tiles.of(s);
         qt = a.tiles - 1 - (s - s_bh * a.tiles);
         const int bh = by8 ? s_bh * 8 + (bid & 7) : s_bh;
-        b = div(bh, a.heads);
+        b = a.by_heads.of(bh);
         hd = bh - b * a.heads;
-        g = div(b, in_group);
+        g = a.by_in_group.of(b);
         slot = split + (a.stacked ? a.prefix_split : 0);
         nsplit = a.split;
         n = a.n;
     }
-    const int kvh = a.by_kv ? hd : div(hd, group);
+    const int kvh = a.by_kv ? hd : a.by_group.of(hd);
     const bool scattered = a.pos_tab != nullptr;
     // ---- this lane's query (the last one again past the end; such lanes do not store)
     const int r0 = qt * BQ + wave * 32, r_raw = r0 + l32, r = r_raw < n ? r_raw : n - 1;
-    const int r_seq = of_prefix ? div(r, a.n) : 0, lb = of_prefix ? g * in_group + r_seq : b, in_seq = r - r_seq * a.n;
-    const int r_hd = a.by_kv ? div(in_seq, a.L) : 0, lhd = a.by_kv ? hd * group + r_hd : hd, lj = in_seq - r_hd * a.L;
+    const int r_seq = of_prefix ? a.by_n.of(r) : 0, lb = of_prefix ? g * in_group + r_seq : b, in_seq = r - r_seq * a.n;
+    const int r_hd = a.by_kv ? a.by_L.of(in_seq) : 0, lhd = a.by_kv ? hd * group + r_hd : hd, lj = in_seq - r_hd * a.L;
     const bool wave_live = r0 < n;
     int P = a.P;
     if (a.P_seq && !of_prefix) {
@@ -148,9 +170,9 @@ __global__ __launch_bounds__(NTH, DH * BKV * (int)sizeof(T) <= 16384 ? 2 : 1) vo
     // own rows of the queries: of this wavefront, of the workgroup (bounds)
     auto first_last = [&](int ra, int rb, int& lo, int& hi) {
         rb = rb < n ? rb : n - 1;
-        const bool one = !a.by_kv || div(ra, a.L) == div(rb, a.L);       // within a head the queries are consecutive
-        lo = P + (one ? (a.by_kv ? mod(ra, a.L) : ra) : 0);
-        hi = P + (one ? (a.by_kv ? mod(rb, a.L) : rb) : a.L - 1);
+        const int ha = a.by_kv ? a.by_L.of(ra) : 0, hb = a.by_kv ? a.by_L.of(rb) : 0;      // within a head the queries are consecutive
+        lo = P + (ha == hb ? ra - ha * a.L : 0);
+        hi = P + (ha == hb ? rb - hb * a.L : a.L - 1);
         if (scattered) { lo = a.P0; hi = a.P0 + a.Lblk - 1; }
     };
     int w_min, w_max, p_min, p_max;
@@ -612,6 +634,12 @@ void run_cfg(Args a, hipStream_t st) {
     static int attr_state = 0;
     if (!ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds, &attr_state)) return;
     a.tiles = (a.n + BQ - 1) / BQ;
+    a.group = a.nh / a.nkv;
+    a.in_group = a.B / a.G;
+    a.shares = a.tiles * a.heads * a.B;
+    a.by_group = Div(a.group); a.by_in_group = Div(a.in_group); a.by_L = Div(a.L); a.by_n = Div(a.n); a.by_heads = Div(a.heads);
+    a.by_tiles = Div(a.tiles); a.by_shares = Div(a.shares); a.by_gk = Div(a.G * a.nkv); a.by_nkv = Div(a.nkv);
+    a.by_prefix_tiles = Div(a.stacked ? a.prefix_tiles : 1);
     const int64_t all_rows = (int64_t)a.B * a.nh * a.L;
     const int slots = a.split + (a.stacked ? a.prefix_split : 0);
     a.ml = a.part ? a.part + slots * all_rows * DH : nullptr;
