@@ -65,6 +65,7 @@ constexpr int STACK_ROWS = 64;       // queries per sequence and key head up to 
 
 // How a launch is laid out (host).
 struct Plan {
+    bool few;          // one workgroup per (sequence, key head), wavefronts with tiles of their own
     bool stacked;      // prefix and own workgroups
     bool by_kv;        // the queries of a workgroup are those of all heads of a key head (else of one head)
     int heads;         // heads, or key heads
@@ -100,8 +101,11 @@ struct Args : ContextAttn, Plan {
     Div by_group, by_in_group, by_L, by_n, by_heads, by_tiles, by_shares, by_gk, by_nkv, by_prefix_tiles;
 };
 
-template <class T, int DH, int BQ, int BKV, int NTH>
-__global__ __launch_bounds__(NTH, DH * BKV * (int)sizeof(T) <= 16384 ? 2 : 1) void k_context(const Args a) {
+// FEW (at most 32 queries, few keys): every wavefront has all of the queries and tiles of its own, in a buffer of its own, so that
+// nobody waits for anybody in front of the end, where the wavefronts' results are joined in LDS.  (Otherwise one of four
+// wavefronts works and a second launch joins.)
+template <class T, int DH, int BQ, int BKV, int NTH, bool FEW>
+__global__ __launch_bounds__(NTH, !FEW && DH * BKV * (int)sizeof(T) <= 16384 ? 2 : 1) void k_context(const Args a) {
     typedef typename Chunk<T>::type chunk;
     constexpr bool BF16 = sizeof(T) == 2;
     constexpr int E = 16 / sizeof(T);      // elements of a chunk
@@ -112,13 +116,16 @@ __global__ __launch_bounds__(NTH, DH * BKV * (int)sizeof(T) <= 16384 ? 2 : 1) vo
     constexpr int NW = NTH / 64;
     constexpr int KRB = DH * sizeof(T), VRB = BKV * sizeof(T);            // bytes of a row of the K tile, of the V^T tile
     constexpr int KT = BKV * KRB, BUF = KT + DH * VRB;
-    constexpr int LK = KT / 1024 / NW, LV = DH * VRB / 1024 / NW;         // loads of a wavefront per tile, a KB of whole rows each
+    constexpr int TW = FEW ? 1 : NW;                                      // wavefronts that share a tile
+    constexpr int LK = KT / 1024 / TW, LV = DH * VRB / 1024 / TW;         // loads of a wavefront per tile, a KB of whole rows each
     constexpr int RK = 1024 / KRB, RV = 1024 / VRB;                       // rows of a load
-    static_assert(LK * NW * 1024 == KT && LV * NW * 1024 == DH * VRB, "whole loads per wavefront");
+    static_assert(LK * TW * 1024 == KT && LV * TW * 1024 == DH * VRB, "whole loads per wavefront");
+    static_assert(!FEW || BQ == 32, "the queries of a wavefront");
 
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];  // [2][BUF]
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];  // [2][BUF]; FEW: [NW][BUF]
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, lh = lane >> 5;
+    const int tw = FEW ? 0 : wave;      // among those that share a tile
     // A line of arguments that is not in the scalar cache is a microsecond's way off: one of each is asked for here, together, not
     // one after the other where they are used.
     asm volatile("" ::"s"(a.dtype), "s"(a.k), "s"(a.rows), "s"(a.G), "s"(a.window), "s"(a.n), "s"(a.group), "s"(a.by_L.m), "s"(a.by_heads.m), "s"(a.by_gk.m), "s"(a.by_prefix_tiles.m));
@@ -150,7 +157,7 @@ __global__ __launch_bounds__(NTH, DH * BKV * (int)sizeof(T) <= 16384 ? 2 : 1) vo
     const int kvh = a.by_kv ? hd : a.by_group.of(hd);
     const bool scattered = a.pos_tab != nullptr;
     // ---- this lane's query (the last one again past the end; such lanes do not store)
-    const int r0 = qt * BQ + wave * 32, r_raw = r0 + l32, r = r_raw < n ? r_raw : n - 1;
+    const int r0 = qt * BQ + tw * 32, r_raw = r0 + l32, r = r_raw < n ? r_raw : n - 1;
     const int r_seq = of_prefix ? a.by_n.of(r) : 0, lb = of_prefix ? g * in_group + r_seq : b, in_seq = r - r_seq * a.n;
     const int r_hd = a.by_kv ? a.by_L.of(in_seq) : 0, lhd = a.by_kv ? hd * group + r_hd : hd, lj = in_seq - r_hd * a.L;
     const bool wave_live = r0 < n;
@@ -211,10 +218,9 @@ __global__ __launch_bounds__(NTH, DH * BKV * (int)sizeof(T) <= 16384 ? 2 : 1) vo
     const int64_t all_rows = (int64_t)a.B * a.nh * a.L;
     const bool partial = a.stacked || a.split > 1;
     const int64_t out_row = ((int64_t)lb * a.nh + lhd) * a.L + lj;
-    auto store_out = [&](int i, int g4, f32x4 w) {       // channels i 32 + g4 8 + lh 4 .. + 3 of this lane's query
-        const int c = i * 32 + g4 * 8 + lh * 4;
-        T* const op = reinterpret_cast<T*>(a.out) + (a.frag ? frag_index(lb * a.L + lj, lhd * DH + c, a.nh * DH)      // 4 | c: inside a run of 8
-                                                            : lb * a.out_batch + lhd * a.out_head + lj * a.out_row + c);
+    auto store4 = [&](int b, int h, int j, int c, f32x4 w) {       // channels c .. c + 3, 4 | c, of a query
+        T* const op = reinterpret_cast<T*>(a.out) + (a.frag ? frag_index(b * a.L + j, h * DH + c, a.nh * DH)      // inside a run of 8
+                                                            : b * a.out_batch + h * a.out_head + j * a.out_row + c);
         if constexpr (BF16) {
             bf16x4 t;
 #pragma unroll
@@ -224,8 +230,9 @@ __global__ __launch_bounds__(NTH, DH * BKV * (int)sizeof(T) <= 16384 ? 2 : 1) vo
             *reinterpret_cast<f32x4*>(op) = w;
         }
     };
+    auto store_out = [&](int i, int g4, f32x4 w) { store4(lb, lhd, lj, i * 32 + g4 * 8 + lh * 4, w); };      // of this lane's query
     if (t_begin >= t_end) {    // uniform over the workgroup, before any barrier: nothing to see
-        if (r_raw < n) {
+        if (r_raw < n && (!FEW || wave == 0)) {
             if (partial) {
                 if (lh == 0) *reinterpret_cast<float2*>(a.ml + 2 * (slot * all_rows + out_row)) = make_float2(-__builtin_huge_valf(), 0.f);
             } else {
@@ -247,37 +254,43 @@ __global__ __launch_bounds__(NTH, DH * BKV * (int)sizeof(T) <= 16384 ? 2 : 1) vo
 
     // Tiles go from memory to LDS directly.  16-byte chunk c of row r sits at chunk position c ^ key(r): 16 lanes that read
     // the same chunk of 16 rows touch every bank once.
-    auto key_of = [](int r, int row_bytes) { return row_bytes >= 256 ? r & 15 : (r >> 1) & 7; };
-    const int krow = wave * RK + lane / (64 / RK), vrow = wave * RV + lane / (64 / RV);
-    static_assert(NW * RV % 16 == 0, "the key of a lane's rows of V^T");
+    auto key_of = [](int r, int row_bytes) { return row_bytes >= 256 ? r & 15 : row_bytes == 128 ? (r >> 1) & 7 : (r >> 2) & 3; };
+    const int krow = tw * RK + lane / (64 / RK), vrow = tw * RV + lane / (64 / RV);
+    static_assert(TW * RV % 16 == 0, "the key of a lane's rows of V^T");
     const int vchunk = lane % (64 / RV) ^ key_of(vrow, VRB);
     const unsigned char* const pk = reinterpret_cast<const unsigned char*>(reinterpret_cast<const T*>(a.pk) + g * a.pk_group + kvh * a.pk_head);
-    const unsigned char* const pv = reinterpret_cast<const unsigned char*>(reinterpret_cast<const T*>(a.pv) + g * a.pv_group + kvh * a.pv_head + (int64_t)wave * RV * a.pv_chan);
+    const unsigned char* const pv = reinterpret_cast<const unsigned char*>(reinterpret_cast<const T*>(a.pv) + g * a.pv_group + kvh * a.pv_head + (int64_t)tw * RV * a.pv_chan);
     const unsigned char* const ok = reinterpret_cast<const unsigned char*>(reinterpret_cast<const T*>(a.k) + b * a.k_batch + kvh * a.k_head);
-    const unsigned char* const ov = reinterpret_cast<const unsigned char*>(reinterpret_cast<const T*>(a.v) + b * a.v_batch + kvh * a.v_head + (int64_t)wave * RV * a.v_chan);
+    const unsigned char* const ov = reinterpret_cast<const unsigned char*>(reinterpret_cast<const T*>(a.v) + b * a.v_batch + kvh * a.v_head + (int64_t)tw * RV * a.v_chan);
     auto to_lds = [](const unsigned char* base, uint32_t off, unsigned char* lds) {
         __builtin_amdgcn_global_load_lds((glb_void*)(base + off), (lds_void*)lds, 16, 0, 0);
     };
     auto tile_of = [&](int i) { return i < np ? (i < np1 ? i : tp2 + i - np1) : (i - np < no1 ? i - np : to2 + (i - np) - no1); };
     // A tile that runs past the end of its cache takes the last row and columns again: nothing sees those keys.
-    auto load_kv = [&](int i) {
+    auto buffer = [&](int i) { return smem + (FEW ? wave : i & 1) * BUF; };
+    auto load = [&](int i, bool of_k, bool of_v) {
         const bool pre = i < np;
         const int t = tile_of(i);
-        unsigned char* const lds = smem + (i & 1) * BUF + wave * 1024;
-        const uint32_t k_row = (uint32_t)(pre ? a.pk_row : a.k_row) * sizeof(T);
-        const int64_t v_chan = (pre ? a.pv_chan : a.v_chan) * (int64_t)sizeof(T);
+        unsigned char* const lds = buffer(i) + tw * 1024;
         const int left = (pre ? a.srows : a.rows) - t * BKV;
-        const unsigned char* const kt = (pre ? pk : ok) + (int64_t)t * BKV * k_row;
-        const unsigned char* const vt = (pre ? pv : ov) + (int64_t)t * VRB;
+        if (of_k) {
+            const uint32_t k_row = (uint32_t)(pre ? a.pk_row : a.k_row) * sizeof(T);
+            const unsigned char* const kt = (pre ? pk : ok) + (int64_t)t * BKV * k_row;
 #pragma unroll
-        for (int x = 0; x < LK; ++x) {
-            const int row = krow + x * NW * RK;
-            to_lds(kt, (uint32_t)(row < left ? row : left - 1) * k_row + ((lane % (64 / RK)) ^ key_of(row, KRB)) * 16, lds + x * NW * 1024);
+            for (int x = 0; x < LK; ++x) {
+                const int row = krow + x * TW * RK;
+                to_lds(kt, (uint32_t)(row < left ? row : left - 1) * k_row + ((lane % (64 / RK)) ^ key_of(row, KRB)) * 16, lds + x * TW * 1024);
+            }
         }
-        const uint32_t vo = (uint32_t)(lane / (64 / RV)) * (uint32_t)v_chan + (uint32_t)(vchunk * E < left - E ? vchunk * E : left - E) * (uint32_t)sizeof(T);
+        if (of_v) {
+            const int64_t v_chan = (pre ? a.pv_chan : a.v_chan) * (int64_t)sizeof(T);
+            const unsigned char* const vt = (pre ? pv : ov) + (int64_t)t * VRB;
+            const uint32_t vo = (uint32_t)(lane / (64 / RV)) * (uint32_t)v_chan + (uint32_t)(vchunk * E < left - E ? vchunk * E : left - E) * (uint32_t)sizeof(T);
 #pragma unroll
-        for (int x = 0; x < LV; ++x) to_lds(vt + x * (NW * RV) * v_chan, vo, lds + KT + x * NW * 1024);
+            for (int x = 0; x < LV; ++x) to_lds(vt + x * (TW * RV) * v_chan, vo, lds + KT + x * TW * 1024);
+        }
     };
+    auto load_kv = [&](int i) { load(i, true, true); };
     auto meet = [&]() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
     // Columns of V^T that no query of the workgroup sees may hold anything: their probabilities are 0, and 0 * NaN must not reach
     // the accumulators.  Between the landing of a tile and the barrier that shows it to the others, every lane clears
@@ -286,7 +299,7 @@ __global__ __launch_bounds__(NTH, DH * BKV * (int)sizeof(T) <= 16384 ? 2 : 1) vo
         const bool pre = i < np;
         const int k0 = tile_of(i) * BKV, end = pre ? S : own_end, lo = pre ? pre_lo : own_lo, head = pre ? pre_a : own_a;
         if (k0 + BKV > end || (k0 < lo && k0 + BKV > head)) {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            if (!FEW) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // FEW: the caller has waited
             const int key = k0 + vchunk * E;
             auto seen = [&](int e) { return key + e < end && (key + e < head || key + e >= lo); };
             auto keep = [&](int w) -> uint32_t {
@@ -296,7 +309,7 @@ __global__ __launch_bounds__(NTH, DH * BKV * (int)sizeof(T) <= 16384 ? 2 : 1) vo
             const u32x4 mask = {keep(0), keep(1), keep(2), keep(3)};
 #pragma unroll
             for (int x = 0; x < LV; ++x) {
-                u32x4* const at = reinterpret_cast<u32x4*>(smem + (i & 1) * BUF + KT + (x * NW + wave) * 1024 + lane * 16);
+                u32x4* const at = reinterpret_cast<u32x4*>(buffer(i) + KT + (x * TW + tw) * 1024 + lane * 16);
                 *at = *at & mask;
             }
         }
@@ -321,7 +334,7 @@ __global__ __launch_bounds__(NTH, DH * BKV * (int)sizeof(T) <= 16384 ? 2 : 1) vo
     auto score = [&](int i) {
         const bool pre = i < np;
         const int kv0 = tile_of(i) * BKV;
-        const unsigned char* const kt = smem + (i & 1) * BUF;
+        const unsigned char* const kt = buffer(i);
 #pragma unroll
         for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
@@ -395,7 +408,7 @@ __global__ __launch_bounds__(NTH, DH * BKV * (int)sizeof(T) <= 16384 ? 2 : 1) vo
         m_run = m_new;
     };
     auto output = [&](int i) {
-        const unsigned char* const vt = smem + (i & 1) * BUF + KT;
+        const unsigned char* const vt = buffer(i) + KT;
         float ps = 0.f;
         auto rescale = [&]() {     // only when some query of the wavefront raised its maximum
             if (!__all(alpha == 1.0f)) {
@@ -479,6 +492,67 @@ __global__ __launch_bounds__(NTH, DH * BKV * (int)sizeof(T) <= 16384 ? 2 : 1) vo
         if (!pre && kv0 > w_max) return false;
         return !window || kv0 < a.sinks - (pre ? 0 : S) || kv0 + BKV - 1 > w_min + (pre ? S : 0) - window;
     };
+    if constexpr (FEW) {
+        // K of the next tile goes out once this one's scores are read, V^T once its products are
+        const int i0 = t_begin + wave;
+        if (i0 < t_end) load_kv(i0);
+        for (int i = i0; i < t_end; i += NW) {
+            const int next = i + NW;
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LV) : "memory");       // K has landed (and the queries)
+            score(i);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (next < t_end) {
+                load(next, true, false);
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LK) : "memory");
+            } else {
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            }
+            clear_unseen(i);
+            asm volatile("" ::: "memory");
+            output(i);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (next < t_end) load(next, false, true);
+        }
+        // the join: every wavefront leaves its output, unnormalised, in its buffer, 16-byte chunk c of row r at c ^ (r mod DH / 4)
+        __shared__ float2 stat[NW][32];
+        l_run += __shfl_xor(l_run, 32);
+        static_assert(32 * DH * 4 <= BUF, "an output in a buffer");
+        f32x4* const mine = reinterpret_cast<f32x4*>(buffer(0)) + l32 * (DH / 4);
+#pragma unroll
+        for (int d = 0; d < NDB; ++d)
+#pragma unroll
+            for (int g4 = 0; g4 < 4; ++g4)
+                mine[(d * 8 + g4 * 2 + lh) ^ (l32 & (DH / 4 - 1))] = f32x4{o[d][g4 * 4], o[d][g4 * 4 + 1], o[d][g4 * 4 + 2], o[d][g4 * 4 + 3]};
+        if (lh == 0) stat[wave][l32] = make_float2(m_run, l_run);
+        __syncthreads();
+        const int live = n - qt * 32 < 32 ? n - qt * 32 : 32;
+        for (int x = tid; x < live * (DH / 4); x += NTH) {
+            const int row = x / (DH / 4), c4 = x % (DH / 4);
+            float M = -__builtin_huge_valf();
+#pragma unroll
+            for (int w = 0; w < NW; ++w) M = fmaxf(M, stat[w][row].x);
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+            float den = 0.f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const float2 st = stat[w][row];
+                const float f = st.x == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(st.x - M);
+                sum += f * reinterpret_cast<const f32x4*>(smem + w * BUF)[row * (DH / 4) + (c4 ^ (row & (DH / 4 - 1)))];
+                den += f * st.y;
+            }
+            const int rr = qt * 32 + row, q_seq = of_prefix ? a.by_n.of(rr) : 0, q_b = of_prefix ? g * in_group + q_seq : b, q_in = rr - q_seq * a.n;
+            const int q_hd = a.by_kv ? a.by_L.of(q_in) : 0, q_h = a.by_kv ? hd * group + q_hd : hd, q_j = q_in - q_hd * a.L;
+            if (partial) {
+                const int64_t at = slot * all_rows + ((int64_t)q_b * a.nh + q_h) * a.L + q_j;
+                *reinterpret_cast<f32x4*>(a.part + at * DH + c4 * 4) = sum;
+                if (c4 == 0) *reinterpret_cast<float2*>(a.ml + 2 * at) = make_float2(M, den);
+            } else {
+                const float inv = den > 0.f ? 1.0f / den : 0.f;
+                store4(q_b, q_h, q_j, c4 * 4, sum * inv);
+            }
+        }
+        return;
+    }
     load_kv(t_begin);
     clear_unseen(t_begin);
 #pragma unroll
@@ -611,6 +685,15 @@ Plan make_plan(const ContextAttn& a, int esz, int64_t part_floats) {
     const int TARGET = 512;           // workgroups: two per CU
     const int64_t base = (int64_t)a.B * p.heads * p.tiles;
     const int n_own = own_tiles(a, bkv), n_pre = prefix_tiles(a, bkv);
+    // One launch instead of two, as long as every (sequence, key head) has a CU and streams its keys there about as fast as more
+    // CUs would and the join adds.  Tokens of 32 heads of 128, us, two launches / one: 1 sequence of 60, 250, 500, 1000 rows 6.0 / 5.8,
+    // 9.1 / 7.5, 10.2 / 9.8, 11.7 / 13.8; 4 of 250, 500, 1000 11.2 / 8.5, 14.4 / 12.2, 21.1 / 23.9; 8 (256 workgroups) of 500, 1000,
+    // 2000 21.5 / 17.8, 32.1 / 28.7, 55.2 / 55.5; 16 of 60, 250 8.5 / 11.5, 17.5 / 20.6.  8 behind a prefix of 250, 1000, 60 own
+    // rows 10.6 / 8.7, 13.5 / 14.4.  (float32 is bound by its matrix instruction: 8 x 4 behind 300 20.8 / 31.9.)
+    if (esz == 2 && p.by_kv && p.n <= 32 && !a.pos_tab && base <= cu_count() && n_pre <= 8 && n_own <= (4 * base >= 3 * cu_count() ? 24 : 8)) {
+        p.few = true;
+        return p;
+    }
     p.stacked = p.by_kv && n_pre > 0 && a.B > a.G && p.n <= STACK_ROWS && !(a.P_seq && a.window) && slots >= 2;
     if (p.stacked) {
         p.prefix_tiles = (int)(((int64_t)(a.B / a.G) * p.n + 127) / 128);
@@ -627,10 +710,10 @@ Plan make_plan(const ContextAttn& a, int esz, int64_t part_floats) {
     return p;
 }
 
-template <class T, int DH, int BQ, int BKV, int NTH>
+template <class T, int DH, int BQ, int BKV, int NTH, bool FEW = false>
 void run_cfg(Args a, hipStream_t st) {
-    auto kern = k_context<T, DH, BQ, BKV, NTH>;
-    const int lds = 2 * 2 * BKV * DH * (int)sizeof(T);
+    auto kern = k_context<T, DH, BQ, BKV, NTH, FEW>;
+    const int lds = (FEW ? NTH / 64 : 2) * 2 * BKV * DH * (int)sizeof(T);
     static int attr_state = 0;
     if (!ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds, &attr_state)) return;
     a.tiles = (a.n + BQ - 1) / BQ;
@@ -654,6 +737,7 @@ void run(const ContextAttn& c, hipStream_t st) {
     static_cast<Plan&>(a) = make_plan(c, sizeof(T), c.part ? c.part_floats : 0);
     constexpr int SMALL = small_tile(sizeof(T), DH);
     if constexpr (sizeof(T) == 2) {
+        if (a.few) return run_cfg<T, DH, 32, 32, 512, true>(a, st);
         // long blocks: tiles of 128 keys, and 256 queries where 128 would not find a CU each (heads of 128), as in attention.hip
         if (c.L > 128 && !c.pos_tab) {
             if (DH == 128 && (int64_t)c.B * c.nh * ((c.L + 127) / 128) > cu_count()) return run_cfg<T, DH, DH == 128 ? 256 : 128, 128, DH == 128 ? 512 : 256>(a, st);
