@@ -288,9 +288,13 @@ def _strided(t, dtype, name, dims):
     return t.data_ptr(), [t.stride(i) if t.shape[i] > 1 else 0 for i in range(dims - 1)]
 
 
-def _on_device(device, stream):
-    """The device of a call without a context, and its stream: a raw hipStream_t, or torch's current stream of that device."""
-    return torch.cuda.device(device), C.c_void_p(torch.cuda.current_stream(device).cuda_stream if stream is None else stream)
+def _on_device(device, stream, call):
+    """Runs a call without a context on its tensors' device; stream: a raw hipStream_t, or torch's current stream of that device."""
+    st = torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream
+    if torch._C._cuda_getDevice() == device.index:
+        return call(st)
+    with torch.cuda.device(device):
+        return call(st)
 
 
 class Attention:
@@ -347,9 +351,8 @@ def mulo_attention(attention, workspace=None, stream=None):
     ptr, n = (None, 0) if workspace is None else (_ptr(workspace), workspace.numel() * workspace.element_size())
     if workspace is not None and workspace.device != attention.device:
         raise ValueError("the workspace lies on another device")
-    dev, st = _on_device(attention.device, stream)
-    with dev:
-        _check(load_library().mulo_attention(st, attention.ref, ptr, n), "mulo_attention")
+    lib = load_library()
+    _check(_on_device(attention.device, stream, lambda st: lib.mulo_attention(st, attention.ref, ptr, n)), "mulo_attention")
 
 
 def mulo_attach_prefix(ctx, kv=None, length=0, rope_cos=None, rope_sin=None, n_prefix=None):
@@ -390,16 +393,21 @@ def mulo_sample_filtered(params, logits, u=None, tokens=None, probs=None, logits
     rows = n // 2 if params.cfg_scale > 0 else n
     if params.cfg_scale > 0 and n % 2:
         raise ValueError("guidance takes a conditional and an unconditional row each")
-    for t, shape in ((u, (rows,)), (tokens, (rows,)), (probs, (rows, V)), (logits_out, (rows, V))):
-        if t is not None and (tuple(t.shape) != shape or t.device != logits.device):
-            raise ValueError("expected %s on the logits' device" % (shape,))
-    f32 = torch.float32
-    dev, st = _on_device(logits.device, stream)
-    with dev:
-        _check(load_library().mulo_sample_filtered(
-            st, C.byref(params), rows, V, MULO_BF16 if logits.dtype == torch.bfloat16 else MULO_F32, ptr, stride if n > 1 else V,
-            _ptr(u, f32, True), _ptr(tokens, torch.int32, True), _ptr(probs, f32, True), _ptr(logits_out, f32, True)),
-            "mulo_sample_filtered")
+    f32, i32 = torch.float32, torch.int32
+    device, lib = logits.device, load_library()
+
+    def ptr_of(t, dtype, *shape):
+        if t is None:
+            return None
+        if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+            raise ValueError("expected %s, contiguous, %s on the logits' device" % (shape, dtype))
+        return t.data_ptr()
+
+    u, tokens = ptr_of(u, f32, rows), ptr_of(tokens, i32, rows)
+    probs, out = ptr_of(probs, f32, rows, V), ptr_of(logits_out, f32, rows, V)
+    _check(_on_device(device, stream, lambda st: lib.mulo_sample_filtered(
+        st, C.byref(params), rows, V, MULO_BF16 if logits.dtype == torch.bfloat16 else MULO_F32, ptr, stride if n > 1 else V,
+        u, tokens, probs, out)), "mulo_sample_filtered")
 
 
 PROF_CLASSES = ["gemm_qkv", "gemm_out", "gemm_gate_up", "gemm_down", "gemm_lm_head", "attention", "norm_embed",

@@ -143,30 +143,60 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
     const size_t esz = bf16 ? 2 : 4;
     const char* const zc = (const char*)a.logits + r * a.row_stride * esz;
     const char* const zu = a.logits_u ? (const char*)a.logits_u + r * a.row_stride * esz : nullptr;
-    // rows whose start and length allow it are read in whole vectors; runs that lie in the row as a whole, without a test of an entry
-    const bool vectors = (((uintptr_t)zc | (uintptr_t)zu) & (esz * 4 - 1)) == 0;
-    auto wide = [](uint2 t) {
-        return make_float4(__uint_as_float(t.x << 16), __uint_as_float(t.x & 0xFFFF0000u), __uint_as_float(t.y << 16), __uint_as_float(t.y & 0xFFFF0000u));
+    // Four entries an access, wherever the row begins (global memory takes vectors at any alignment of their elements).  Four
+    // runs that lie in the row as a whole take one address; else an access that would pass the end moves back to it, and what it
+    // then holds too early is shifted out.
+    struct __attribute__((packed)) Four { float v[4]; };
+    struct __attribute__((packed)) FourShort { uint16_t v[4]; };
+    auto wide = [](const FourShort t) {
+        auto one = [&](int e) { return __uint_as_float((uint32_t)t.v[e] << 16); };
+        return make_float4(one(0), one(1), one(2), one(3));
     };
     auto four_runs = [&](const char* row, int i, float4 v[4]) {      // entries i .. i + 3 and 256, 512 and 768 further on
-        if (vectors && i - lane * 4 + 1024 <= V) {
+        if (i - lane * 4 + 1024 <= V) {
             if (bf16) {
-                uint2 t[4];
+                FourShort t[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) t[j] = reinterpret_cast<const uint2*>(row + (size_t)i * 2)[j * 64];
+                for (int j = 0; j < 4; ++j) t[j] = reinterpret_cast<const FourShort*>(row + (size_t)i * 2)[j * 64];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[j] = wide(t[j]);
             } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = reinterpret_cast<const float4*>(row + (size_t)i * 4)[j * 64];
+                for (int j = 0; j < 4; ++j) {
+                    const Four t = reinterpret_cast<const Four*>(row + (size_t)i * 4)[j * 64];
+                    v[j] = make_float4(t.v[0], t.v[1], t.v[2], t.v[3]);
+                }
+            }
+        } else if (V >= 4) {
+            int at[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) at[j] = i + j * 256 < V - 4 ? i + j * 256 : V - 4;
+            if (bf16) {
+                FourShort t[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) t[j] = *reinterpret_cast<const FourShort*>(row + (size_t)at[j] * 2);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = wide(t[j]);
+            } else {
+                Four t[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) t[j] = *reinterpret_cast<const Four*>(row + (size_t)at[j] * 4);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = make_float4(t[j].v[0], t[j].v[1], t[j].v[2], t[j].v[3]);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int past = i + j * 256 - at[j];      // four and more: all of them lie behind the end
+                if (past & 1) { v[j].x = v[j].y; v[j].y = v[j].z; v[j].z = v[j].w; }
+                if (past & 2) { v[j].x = v[j].z; v[j].y = v[j].w; }
             }
         } else {
-            auto one = [&](int k) {      // entries past the end re-read the row's first
+            auto one = [&](int k) {
                 k = k < V ? k : 0;
                 return bf16 ? __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(row)[k] << 16) : reinterpret_cast<const float*>(row)[k];
             };
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = make_float4(one(i + j * 256), one(i + j * 256 + 1), one(i + j * 256 + 2), one(i + j * 256 + 3));
+            for (int j = 0; j < 4; ++j) v[j] = make_float4(one(0), one(1), one(2), one(3));
         }
     };
     // f(index of the first, four entries, number of the run), four runs requested together; guided; NaN, and what lies past the
@@ -203,15 +233,13 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
             from_memory([&](int i, const float4 z, int) { f(i, z); });
         }
     };
-    const bool out_vectors = (((uintptr_t)a.probs | (uintptr_t)a.kept) & 15) == 0 && (V & 3) == 0;
     auto put = [&](float* row, int i, const float4 v) {
-        if (out_vectors) {
-            if (i < V) *reinterpret_cast<float4*>(row + i) = v;
+        if (i + 4 <= V) {
+            *reinterpret_cast<Four*>(row + i) = Four{{v.x, v.y, v.z, v.w}};
         } else {
             if (i < V) row[i] = v.x;
             if (i + 1 < V) row[i + 1] = v.y;
             if (i + 2 < V) row[i + 2] = v.z;
-            if (i + 3 < V) row[i + 3] = v.w;
         }
     };
     for (int i = tid; i < BINS; i += NT) hist[i] = 0;
