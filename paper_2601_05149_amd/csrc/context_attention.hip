@@ -707,6 +707,18 @@ Plan make_plan(const ContextAttn& a, int esz, int64_t part_floats) {
     }
     const int n = n_own + n_pre;
     if (slots >= 2 && a.L <= 128) p.split = clamp_int(TARGET / base, 1, slots < n ? slots : n);
+    // Long blocks that do not find a CU each: shares of at least 4 tiles (float32, whose matrix instruction takes 16 times as long: 2) of
+    // what a query sees on average, bf16 from 12 of them on.  1 x 300 queries, 1000 rows in front, us, whole / in shares: bf16
+    // 32 heads of 128 37 / 27, 16 of 64 24 / 16, float32 8 of 64 101 / 25; 1 x 1024, nothing in front (8 tiles): 16 of 64 19 / 22;
+    // 2 x 600 through a window of 545 (10) 20 / 23, float32 8 of 64 64 / 34.
+    if (slots >= 2 && a.L > 128 && base < cu_count()) {
+        ContextAttn half = a;
+        half.L = a.L / 2;
+        int seen = n_pre + own_tiles(half, bkv);
+        if (a.window && ((int64_t)a.window + a.sinks) / bkv + 1 < seen) seen = (a.window + a.sinks) / bkv + 1;
+        const int most = seen / (esz == 2 ? 4 : 2);
+        if (esz == 4 || seen >= 12) p.split = clamp_int(TARGET / base, 1, most < 1 ? 1 : most < slots ? most : slots);
+    }
     return p;
 }
 
@@ -738,8 +750,8 @@ void run(const ContextAttn& c, hipStream_t st) {
     constexpr int SMALL = small_tile(sizeof(T), DH);
     if constexpr (sizeof(T) == 2) {
         if (a.few) return run_cfg<T, DH, 32, 32, 512, true>(a, st);
-        // long blocks: tiles of 128 keys, and 256 queries where 128 would not find a CU each (heads of 128), as in attention.hip
-        if (c.L > 128 && !c.pos_tab) {
+        // long blocks that go over their keys as a whole: tiles of 128 keys, and 256 queries where 128 would not find a CU each (heads of 128), as in attention.hip
+        if (c.L > 128 && !c.pos_tab && a.split == 1) {
             if (DH == 128 && (int64_t)c.B * c.nh * ((c.L + 127) / 128) > cu_count()) return run_cfg<T, DH, DH == 128 ? 256 : 128, 128, DH == 128 ? 512 : 256>(a, st);
             return run_cfg<T, DH, 128, 128, 256>(a, st);
         }

@@ -89,6 +89,11 @@ CASES = [
     ("f32", 2, 150, 4, 2, 128, 9, dict(S=33)),
     ("f32", 1, 260, 2, 2, 64, 0, {}),
     ("bf16", 1, 257, 2, 2, 64, 0, {}),
+    # blocks whose keys are dealt to several workgroups
+    ("bf16", 1, 150, 4, 2, 128, 900, dict(S=100)),
+    ("f32", 1, 140, 2, 2, 128, 300, {}),
+    ("bf16", 2, 135, 2, 2, 64, 1000, dict(window=900, sinks=30, starts=[1000, -1])),
+    ("f32", 2, 133, 2, 1, 64, 200, dict(S=70, starts=[50, 200])),
     # windows: one key, shorter than a tile, longer than everything, across the border of prefix and own rows, sinks in both
     ("bf16", 2, 1, 2, 2, 128, 200, dict(window=1)),
     ("f32", 2, 7, 2, 2, 64, 200, dict(window=1, sinks=1)),
