@@ -647,8 +647,10 @@ void join(const Args& a, int slots, hipStream_t st) {
     else hipLaunchKernelGGL((k_context_join<T, DH, 16>), grid, block, 0, st, a, slots);
 }
 
-// Keys per tile where queries are few (64 KB of LDS, two workgroups per CU).
-constexpr int small_tile(int esz, int dh) { return esz == 2 ? 64 : 4096 / dh; }
+// Keys per tile where queries are few: at most 64 KB of LDS, two workgroups per CU.  float32 is bound by its matrix instruction (2 us a
+// tile of 32 keys and wavefront): smaller tiles deal its keys to more workgroups (heads of 64, 64 / 32 keys, us: 1 x 150 queries,
+// 500 rows 22.5 / 17.9, 16 tokens of 8 heads, 1000 shared and 1000 own rows 50 / 34, 2 x 8 16.5 / 13; 4 tokens of 16 heads, 2000 rows 47 / 51).
+constexpr int small_tile(int esz) { return esz == 2 ? 64 : 32; }
 
 // Key tiles that the queries see at most (host; P rows in front of the block)
 int own_tiles(const ContextAttn& a, int bkv) {
@@ -674,7 +676,7 @@ int clamp_int(int64_t v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : (i
 // part_floats: the scratch there is (context_attention_floats asks with as much as can be wanted)
 Plan make_plan(const ContextAttn& a, int esz, int64_t part_floats) {
     Plan p{};
-    const int group = a.nh / a.nkv, bkv = small_tile(esz, a.dh);
+    const int group = a.nh / a.nkv, bkv = small_tile(esz);
     const int64_t slot_floats = (int64_t)a.B * a.nh * a.L * (a.dh + 2);
     const int slots = clamp_int(part_floats / slot_floats, 0, MAX_SLOTS);
     p.by_kv = (int64_t)group * a.L <= 128;
@@ -715,7 +717,7 @@ Plan make_plan(const ContextAttn& a, int esz, int64_t part_floats) {
         ContextAttn half = a;
         half.L = a.L / 2;
         int seen = n_pre + own_tiles(half, bkv);
-        if (a.window && ((int64_t)a.window + a.sinks) / bkv + 1 < seen) seen = (a.window + a.sinks) / bkv + 1;
+        if (a.window) seen = clamp_int(((int64_t)a.window + a.sinks + 128) / bkv + 1, 1, seen);      // of a workgroup's 128
         const int most = seen / (esz == 2 ? 4 : 2);
         if (esz == 4 || seen >= 12) p.split = clamp_int(TARGET / base, 1, most < 1 ? 1 : most < slots ? most : slots);
     }
@@ -747,7 +749,7 @@ void run(const ContextAttn& c, hipStream_t st) {
     Args a{};
     static_cast<ContextAttn&>(a) = c;
     static_cast<Plan&>(a) = make_plan(c, sizeof(T), c.part ? c.part_floats : 0);
-    constexpr int SMALL = small_tile(sizeof(T), DH);
+    constexpr int SMALL = small_tile(sizeof(T));
     if constexpr (sizeof(T) == 2) {
         if (a.few) return run_cfg<T, DH, 32, 32, 512, true>(a, st);
         // long blocks that go over their keys as a whole: tiles of 128 keys, and 256 queries where 128 would not find a CU each (heads of 128), as in attention.hip

@@ -236,6 +236,7 @@ struct SampleArgs {
     float cfg_scale;
     int rows, V;
     double temperature, top_p, min_p;
+    double min_p_below;   // temperature ln(min_p), the launcher's: how far below the maximum an entry has min_p of its weight
     int top_k;
     const float* u;
     int32_t* tokens;

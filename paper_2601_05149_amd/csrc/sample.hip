@@ -527,7 +527,7 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
     }
     // min-p: the least value with enough weight.  It is within a few steps of float32 of where its logarithm says: a lane looks at each.
     if (!greedy && a.min_p > 0.0 && !none) {
-        const int64_t most = key_of(hi), least = key_of(-MOST), guess = key_of((float)fmax((double)hi + log(a.min_p) * a.temperature, -(double)MOST));
+        const int64_t most = key_of(hi), least = key_of(-MOST), guess = key_of((float)fmax((double)hi + a.min_p_below, -(double)MOST));
         const int64_t at = guess - 32 + lane, k = at < least ? least : at < most ? at : most;
         const float z = of_key((uint32_t)k);
         const u64 enough = __ballot(k == most || w.value(z) >= a.min_p);      // of the last lane on, at the least
@@ -619,7 +619,9 @@ void run(const SampleArgs& a, hipStream_t st) {
 
 }  // namespace
 
-void launch_sample_filtered(const SampleArgs& a, hipStream_t st) {
+void launch_sample_filtered(const SampleArgs& args, hipStream_t st) {
+    SampleArgs a = args;
+    a.min_p_below = a.min_p > 0.0 ? a.temperature * log(a.min_p) : 0.0;
     if (a.V <= 2048) run<256, true, 2>(a, st);
     else if (a.V <= LDS_ENTRIES) {
         if (a.rows > cu_count()) run<512, true, 1>(a, st);
