@@ -337,7 +337,7 @@ MULO_API mulo_status mulo_resample_islands(mulo_ctx *ctx, mulo_kv *kv, int32_t B
  *   prefix_k, prefix_v  the prefixes, laid out as k and v with a group in the place of a sequence; prefix_rows rows allocated,
  *                prefix_len in use.  prefix_len == 0: no prefix (the pointers are not read)
  *   sinks, window   window == 0: every earlier key is seen, and sinks is not read
- *   scale        0: 1 / sqrt(head_dim)
+ *   scale        0: 1 / sqrt(head_dim); at most 1e6
  * Rows that no query of the call sees may hold anything, NaN included; what some query sees has to be finite.  q and out must
  * not overlap.
  * Limits: head_dim 64 or 128; n_heads a multiple of n_kv_heads, B of n_prefix; rows, prefix_rows and every stride a multiple
@@ -370,7 +370,8 @@ MULO_API uint64_t mulo_attention_workspace_bytes(const mulo_attention_args *a);
 /* Runs on the current HIP device and allocates nothing.  workspace: device memory, 16-byte aligned, used until the call's
  * stream work has finished (calls that may overlap need one each, and so do graphs that may replay at the same time), or
  * NULL; with fewer bytes than mulo_attention_workspace_bytes says the keys are dealt to fewer workgroups.  The
- * number of shares follows from the sizes alone, so equal calls give equal bits.
+ * number of shares follows from the sizes alone, so equal calls give equal bits.  (A recorded call needs an ordinary one of the
+ * same sizes before it, as the compute entry points of a context do.)
  * Errors: as mulo_check_attention; a workspace that is not 16-byte aligned -> MULO_ERR_UNSUPPORTED. */
 MULO_API mulo_status mulo_attention(void *hip_stream, const mulo_attention_args *a, void *workspace, uint64_t workspace_bytes);
 
@@ -427,7 +428,7 @@ typedef struct {
  *               what mulo_upsample_draft and the accept test take as a draft's
  *   logits_out  device float32 [rows, vocab] (out) or NULL: z / temperature where the entry stays (z with temperature 0;
  *               kept within float32's finite range), -inf elsewhere: what the accept test takes as the target's.  May be `logits` itself for float32 rows
- *               that lie next to each other
+ *               that lie next to each other; no other output may overlap an input or an output
  * Errors: no output -> MULO_ERR_NULL; vocab > 262144 -> MULO_ERR_UNSUPPORTED; row_stride < vocab -> MULO_ERR_SHAPE. */
 MULO_API mulo_status mulo_sample_filtered(void *hip_stream, const mulo_sample_params *p, int32_t rows, int32_t vocab,
                                  int32_t dtype, const void *logits, int64_t row_stride, const float *u,

@@ -327,6 +327,8 @@ def make_attention(q, out, k, v, P, P_seq=None, prefix_k=None, prefix_v=None, pr
             raise ValueError("P_seq has one entry per sequence")
         a.P_seq = _ptr(P_seq, torch.int32)
         tensors.append(P_seq)
+    if prefix_len and (prefix_k is None or prefix_v is None):
+        raise ValueError("a prefix of %d rows without its keys or values" % prefix_len)
     if prefix_len:
         G, prows = prefix_k.shape[0], prefix_k.shape[2]
         if prefix_k.shape != (G, nkv, prows, dh) or prefix_v.shape != (G, nkv, dh, prows):

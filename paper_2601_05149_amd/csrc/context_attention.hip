@@ -131,7 +131,7 @@ __global__ __launch_bounds__(NTH, !FEW && DH * BKV * (int)sizeof(T) <= 16384 ? 2
     asm volatile("" ::"s"(a.dtype), "s"(a.k), "s"(a.rows), "s"(a.G), "s"(a.window), "s"(a.n), "s"(a.group), "s"(a.by_L.m), "s"(a.by_heads.m), "s"(a.by_gk.m), "s"(a.by_prefix_tiles.m));
     const int group = a.group, in_group = a.in_group;
     // ---- which queries, which share of which keys
-    const bool of_prefix = a.stacked && (int)blockIdx.x < a.prefix_wgs;
+    const bool stacked = !FEW && a.stacked, of_prefix = stacked && (int)blockIdx.x < a.prefix_wgs;
     int b = 0, hd, qt, split, nsplit, slot, n, g;
     if (of_prefix) {      // consecutive ids: consecutive (group, head)s, one XCD each; the row tiles of one lie on one XCD
         const int gk = a.G * a.nkv, bid = blockIdx.x;
@@ -142,20 +142,20 @@ __global__ __launch_bounds__(NTH, !FEW && DH * BKV * (int)sizeof(T) <= 16384 ? 2
         nsplit = a.prefix_split;
         n = in_group * a.n;
     } else {              // all query tiles of a (sequence, head) on one XCD, next to each other; long tiles first
-        const int nbh = a.B * a.heads, id = (int)blockIdx.x - (a.stacked ? a.prefix_wgs : 0);
-        split = a.by_shares.of(id);
+        const int nbh = a.B * a.heads, id = (int)blockIdx.x - (stacked ? a.prefix_wgs : 0);
+        split = FEW ? 0 : a.by_shares.of(id);
         const int bid = id - split * a.shares, by8 = (nbh & 7) == 0, s = by8 ? bid >> 3 : bid, s_bh = a.by_tiles.of(s);
         qt = a.tiles - 1 - (s - s_bh * a.tiles);
         const int bh = by8 ? s_bh * 8 + (bid & 7) : s_bh;
         b = a.by_heads.of(bh);
         hd = bh - b * a.heads;
         g = a.by_in_group.of(b);
-        slot = split + (a.stacked ? a.prefix_split : 0);
-        nsplit = a.split;
+        slot = split + (stacked ? a.prefix_split : 0);
+        nsplit = FEW ? 1 : a.split;
         n = a.n;
     }
     const int kvh = a.by_kv ? hd : a.by_group.of(hd);
-    const bool scattered = a.pos_tab != nullptr;
+    const bool scattered = !FEW && a.pos_tab != nullptr;
     // ---- this lane's query (the last one again past the end; such lanes do not store)
     const int r0 = qt * BQ + tw * 32, r_raw = r0 + l32, r = r_raw < n ? r_raw : n - 1;
     const int r_seq = of_prefix ? a.by_n.of(r) : 0, lb = of_prefix ? g * in_group + r_seq : b, in_seq = r - r_seq * a.n;
@@ -190,7 +190,7 @@ __global__ __launch_bounds__(NTH, !FEW && DH * BKV * (int)sizeof(T) <= 16384 ? 2
     const int S = a.S, window = a.window;
     int pre_a = 0, pre_lo = 0, own_a = 0, own_lo = 0, np1 = 0, np = 0, tp2 = 0, no1 = 0, no = 0, to2 = 0;
     const int own_end = p_max + 1;
-    if (S > 0 && (of_prefix || !a.stacked)) {
+    if (S > 0 && (of_prefix || !stacked)) {
         if (window) {
             const int lo = S + p_min - window + 1;       // S + p_min < 2^25
             pre_lo = lo < 0 ? 0 : lo < S ? lo : S;
@@ -216,7 +216,7 @@ __global__ __launch_bounds__(NTH, !FEW && DH * BKV * (int)sizeof(T) <= 16384 ? 2
     const int per = (n_tiles + nsplit - 1) / nsplit;
     const int t_begin = split * per, t_end = t_begin + per < n_tiles ? t_begin + per : n_tiles;
     const int64_t all_rows = (int64_t)a.B * a.nh * a.L;
-    const bool partial = a.stacked || a.split > 1;
+    const bool partial = !FEW && (stacked || a.split > 1);
     const int64_t out_row = ((int64_t)lb * a.nh + lhd) * a.L + lj;
     auto store4 = [&](int b, int h, int j, int c, f32x4 w) {       // channels c .. c + 3, 4 | c, of a query
         T* const op = reinterpret_cast<T*>(a.out) + (a.frag ? frag_index(b * a.L + j, h * DH + c, a.nh * DH)      // inside a run of 8
@@ -525,8 +525,7 @@ __global__ __launch_bounds__(NTH, !FEW && DH * BKV * (int)sizeof(T) <= 16384 ? 2
                 mine[(d * 8 + g4 * 2 + lh) ^ (l32 & (DH / 4 - 1))] = f32x4{o[d][g4 * 4], o[d][g4 * 4 + 1], o[d][g4 * 4 + 2], o[d][g4 * 4 + 3]};
         if (lh == 0) stat[wave][l32] = make_float2(m_run, l_run);
         __syncthreads();
-        const int live = n - qt * 32 < 32 ? n - qt * 32 : 32;
-        for (int x = tid; x < live * (DH / 4); x += NTH) {
+        for (int x = tid; x < n * (DH / 4); x += NTH) {
             const int row = x / (DH / 4), c4 = x % (DH / 4);
             float M = -__builtin_huge_valf();
 #pragma unroll
@@ -540,16 +539,8 @@ __global__ __launch_bounds__(NTH, !FEW && DH * BKV * (int)sizeof(T) <= 16384 ? 2
                 sum += f * reinterpret_cast<const f32x4*>(smem + w * BUF)[row * (DH / 4) + (c4 ^ (row & (DH / 4 - 1)))];
                 den += f * st.y;
             }
-            const int rr = qt * 32 + row, q_seq = of_prefix ? a.by_n.of(rr) : 0, q_b = of_prefix ? g * in_group + q_seq : b, q_in = rr - q_seq * a.n;
-            const int q_hd = a.by_kv ? a.by_L.of(q_in) : 0, q_h = a.by_kv ? hd * group + q_hd : hd, q_j = q_in - q_hd * a.L;
-            if (partial) {
-                const int64_t at = slot * all_rows + ((int64_t)q_b * a.nh + q_h) * a.L + q_j;
-                *reinterpret_cast<f32x4*>(a.part + at * DH + c4 * 4) = sum;
-                if (c4 == 0) *reinterpret_cast<float2*>(a.ml + 2 * at) = make_float2(M, den);
-            } else {
-                const float inv = den > 0.f ? 1.0f / den : 0.f;
-                store4(q_b, q_h, q_j, c4 * 4, sum * inv);
-            }
+            const int in_head = a.by_L.of(row);      // one tile of queries, of the heads of a key head
+            store4(b, hd * group + in_head, row - in_head * a.L, c4 * 4, sum * (den > 0.f ? 1.0f / den : 0.f));
         }
         return;
     }
@@ -728,8 +719,8 @@ template <class T, int DH, int BQ, int BKV, int NTH, bool FEW = false>
 void run_cfg(Args a, hipStream_t st) {
     auto kern = k_context<T, DH, BQ, BKV, NTH, FEW>;
     const int lds = (FEW ? NTH / 64 : 2) * 2 * BKV * DH * (int)sizeof(T);
-    static int attr_state = 0;
-    if (!ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds, &attr_state)) return;
+    static int attr_state[MAX_DEVICES] = {};
+    if (!ensure_dynamic_lds_here(reinterpret_cast<const void*>(kern), lds, attr_state)) return;
     a.tiles = (a.n + BQ - 1) / BQ;
     a.group = a.nh / a.nkv;
     a.in_group = a.B / a.G;

@@ -26,6 +26,15 @@ hipError_t g_config_error = hipSuccess;   // first failed configuration call sin
 void note_hip_error(hipError_t e) {
     if (e != hipSuccess && g_config_error == hipSuccess) g_config_error = e;
 }
+bool ensure_dynamic_lds_here(const void* kern, int bytes, int* per_device) {
+    int dev = -1;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= MAX_DEVICES) {
+        (void)hipGetLastError();
+        note_hip_error(hipErrorInvalidDevice);
+        return false;
+    }
+    return ensure_dynamic_lds(kern, bytes, per_device + dev);
+}
 bool ensure_dynamic_lds(const void* kern, int bytes, int* state) {
     if (*state == 0) {
         const hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
@@ -154,7 +163,6 @@ mulo_status check_launch() {
 }
 
 // Device address of `scratch` on the current device, looked up once per device (with that device current).
-constexpr int MAX_DEVICES = 64;
 float* static_scratch() {
     static float* per_device[MAX_DEVICES] = {};
     int dev = -1;
@@ -548,7 +556,7 @@ mulo_status mulo_check_attention(const mulo_attention_args* a) {
     if (!a || !a->q || !a->out || !a->k || !a->v) return MULO_ERR_NULL;
     if (a->dtype != MULO_F32 && a->dtype != MULO_BF16) return MULO_ERR_RANGE;
     if (a->B < 1 || a->L < 1 || a->n_heads < 1 || a->n_kv_heads < 1 || a->head_dim < 1 || a->rows < 1 || a->P < 0 ||
-        a->prefix_len < 0 || a->sinks < 0 || a->window < 0 || !(a->scale >= 0.f && a->scale <= 3.0e38f))
+        a->prefix_len < 0 || a->sinks < 0 || a->window < 0 || !(a->scale >= 0.f && a->scale <= 1.0e6f))
         return MULO_ERR_RANGE;
     const bool prefix = a->prefix_len > 0;
     if (prefix && (!a->prefix_k || !a->prefix_v)) return MULO_ERR_NULL;
@@ -643,6 +651,7 @@ mulo_status mulo_sample_filtered(void* hip_stream, const mulo_sample_params* p, 
     const size_t e = dtype == MULO_BF16 ? 2 : 4;
     if (((uintptr_t)logits & (e - 1)) || ((uintptr_t)probs & 3) || ((uintptr_t)logits_out & 3)) return MULO_ERR_UNSUPPORTED;
     if (logits_out == logits && (dtype != MULO_F32 || row_stride != vocab)) return MULO_ERR_SHAPE;
+    if (probs && (probs == logits || probs == logits_out)) return MULO_ERR_SHAPE;
     SampleArgs a{};
     a.logits = logits;
     a.logits_u = p->cfg_scale > 0.f ? (const char*)logits + (size_t)rows * row_stride * e : nullptr;

@@ -13,6 +13,9 @@ void note_hip_error(hipError_t e);
 // Raises the dynamic-LDS limit of `kern` to `bytes` once per process (state: 0 = not tried, 1 = done, -1 = failed);
 // false, with the error noted, when the runtime refuses.
 bool ensure_dynamic_lds(const void* kern, int bytes, int* state);
+// The same for entry points without a context, which run on whatever device is current: per_device holds MAX_DEVICES states.
+constexpr int MAX_DEVICES = 64;
+bool ensure_dynamic_lds_here(const void* kern, int bytes, int* per_device);
 
 int cu_count();   // compute units of the device (gemm.hip)
 

@@ -611,8 +611,8 @@ void run(const SampleArgs& a, hipStream_t st) {
     const int lds = LDS ? runs * NT * (int)sizeof(float4) : 0;
     auto kern = k_sample<NT, LDS, PER>;
     if constexpr (LDS) {
-        static int attr_state = 0;
-        if (!ensure_dynamic_lds(reinterpret_cast<const void*>(kern), LDS_ENTRIES * 4, &attr_state)) return;
+        static int attr_state[MAX_DEVICES] = {};
+        if (!ensure_dynamic_lds_here(reinterpret_cast<const void*>(kern), LDS_ENTRIES * 4, attr_state)) return;
     }
     hipLaunchKernelGGL(kern, dim3(a.rows), dim3(NT), lds, st, a, runs);
 }

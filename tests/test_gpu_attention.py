@@ -107,6 +107,10 @@ CASES = [
     ("bf16", 2, 290, 2, 2, 128, 400, dict(window=130, sinks=10)),
     ("bf16", 2, 290, 4, 2, 64, 100, dict(S=200, window=150, sinks=30)),
     ("f32", 1, 200, 2, 2, 64, 300, dict(window=90, sinks=70)),
+    # a window and sinks as large as they come
+    ("bf16", 2, 3, 2, 2, 128, 70, dict(S=40, window=2 ** 31 - 1, sinks=2 ** 31 - 1)),
+    ("f32", 1, 140, 2, 2, 64, 70, dict(window=2 ** 31 - 1)),
+    ("bf16", 2, 1, 2, 2, 64, 700, dict(S=40, window=30, sinks=2 ** 31 - 1)),
     # a window that never reaches the prefix, without sinks: the prefix is not read at all
     ("bf16", 4, 2, 2, 2, 128, 300, dict(S=64, window=50)),
     # sequences of unequal length, absent ones, one that is longer than the cache allows

@@ -149,6 +149,14 @@ def test_strides_alignment_and_outputs_in_place():
     want = run(zz, uu[:3].contiguous(), cfg_scale=4.0, **kw)
     got = run(zz, uu[:3].contiguous(), in_place=True, cfg_scale=4.0, **kw)
     assert all(np.array_equal(a, b) for a, b in zip(want, got))
+    # bf16 rows that begin anywhere
+    zb, ub = rows_of(4, 1501, seed=8, dtype=torch.bfloat16)
+    check(zb, ub, **kw)
+    wb = torch.full((4, 1603), 50.0, dtype=torch.bfloat16, device=DEV)
+    for first in (1, 2, 3):
+        wb[:, first:first + 1501] = zb
+        got = run(wb[:, first:first + 1501], ub, **kw)
+        assert all(np.array_equal(a, b) for a, b in zip(run(zb, ub, **kw), got))
     # outputs one at a time
     p = mulo.make_sample_params(**kw)
     want = run(z, u, **kw)

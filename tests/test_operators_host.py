@@ -42,7 +42,7 @@ def attention_args(**changes):
     (NULL, dict(q=None)), (NULL, dict(out=None)), (NULL, dict(k=None)), (NULL, dict(v=None)), (NULL, dict(prefix_k=None)), (NULL, dict(prefix_v=None)),
     (RANGE, dict(dtype=2)), (RANGE, dict(B=0)), (RANGE, dict(L=0)), (RANGE, dict(n_heads=0)), (RANGE, dict(n_kv_heads=0)), (RANGE, dict(P=-1)),
     (RANGE, dict(rows=0)), (RANGE, dict(prefix_len=-1)), (RANGE, dict(sinks=-1)), (RANGE, dict(window=-1)), (RANGE, dict(n_prefix=0)),
-    (RANGE, dict(scale=-1.0)), (RANGE, dict(scale=math.nan)), (RANGE, dict(scale=math.inf)), (RANGE, dict(q_batch=-8)), (RANGE, dict(v_chan=1 << 41)),
+    (RANGE, dict(scale=-1.0)), (RANGE, dict(scale=math.nan)), (RANGE, dict(scale=math.inf)), (RANGE, dict(scale=1.1e6)), (RANGE, dict(q_batch=-8)), (RANGE, dict(v_chan=1 << 41)),
     (SHAPE, dict(P=63)), (SHAPE, dict(n_kv_heads=3)), (SHAPE, dict(n_prefix=3)), (SHAPE, dict(prefix_len=65)), (SHAPE, dict(k_row=32)),
     (SHAPE, dict(v_chan=56)), (SHAPE, dict(prefix_k_row=56)), (SHAPE, dict(prefix_v_chan=56)),
     # outputs on top of each other
@@ -92,6 +92,7 @@ def test_prefix_and_window_need_a_context(lib):
     (RANGE, dict(cfg_scale=math.nan), {}), (UNSUPPORTED, {}, dict(vocab=262145, stride=262145)), (SHAPE, {}, dict(stride=99)),
     (SHAPE, {}, dict(stride=1 << 41)), (UNSUPPORTED, {}, dict(logits=258)), (UNSUPPORTED, {}, dict(dtype=1, logits=257)),
     (UNSUPPORTED, {}, dict(probs=1025)), (SHAPE, {}, dict(kept=256, dtype=1)), (SHAPE, {}, dict(kept=256, stride=104)),
+    (SHAPE, {}, dict(probs=256)), (SHAPE, {}, dict(probs=1024, kept=1024)),
 ], ids=str)
 def test_sample_arguments(lib, status, changes, call):
     p = mulo.make_sample_params(**changes)
