@@ -678,12 +678,15 @@ Plan make_plan(const ContextAttn& a, int esz, int64_t part_floats) {
     const int TARGET = 512;           // workgroups: two per CU
     const int64_t base = (int64_t)a.B * p.heads * p.tiles;
     const int n_own = own_tiles(a, bkv), n_pre = prefix_tiles(a, bkv);
-    // One launch instead of two, as long as every (sequence, key head) has a CU and streams its keys there about as fast as more
-    // CUs would and the join adds.  Tokens of 32 heads of 128, us, two launches / one: 1 sequence of 60, 250, 500, 1000 rows 6.0 / 5.8,
-    // 9.1 / 7.5, 10.2 / 9.8, 11.7 / 13.8; 4 of 250, 500, 1000 11.2 / 8.5, 14.4 / 12.2, 21.1 / 23.9; 8 (256 workgroups) of 500, 1000,
-    // 2000 21.5 / 17.8, 32.1 / 28.7, 55.2 / 55.5; 16 of 60, 250 8.5 / 11.5, 17.5 / 20.6.  8 behind a prefix of 250, 1000, 60 own
-    // rows 10.6 / 8.7, 13.5 / 14.4.  (float32 is bound by its matrix instruction: 8 x 4 behind 300 20.8 / 31.9.)
-    if (esz == 2 && p.by_kv && p.n <= 32 && !a.pos_tab && base <= cu_count() && n_pre <= 8 && n_own <= (4 * base >= 3 * cu_count() ? 24 : 8)) {
+    // One launch instead of two, as long as every (sequence, key head) has its place on a CU (128 KB of LDS; heads of 64 half) and
+    // streams its keys there about as fast as more CUs would and the join adds.  Tokens of 32 heads of 128, us, two launches / one:
+    // 1 sequence of 60, 250, 500, 700, 1000 rows 6.2 / 5.2, 9.3 / 7.0, 10.2 / 9.3, 11.3 / 10.6, 11.9 / 13.3; 4 of 250, 700, 1000
+    // 11.3 / 8.1, 15.8 / 14.5, 20.7 / 23.4; 8 (256 workgroups) of 500, 1000, 1500 21 / 17, 32 / 28, 44 / 40; 16 of 60, 500 8.8 / 10.7,
+    // 29 / 31; 8 behind a prefix of 250, 500, 1000, 60 own rows 11 / 8, 12.2 / 10, 13.8 / 14.  16 heads of 64: 4, 16, 32
+    // sequences of 1000 rows 11.5 / 9.2, 22 / 16, 30 / 28.  (float32 is bound by its matrix instruction: 8 x 4 behind 300 21 / 32.)
+    const int per_cu = 128 / a.dh, places = cu_count() * per_cu;
+    if (esz == 2 && p.by_kv && p.n <= 32 && !a.pos_tab && base <= places && n_pre <= 12 * per_cu &&
+        n_own + n_pre <= (4 * base >= 3 * places ? 24 : 12) * per_cu) {
         p.few = true;
         return p;
     }
