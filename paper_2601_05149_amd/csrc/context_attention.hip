@@ -525,7 +525,8 @@ __global__ __launch_bounds__(NTH, !FEW && DH * BKV * (int)sizeof(T) <= 16384 ? 2
                 mine[(d * 8 + g4 * 2 + lh) ^ (l32 & (DH / 4 - 1))] = f32x4{o[d][g4 * 4], o[d][g4 * 4 + 1], o[d][g4 * 4 + 2], o[d][g4 * 4 + 3]};
         if (lh == 0) stat[wave][l32] = make_float2(m_run, l_run);
         __syncthreads();
-        for (int x = tid; x < n * (DH / 4); x += NTH) {
+        const int live = n - qt * 32 < 32 ? n - qt * 32 : 32;
+        for (int x = tid; x < live * (DH / 4); x += NTH) {
             const int row = x / (DH / 4), c4 = x % (DH / 4);
             float M = -__builtin_huge_valf();
 #pragma unroll
@@ -539,8 +540,8 @@ __global__ __launch_bounds__(NTH, !FEW && DH * BKV * (int)sizeof(T) <= 16384 ? 2
                 sum += f * reinterpret_cast<const f32x4*>(smem + w * BUF)[row * (DH / 4) + (c4 ^ (row & (DH / 4 - 1)))];
                 den += f * st.y;
             }
-            const int in_head = a.by_L.of(row);      // one tile of queries, of the heads of a key head
-            store4(b, hd * group + in_head, row - in_head * a.L, c4 * 4, sum * (den > 0.f ? 1.0f / den : 0.f));
+            const int rr = qt * 32 + row, in_head = a.by_L.of(rr);      // of the heads of a key head
+            store4(b, hd * group + in_head, rr - in_head * a.L, c4 * 4, sum * (den > 0.f ? 1.0f / den : 0.f));
         }
         return;
     }
@@ -685,9 +686,14 @@ Plan make_plan(const ContextAttn& a, int esz, int64_t part_floats) {
     // 29 / 31; 8 behind a prefix of 250, 500, 1000, 60 own rows 11 / 8, 12.2 / 10, 13.8 / 14.  16 heads of 64: 4, 16, 32
     // sequences of 1000 rows 11.5 / 9.2, 22 / 16, 30 / 28.  (float32 is bound by its matrix instruction: 8 x 4 behind 300 21 / 32.)
     const int per_cu = 128 / a.dh, places = cu_count() * per_cu;
-    if (esz == 2 && p.by_kv && p.n <= 32 && !a.pos_tab && base <= places && n_pre <= 12 * per_cu &&
-        n_own + n_pre <= (4 * base >= 3 * places ? 24 : 12) * per_cu) {
+    const int64_t few = ((int64_t)group * a.L + 31) / 32 * a.B * a.nkv;
+    int few_keys = n_own + n_pre;      // tiles that 32 queries see
+    if (a.window) few_keys = clamp_int(((int64_t)a.window + 32) / bkv + 2 + ((int64_t)a.sinks + bkv - 1) / bkv, 1, few_keys);
+    if (esz == 2 && !a.pos_tab && few <= places && n_pre <= 12 * per_cu && few_keys <= (4 * few >= 3 * places ? 24 : 12) * per_cu) {
         p.few = true;
+        p.by_kv = true;
+        p.heads = a.nkv;
+        p.n = group * a.L;
         return p;
     }
     p.stacked = p.by_kv && n_pre > 0 && a.B > a.G && p.n <= STACK_ROWS && !(a.P_seq && a.window) && slots >= 2;
