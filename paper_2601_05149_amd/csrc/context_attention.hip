@@ -65,7 +65,7 @@ constexpr int STACK_ROWS = 64;       // queries per sequence and key head up to 
 
 // How a launch is laid out (host).
 struct Plan {
-    bool few;          // one workgroup per (sequence, key head), wavefronts with tiles of their own
+    bool few;          // a workgroup per 32 queries, wavefronts with tiles of keys of their own
     bool stacked;      // prefix and own workgroups
     bool by_kv;        // the queries of a workgroup are those of all heads of a key head (else of one head)
     int heads;         // heads, or key heads
@@ -101,7 +101,7 @@ struct Args : ContextAttn, Plan {
     Div by_group, by_in_group, by_L, by_n, by_heads, by_tiles, by_shares, by_gk, by_nkv, by_prefix_tiles;
 };
 
-// FEW (at most 32 queries, few keys): every wavefront has all of the queries and tiles of its own, in a buffer of its own, so that
+// FEW (few keys): every wavefront has all of the workgroup's 32 queries and tiles of keys of its own, in a buffer of its own, so that
 // nobody waits for anybody in front of the end, where the wavefronts' results are joined in LDS.  (Otherwise one of four
 // wavefronts works and a second launch joins.)
 template <class T, int DH, int BQ, int BKV, int NTH, bool FEW>
@@ -684,12 +684,14 @@ Plan make_plan(const ContextAttn& a, int esz, int64_t part_floats) {
     // 1 sequence of 60, 250, 500, 700, 1000 rows 6.2 / 5.2, 9.3 / 7.0, 10.2 / 9.3, 11.3 / 10.6, 11.9 / 13.3; 4 of 250, 700, 1000
     // 11.3 / 8.1, 15.8 / 14.5, 20.7 / 23.4; 8 (256 workgroups) of 500, 1000, 1500 21 / 17, 32 / 28, 44 / 40; 16 of 60, 500 8.8 / 10.7,
     // 29 / 31; 8 behind a prefix of 250, 500, 1000, 60 own rows 11 / 8, 12.2 / 10, 13.8 / 14.  16 heads of 64: 4, 16, 32
-    // sequences of 1000 rows 11.5 / 9.2, 22 / 16, 30 / 28.  (float32 is bound by its matrix instruction: 8 x 4 behind 300 21 / 32.)
+    // sequences of 1000 rows 11.5 / 9.2, 22 / 16, 30 / 28.  Blocks, a workgroup per 32 queries, up to two rounds of them: 1 x 150 queries
+    // of 32 heads of 128, 500 rows in front 22.6 / 12.4, 1 x 300 (320 workgroups) 26 / 21.5, 1 x 403 through a window of 35 22 / 13,
+    // four rounds: 4 x 256 18 / 30, 2 x 502 through one of 27 26.7 / 30; 16 heads of 64: 1 x 500 12 / 7, 1 x 250 through one of 300 18 / 7.  (float32 is bound by its matrix instruction: 8 x 4 behind 300 21 / 32.)
     const int per_cu = 128 / a.dh, places = cu_count() * per_cu;
     const int64_t few = ((int64_t)group * a.L + 31) / 32 * a.B * a.nkv;
     int few_keys = n_own + n_pre;      // tiles that 32 queries see
     if (a.window) few_keys = clamp_int(((int64_t)a.window + 32) / bkv + 2 + ((int64_t)a.sinks + bkv - 1) / bkv, 1, few_keys);
-    if (esz == 2 && !a.pos_tab && few <= places && n_pre <= 12 * per_cu && few_keys <= (4 * few >= 3 * places ? 24 : 12) * per_cu) {
+    if (esz == 2 && !a.pos_tab && few <= (group * a.L > 32 ? 2 : 1) * (int64_t)places && n_pre <= 12 * per_cu && few_keys <= (4 * few >= 3 * places ? 24 : 12) * per_cu) {
         p.few = true;
         p.by_kv = true;
         p.heads = a.nkv;
