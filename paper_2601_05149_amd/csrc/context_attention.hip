@@ -61,7 +61,6 @@ template <> struct Chunk<float> {
 
 constexpr float LAZY_EXP = 8.0f;     // the reference of the exponentials moves once the maximum has outgrown it by 2^8 (bf16; see attention.hip)
 constexpr int MAX_SLOTS = 64;        // shares of a query that k_context_join joins: a lane each
-constexpr int STACK_ROWS = 64;       // queries per sequence and key head up to which sequences are stacked over their prefix
 
 // How a launch is laid out (host).
 struct Plan {
@@ -256,8 +255,12 @@ __global__ __launch_bounds__(NTH, !FEW && DH * BKV * (int)sizeof(T) <= 16384 ? 2
     // the same chunk of 16 rows touch every bank once.
     auto key_of = [](int r, int row_bytes) { return row_bytes >= 256 ? r & 15 : row_bytes == 128 ? (r >> 1) & 7 : (r >> 2) & 3; };
     const int krow = tw * RK + lane / (64 / RK), vrow = tw * RV + lane / (64 / RV);
-    static_assert(TW * RV % 16 == 0, "the key of a lane's rows of V^T");
-    const int vchunk = lane % (64 / RV) ^ key_of(vrow, VRB);
+    // this lane's chunk of a row of V^T in load x: the same in all where the rows of a load repeat the key, else one in the even and one in the odd
+    constexpr int VKEYS = TW * RV % 16 == 0 ? 1 : 2;
+    static_assert(VKEYS * TW * RV % 16 == 0, "the keys of a lane's rows of V^T");
+    int vchunk[VKEYS];
+#pragma unroll
+    for (int y = 0; y < VKEYS; ++y) vchunk[y] = lane % (64 / RV) ^ key_of(vrow + y * TW * RV, VRB);
     const unsigned char* const pk = reinterpret_cast<const unsigned char*>(reinterpret_cast<const T*>(a.pk) + g * a.pk_group + kvh * a.pk_head);
     const unsigned char* const pv = reinterpret_cast<const unsigned char*>(reinterpret_cast<const T*>(a.pv) + g * a.pv_group + kvh * a.pv_head + (int64_t)tw * RV * a.pv_chan);
     const unsigned char* const ok = reinterpret_cast<const unsigned char*>(reinterpret_cast<const T*>(a.k) + b * a.k_batch + kvh * a.k_head);
@@ -285,9 +288,13 @@ __global__ __launch_bounds__(NTH, !FEW && DH * BKV * (int)sizeof(T) <= 16384 ? 2
         if (of_v) {
             const int64_t v_chan = (pre ? a.pv_chan : a.v_chan) * (int64_t)sizeof(T);
             const unsigned char* const vt = (pre ? pv : ov) + (int64_t)t * VRB;
-            const uint32_t vo = (uint32_t)(lane / (64 / RV)) * (uint32_t)v_chan + (uint32_t)(vchunk * E < left - E ? vchunk * E : left - E) * (uint32_t)sizeof(T);
 #pragma unroll
-            for (int x = 0; x < LV; ++x) to_lds(vt + x * (TW * RV) * v_chan, vo, lds + KT + x * TW * 1024);
+            for (int y = 0; y < VKEYS; ++y) {
+                const int c = vchunk[y] * E;
+                const uint32_t vo = (uint32_t)(lane / (64 / RV)) * (uint32_t)v_chan + (uint32_t)(c < left - E ? c : left - E) * (uint32_t)sizeof(T);
+#pragma unroll
+                for (int x = y; x < LV; x += VKEYS) to_lds(vt + x * (TW * RV) * v_chan, vo, lds + KT + x * TW * 1024);
+            }
         }
     };
     auto load_kv = [&](int i) { load(i, true, true); };
@@ -300,17 +307,20 @@ __global__ __launch_bounds__(NTH, !FEW && DH * BKV * (int)sizeof(T) <= 16384 ? 2
         const int k0 = tile_of(i) * BKV, end = pre ? S : own_end, lo = pre ? pre_lo : own_lo, head = pre ? pre_a : own_a;
         if (k0 + BKV > end || (k0 < lo && k0 + BKV > head)) {
             if (!FEW) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // FEW: the caller has waited
-            const int key = k0 + vchunk * E;
-            auto seen = [&](int e) { return key + e < end && (key + e < head || key + e >= lo); };
-            auto keep = [&](int w) -> uint32_t {
-                if constexpr (BF16) return (seen(2 * w) ? 0xFFFFu : 0u) | (seen(2 * w + 1) ? 0xFFFF0000u : 0u);
-                else return seen(w) ? 0xFFFFFFFFu : 0u;
-            };
-            const u32x4 mask = {keep(0), keep(1), keep(2), keep(3)};
 #pragma unroll
-            for (int x = 0; x < LV; ++x) {
-                u32x4* const at = reinterpret_cast<u32x4*>(buffer(i) + KT + (x * TW + tw) * 1024 + lane * 16);
-                *at = *at & mask;
+            for (int y = 0; y < VKEYS; ++y) {
+                const int key = k0 + vchunk[y] * E;
+                auto seen = [&](int e) { return key + e < end && (key + e < head || key + e >= lo); };
+                auto keep = [&](int w) -> uint32_t {
+                    if constexpr (BF16) return (seen(2 * w) ? 0xFFFFu : 0u) | (seen(2 * w + 1) ? 0xFFFF0000u : 0u);
+                    else return seen(w) ? 0xFFFFFFFFu : 0u;
+                };
+                const u32x4 mask = {keep(0), keep(1), keep(2), keep(3)};
+#pragma unroll
+                for (int x = y; x < LV; x += VKEYS) {
+                    u32x4* const at = reinterpret_cast<u32x4*>(buffer(i) + KT + (x * TW + tw) * 1024 + lane * 16);
+                    *at = *at & mask;
+                }
             }
         }
     };
@@ -643,6 +653,8 @@ void join(const Args& a, int slots, hipStream_t st) {
 // tile of 32 keys and wavefront): smaller tiles deal its keys to more workgroups (heads of 64, 64 / 32 keys, us: 1 x 150 queries,
 // 500 rows 22.5 / 17.9, 16 tokens of 8 heads, 1000 shared and 1000 own rows 50 / 34, 2 x 8 16.5 / 13; 4 tokens of 16 heads, 2000 rows 47 / 51).
 constexpr int small_tile(int esz) { return esz == 2 ? 64 : 32; }
+// Wavefronts of the one-launch kernel: 8, or as many as have room for a tile of 32 keys each in 128 KB.
+constexpr int few_waves(int esz, int dh) { return esz * dh > 256 ? 4 : 8; }
 
 // Key tiles that the queries see at most (host; P rows in front of the block)
 int own_tiles(const ContextAttn& a, int bkv) {
@@ -665,6 +677,19 @@ int prefix_tiles(const ContextAttn& a, int bkv) {
 
 int clamp_int(int64_t v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : (int)v; }
 
+// What a tile costs a workgroup, in halves of what it costs one with 32 queries: float32 wavefronts get in each other's way (16 x 5 of
+// 16 heads of 128, 100 own rows, 300 and 600 shared: as 3 halves 33.5 and 35 us, as 2 42.5 and 43; bf16 8 x 16 of 32 heads, 200 and
+// 1000 rows, 27.7 and 23.8).
+int tile_cost(int esz, int64_t queries) { return esz == 4 && queries > 32 ? 3 : 2; }
+// When the last of a launch's workgroups ends, where `places` run at a time: first `prefix` ones of `prefix_time` each, behind them `own` ones.
+int64_t makespan(int64_t prefix, int64_t prefix_time, int64_t own, int64_t own_time, int64_t places) {
+    const int64_t t = prefix / places * prefix_time, busy = prefix % places;
+    if (!busy) return t + (own + places - 1) / places * own_time;
+    if (own <= places - busy) return t + (prefix_time > own_time ? prefix_time : own_time);
+    const int64_t left = own - (places - busy) * (prefix_time / own_time);      // once the last prefix workgroup has ended
+    return t + prefix_time + (left > 0 ? (left + places - 1) / places * own_time : 0);
+}
+
 // part_floats: the scratch there is (context_attention_floats asks with as much as can be wanted)
 Plan make_plan(const ContextAttn& a, int esz, int64_t part_floats) {
     Plan p{};
@@ -686,31 +711,61 @@ Plan make_plan(const ContextAttn& a, int esz, int64_t part_floats) {
     // 29 / 31; 8 behind a prefix of 250, 500, 1000, 60 own rows 11 / 8, 12.2 / 10, 13.8 / 14.  16 heads of 64: 4, 16, 32
     // sequences of 1000 rows 11.5 / 9.2, 22 / 16, 30 / 28.  Blocks, a workgroup per 32 queries, up to two rounds of them: 1 x 150 queries
     // of 32 heads of 128, 500 rows in front 22.6 / 12.4, 1 x 300 (320 workgroups) 26 / 21.5, 1 x 403 through a window of 35 22 / 13,
-    // four rounds: 4 x 256 18 / 30, 2 x 502 through one of 27 26.7 / 30; 16 heads of 64: 1 x 500 12 / 7, 1 x 250 through one of 300 18 / 7.  (float32 is bound by its matrix instruction: 8 x 4 behind 300 21 / 32.)
+    // four rounds: 4 x 256 18 / 30, 2 x 502 through one of 27 26.7 / 30; 16 heads of 64: 1 x 500 12 / 7, 1 x 250 through one of 300 18 / 7.
+    // float32 is bound by its matrix instruction: only where every wavefront has one tile.  8 heads of 64 and 8 key heads, us: 1 token,
+    // 40 rows 8.9 / 6.3, 16 behind a prefix of 100 11.7 / 7.4, 1 x 100 queries 10.0 / 6.6, three tiles a wavefront: 1 of 500 rows
+    // 9.3 / 13.3, 1 x 60 queries behind 200 rows 10.3 / 12.0; 8 heads of 128: 4 tokens of 50 rows 11.0 / 9.6, 1 x 100 13.9 / 10.2.
     const int per_cu = 128 / a.dh, places = cu_count() * per_cu;
     const int64_t few = ((int64_t)group * a.L + 31) / 32 * a.B * a.nkv;
     int few_keys = n_own + n_pre;      // tiles that 32 queries see
     if (a.window) few_keys = clamp_int(((int64_t)a.window + 32) / bkv + 2 + ((int64_t)a.sinks + bkv - 1) / bkv, 1, few_keys);
-    if (esz == 2 && !a.pos_tab && few <= (group * a.L > 32 ? 2 : 1) * (int64_t)places && n_pre <= 12 * per_cu && few_keys <= (4 * few >= 3 * places ? 24 : 12) * per_cu) {
+    const bool fits = esz == 2 ? few <= (group * a.L > 32 ? 2 : 1) * (int64_t)places && n_pre <= 12 * per_cu && few_keys <= (4 * few >= 3 * places ? 24 : 12) * per_cu
+                               : few <= cu_count() && few_keys <= few_waves(4, a.dh);
+    if (!a.pos_tab && fits) {
         p.few = true;
         p.by_kv = true;
         p.heads = a.nkv;
         p.n = group * a.L;
         return p;
     }
-    p.stacked = p.by_kv && n_pre > 0 && a.B > a.G && p.n <= STACK_ROWS && !(a.P_seq && a.window) && slots >= 2;
-    if (p.stacked) {
+    const int n = n_own + n_pre;
+    const int whole_split = a.L <= 128 ? clamp_int(TARGET / base, 1, MAX_SLOTS < n ? MAX_SLOTS : n) : 1;
+    // Stacked or whole: the tiles that follow one another on a place, at some 1.2 us a tile (float32, bound by its matrix instruction: 2.6
+    // and 5.1 us with heads of 64 and 128), against the partial results that stacking writes and reads more of (5 TB/s), and the join's launch
+    // where there would be none.  How finely the keys are dealt is that of the shortest makespan: a few workgroups more than have a
+    // place cost as much as a second round of them (4 tokens of 32 heads of 128, 2000 own and shared rows: 640 workgroups 47.7 us, 448
+    // 37.7).  us, whole / stacked, 32 heads of 128, rows own + shared: 4 tokens 100 + 2000 23.2 / 15.7, 8 of 1000 + 1000 42.4 / 43.3,
+    // 2000 + 500 61 / 68, 32 of 200 + 4000 225 / 47; 16 x 4 200 + 500 29.4 / 27.3; 8 x 64 500 + 2000 63 / 53; 8 key heads: 16 x 4
+    // 100 + 1000 16.8 / 18.6 and 100 + 4000 35.7 / 25; 64 x 16 100 + 300 24 / 39.  float32, 8 heads of 64: 16 tokens 100 + 400
+    // 22.4 / 13.9, 6 x 5 300 + 333 17.3 / 14.1; 16 of 128: 16 x 5 100 + 600 61 / 35, 800 + 300 94 / 130.
+    if (p.by_kv && n_pre > 0 && !(a.P_seq && a.window) && slots >= 2) {
         p.prefix_tiles = (int)(((int64_t)(a.B / a.G) * p.n + 127) / 128);
         const int64_t pbase = (int64_t)a.G * a.nkv * p.prefix_tiles;
-        const int64_t work = base * n_own + pbase * n_pre;      // tiles of all workgroups
-        const int64_t per = (work + TARGET - 1) / TARGET;
-        p.split = clamp_int((n_own + per - 1) / per, 1, slots / 2 < n_own ? slots / 2 : n_own);
-        p.prefix_split = clamp_int((n_pre + per - 1) / per, 1, slots - p.split < n_pre ? slots - p.split : n_pre);
-        p.prefix_wgs = (int)(pbase * p.prefix_split);
+        const int own_cost = tile_cost(esz, p.n), prefix_cost = tile_cost(esz, (int64_t)(a.B / a.G) * p.n);
+        int64_t best = INT64_MAX;
+        for (int64_t per = (base * n_own + pbase * n_pre + TARGET - 1) / TARGET;; per += 1 + per / 16) {      // tiles of a workgroup
+            const int s = clamp_int((n_own + per - 1) / per, 1, MAX_SLOTS / 2), ps = clamp_int((n_pre + per - 1) / per, 1, MAX_SLOTS - s);
+            const int64_t t = makespan(pbase * ps, (n_pre + ps - 1) / ps * prefix_cost, base * s, (n_own + s - 1) / s * own_cost, TARGET);
+            if (t <= best) best = t, p.split = s, p.prefix_split = ps;
+            if (s == 1 && ps == 1) break;
+        }
+        const int64_t whole = (base * whole_split + TARGET - 1) / TARGET * ((n + whole_split - 1) / whole_split) * own_cost;
+        const int more = p.split + p.prefix_split - (whole_split > 1 ? whole_split : 0);
+        const double gain = (double)(whole - best) / 2 * (esz == 2 ? 1.2 : a.dh * 0.04);
+        const double cost = (more > 0 ? more : 0) * (double)slot_floats * 8 / 5e6 + (whole_split > 1 ? 0 : 3);
+        p.stacked = gain > cost;
+    }
+    if (p.stacked) {
+        if (p.split + p.prefix_split > slots) {      // less scratch than this runs fastest with
+            const int half = slots / 2;
+            if (p.split <= half) p.prefix_split = slots - p.split;
+            else if (p.prefix_split <= half) p.split = slots - p.prefix_split;
+            else p.split = half, p.prefix_split = slots - half;
+        }
+        p.prefix_wgs = (int)((int64_t)a.G * a.nkv * p.prefix_tiles * p.prefix_split);
         return p;
     }
-    const int n = n_own + n_pre;
-    if (slots >= 2 && a.L <= 128) p.split = clamp_int(TARGET / base, 1, slots < n ? slots : n);
+    p.split = whole_split < slots ? whole_split : slots < 1 ? 1 : slots;
     // Long blocks that do not find a CU each: shares of at least 4 tiles (float32, whose matrix instruction takes 16 times as long: 2) of
     // what a query sees on average, bf16 from 12 of them on.  1 x 300 queries, 1000 rows in front, us, whole / in shares: bf16
     // 32 heads of 128 37 / 27, 16 of 64 24 / 16, float32 8 of 64 101 / 25; 1 x 1024, nothing in front (8 tiles): 16 of 64 19 / 22;
@@ -752,8 +807,8 @@ void run(const ContextAttn& c, hipStream_t st) {
     static_cast<ContextAttn&>(a) = c;
     static_cast<Plan&>(a) = make_plan(c, sizeof(T), c.part ? c.part_floats : 0);
     constexpr int SMALL = small_tile(sizeof(T));
+    if (a.few) return run_cfg<T, DH, 32, 32, 64 * few_waves(sizeof(T), DH), true>(a, st);
     if constexpr (sizeof(T) == 2) {
-        if (a.few) return run_cfg<T, DH, 32, 32, 512, true>(a, st);
         // long blocks that go over their keys as a whole: tiles of 128 keys, and 256 queries where 128 would not find a CU each (heads of 128), as in attention.hip
         if (c.L > 128 && !c.pos_tab && a.split == 1) {
             if (DH == 128 && (int64_t)c.B * c.nh * ((c.L + 127) / 128) > cu_count()) return run_cfg<T, DH, DH == 128 ? 256 : 128, 128, DH == 128 ? 512 : 256>(a, st);
