@@ -10,6 +10,10 @@
 // Masses are integers, w = rint(2^44 2^((z - max z) log2(e) / T)): their sums (at most 2^62) do not depend on their order, so
 // neither atomics nor the shape of a launch show in a result, and at 2^-45 of the largest weight an entry they place a
 // border or a draw where sums in 64-bit floating point place it.
+//
+// What bounds it: one row, the chain of its passes and barriers (16384 entries, top-k 2000: 26 thousand cycles, 11.7 us, of which
+// the launch is 5; 32 guided rows 16.1); many rows, vector instructions: 61 an entry, the vector pipes busy 87 % (2048 rows of 16384,
+// top-p and min-p, logits out: 81 us, 3.3 TB/s of the 5.05 that a copy reaches).
 #include <hip/hip_bf16.h>
 
 #include <type_traits>
@@ -118,7 +122,9 @@ __device__ __forceinline__ float wave_max(float v) {
 // Wavefront w has the stretch [w seg, (w + 1) seg) of the row, in runs of 256: consecutive lanes, consecutive entries.
 // A thread takes the same entries in every pass.
 // PER: entries of the list a thread takes.  Where top-k leaves at most PER NT entries they are listed, and everything behind it
-// (masses, top-p, the draw's sums, what is written of them) goes by the list: of 16384 entries 2000 cost an eighth.
+// (masses, top-p, the draw's sums, what is written of them) goes by the list: of 16384 entries 2000 cost an eighth (a row of 16384,
+// 512 threads, top-p 0.9 alone 19.6 us, behind top-k 200 13.6).  With 512 threads two entries a thread would take 8 KB
+// that the second row of a CU needs.
 template <int NT, bool LDS, int PER>
 __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
     constexpr int NW = NT / 64;
@@ -622,11 +628,16 @@ void run(const SampleArgs& a, hipStream_t st) {
 void launch_sample_filtered(const SampleArgs& args, hipStream_t st) {
     SampleArgs a = args;
     a.min_p_below = a.min_p > 0.0 ? a.temperature * log(a.min_p) : 0.0;
-    if (a.V <= 2048) run<256, true, 2>(a, st);
-    else if (a.V <= LDS_ENTRIES) {
-        if (a.rows > cu_count()) run<512, true, 1>(a, st);
-        else run<1024, true, 2>(a, st);
-    }
+    // A row that has a CU to itself ends soonest with 1024 threads, a short one with 256, whose barriers cost less; more rows than CUs
+    // share them, by the side of each other while two rows and their bins find room in LDS.  us, threads 256 / 512 / 1024:
+    //   1 row of 1000 entries 7.9 / - / 8.2, 4096 11.2 / 9.2 / 9.5, 16384 29 / 19.6 / 16.4, 32768 - / 34 / 27
+    //   600 rows of 1000 10.9 / 15.0 / -, 4096 17.2 / 19.6 / 27, 8192 26.5 / 27.6 / 33, 16384 64 / 47 / 53, 32768 - / 110 / 89
+    //   2048 rows of 2048 23.5 / 34 / -, 4096 34 / 44 / 68, 8192 64 / 62 / 87, 16384 146 / 108 / 138
+    // Kept in LDS / read again in every pass (1024 threads): 1 row of 8192 11.9 / 14.7, of 32768 26.9 / 30.5, 256 of 32768 33.6 / 37.5.
+    const bool many = a.rows > cu_count();
+    if (a.V <= (many ? 4096 : 2048)) run<256, true, 2>(a, st);
+    else if (many && a.V <= LDS_ENTRIES / 2) run<512, true, 1>(a, st);
+    else if (a.V <= LDS_ENTRIES) run<1024, true, 2>(a, st);
     else run<1024, false, 2>(a, st);
 }
 

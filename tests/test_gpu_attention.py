@@ -12,6 +12,12 @@ DT = {"bf16": torch.bfloat16, "f32": torch.float32}
 NAN = float("nan")
 
 
+def sees(p, L, n, sinks, window):
+    """[L, n]: which of n positions the queries at p, p + 1, ... see."""
+    t, at = torch.arange(n), torch.arange(p, p + L)[:, None]
+    return (t <= at) & (torch.tensor(window == 0) | (t < sinks) | (at - t < window))
+
+
 def make(dtype, B, L, nh, nkv, dh, P, G=1, S=0, sinks=0, window=0, starts=None, seed=0, gain=1.0, rows=None):
     g = torch.Generator().manual_seed(seed)
     dt = DT[dtype]
@@ -25,12 +31,10 @@ def make(dtype, B, L, nh, nkv, dh, P, G=1, S=0, sinks=0, window=0, starts=None, 
     own, pre = torch.zeros(B, rows, dtype=torch.bool), torch.zeros(G, max(srows, 1), dtype=torch.bool)
     c["starts"] = [min(p, rows - L) for p in c["starts"]]
     for b, p in enumerate(c["starts"]):
-        for j in range(L if p >= 0 else 0):
-            for t in OC.visible_keys(S + p + j, sinks, window):
-                if t < S:
-                    pre[b // (B // G), t] = True
-                else:
-                    own[b, t - S] = True
+        if p >= 0:
+            seen = sees(S + p, L, S + p + L, sinks, window).any(0)
+            pre[b // (B // G), :S] |= seen[:S]
+            own[b, :p + L] |= seen[S:]
     for b in range(B):
         c["k"][b, :, ~own[b]] = NAN
         c["v"][b, :, :, ~own[b]] = NAN
@@ -55,9 +59,37 @@ def workspace(plan, fill=0xFF):
     return torch.full((n,), fill, dtype=torch.uint8, device=DEV) if n else None      # 0xFF..: NaN as bf16 and as float32
 
 
-def check(c, out, label, scale=None):
+def plain(c):
+    """The definition with the queries of a sequence side by side, for cases that the oracle takes too long over; float64, on the device."""
+    B, nh, L, dh = c["q"].shape
+    group, S = nh // c["k"].shape[1], c["S"]
+    out, mass = torch.zeros(B, nh, L, dh, dtype=torch.float64), torch.zeros(B, nh, L, dh, dtype=torch.float64)
+    reach, keys = torch.zeros(B, nh, L, dtype=torch.float64), torch.zeros(B, L)
+    for b, p in enumerate(c["starts"]):
+        if p < 0:
+            continue
+        n = S + p + L
+        K, V = c["k"][b, :, :p + L], c["v"][b, :, :, :p + L].transpose(1, 2)
+        if S:
+            g = b // (B // c["pk"].shape[0])
+            K, V = torch.cat([c["pk"][g, :, :S], K], 1), torch.cat([c["pv"][g, :, :, :S].transpose(1, 2), V], 1)
+        see = sees(S + p, L, n, c["sinks"], c["window"])
+        keys[b] = see.sum(1)
+        see = see.to(DEV)
+        for h in range(nh):
+            q, Kh, Vh = c["q"][b, h].to(DEV).double(), K[h // group].to(DEV).double(), V[h // group].to(DEV).double()
+            Kh, Vh = torch.nan_to_num(Kh), torch.nan_to_num(Vh)          # no query sees those rows
+            z = (q @ Kh.t().contiguous() * dh ** -0.5).masked_fill(~see, float("-inf"))
+            e = torch.exp(z - z.max(-1, keepdim=True).values)
+            w = e / e.sum(-1, keepdim=True)
+            out[b, h], mass[b, h] = (w @ Vh).cpu(), (w @ Vh.abs()).cpu()
+            reach[b, h] = (q.abs() @ Kh.abs().t().contiguous() * dh ** -0.5).masked_fill(~see, 0.0).max(-1).values.cpu()
+    return out, mass, reach, keys
+
+
+def check(c, out, label, scale=None, reference=None):
     # a NaN in the caches would spread through the oracle's products, which take the visible rows only
-    want, mass, reach, keys = OC.context_attention(c["q"], c["k"], c["v"], c["starts"], c["pk"], c["pv"], c["S"], c["sinks"], c["window"], scale)
+    want, mass, reach, keys = reference or OC.context_attention(c["q"], c["k"], c["v"], c["starts"], c["pk"], c["pv"], c["S"], c["sinks"], c["window"], scale)
     tol = OC.tolerance(mass, reach, keys, want, c["q"].shape[-1], c["bf16"])
     err = (out.double().cpu() - want).abs()
     assert torch.isfinite(out).all(), "%s: not finite" % label
@@ -136,6 +168,76 @@ def test_attention(case):
         check(c, out, "scratch" if use else "no scratch")
 
 
+# Sizes at which keys are dealt to several workgroups, and those of more queries
+DEALT = [
+    # the rows of all sequences over the prefix together: single tokens, two and three groups, shared key heads, more than 64 rows of a
+    # sequence, ragged and absent sequences, a window that cuts the prefix, sinks that the window has left behind
+    ("bf16", 8, 1, 8, 8, 128, 70, dict(S=1000)),
+    ("bf16", 10, 1, 8, 8, 64, 100, dict(S=1801, G=2)),
+    ("bf16", 15, 5, 16, 4, 128, 150, dict(S=1901, G=3)),
+    ("bf16", 16, 24, 8, 4, 64, 30, dict(S=4000)),
+    ("bf16", 16, 91, 8, 8, 64, 9, dict(S=3001)),
+    ("bf16", 8, 3, 8, 8, 128, 300, dict(S=1000, starts=[300, 0, -1, 5, 64, 63, 128, -9])),
+    ("bf16", 8, 2, 8, 8, 128, 200, dict(S=1500, window=1300, sinks=130)),
+    ("bf16", 8, 2, 8, 8, 128, 400, dict(S=1500, window=300, sinks=1400)),
+    ("f32", 16, 3, 8, 8, 64, 40, dict(S=333)),
+    ("f32", 8, 7, 8, 4, 128, 100, dict(S=500, G=2, starts=[-1, 100, 0, 31, 32, 33, -1, 99])),
+    ("f32", 8, 40, 8, 8, 64, 70, dict(S=400)),
+    # each sequence on its own, its keys dealt to 8 and more workgroups
+    ("bf16", 2, 1, 4, 4, 128, 1500, {}),
+    ("bf16", 1, 100, 2, 2, 128, 1700, {}),
+    ("bf16", 3, 16, 8, 1, 64, 1600, dict(window=1555, sinks=33)),
+    ("bf16", 3, 4, 4, 2, 128, 1800, dict(starts=[1800, -1, 3], window=1700, sinks=2)),
+    ("bf16", 2, 1, 4, 2, 128, 900, dict(S=800, G=2, starts=[10, 900])),
+    ("bf16", 16, 45, 8, 4, 128, 30, dict(S=2500)),
+    # float32 over few keys: a tile a wavefront
+    ("f32", 3, 5, 4, 2, 128, 60, dict(S=33)),
+    ("f32", 2, 40, 2, 2, 128, 300, dict(window=20, sinks=3)),
+    ("f32", 4, 2, 4, 2, 128, 50, dict(S=20, G=2, starts=[50, -1, 0, 7])),
+    ("f32", 3, 70, 2, 1, 64, 100, dict(S=40, starts=[-1, 100, 31], window=90, sinks=41)),
+    # long blocks: 256 and 128 queries a workgroup over tiles of 128 keys
+    ("bf16", 5, 150, 32, 32, 128, 33, dict(S=77)),
+    ("bf16", 4, 150, 32, 32, 128, 33, {}),
+    ("bf16", 5, 140, 32, 8, 128, 100, dict(starts=[100, -1, 0, 17, 64], S=50)),
+    ("bf16", 5, 260, 32, 32, 128, 60, dict(window=100, sinks=10)),
+    ("bf16", 8, 150, 32, 32, 64, 40, dict(S=200, window=150, sinks=9)),
+    ("f32", 2, 150, 2, 2, 64, 900, dict(S=70)),
+]
+name_of = lambda c: "%s-%dx%d-h%d.%d-%d-P%d%s" % (c[:7] + ("".join("-%s%s" % (k, v) for k, v in c[7].items() if k != "starts"),))
+
+
+@pytest.mark.parametrize("case", [CASES[i] for i in (2, 11, 20, 29, 40)], ids=name_of)
+def test_plain_form_is_the_oracle(case):
+    dtype, B, L, nh, nkv, dh, P, kw = case
+    c = make(dtype, B, L, nh, nkv, dh, P, **kw)
+    out, mass, reach, keys = plain(c)
+    want = OC.context_attention(c["q"], c["k"], c["v"], c["starts"], c["pk"], c["pv"], c["S"], c["sinks"], c["window"])
+    # Two forms of float64, each off by what the bound of the oracle's module says of float32 with 2^-53 for 2^-24 (and 2^-50 for an
+    # exponential's 2^-22): a score by (dh + 8) 2^-53 reach, so a weight, numerator and denominator, by twice that; sums of n terms
+    # by (n + 8) 2^-53, twice.
+    rel = 2 * ((dh + 8) * 2.0 ** -53 * reach + 2.0 ** -50) + 2 * (keys[:, None, :] + 8) * 2.0 ** -53
+    far = [((a - b).abs() > 2 * tol).sum().item() for a, b, tol in zip(
+        (out, mass, reach), want, (mass * rel[..., None], mass * rel[..., None], (dh + 8) * 2.0 ** -53 * reach))]
+    assert far == [0, 0, 0] and torch.equal(keys, want[3])
+
+
+@pytest.mark.parametrize("case", DEALT, ids=name_of)
+def test_dealt_keys_and_many_queries(case):
+    dtype, B, L, nh, nkv, dh, P, kw = case
+    c = make(dtype, B, L, nh, nkv, dh, P, **kw)
+    d = on_device(c)
+    reference = plain(c)
+    plan = plan_of(c, d, torch.empty_like(d["q"]))
+    asked = mulo.mulo_attention_workspace_bytes(plan)
+    least = B * nh * L * (dh + 2) * 4
+    for share in (1.0, 0.6, 0.0):            # with the scratch it asks for (holding NaN), with less, and with none
+        out = torch.full_like(d["q"], NAN)
+        n = int(asked * share) // 4 * 4
+        mulo.mulo_attention(plan_of(c, d, out), torch.full((n,), 0xFF, dtype=torch.uint8, device=DEV) if n else None)
+        torch.cuda.synchronize()
+        check(c, out, "%d of %d results of a query" % (n // least, asked // least), reference=reference)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_sharp_and_scaled_scores(dtype):
     """Scores of a hundred and more: nearly all of the mass on one key; and a scale of the caller's."""
@@ -195,8 +297,9 @@ def test_offsets_beyond_32_bits():
         assert torch.isfinite(outs[0]).all() and off <= 2.0 ** -6, off      # keys meet in other tiles: other roundings
 
 
-def test_bits_do_not_depend_on_the_workspace_or_the_run():
-    c = make("bf16", 8, 1, 4, 4, 128, 500, S=300, G=2)
+@pytest.mark.parametrize("dtype, nh, S", [("bf16", 4, 300), ("bf16", 8, 1300), ("f32", 4, 300)])
+def test_bits_do_not_depend_on_the_workspace_or_the_run(dtype, nh, S):
+    c = make(dtype, 8, 1, nh, nh, 128, 500, S=S, G=2)
     d = on_device(c)
     outs = []
     for fill in (0, 0xFF, 0x7F):
@@ -207,16 +310,17 @@ def test_bits_do_not_depend_on_the_workspace_or_the_run():
     assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
 
 
-def test_recorded_and_replayed_with_growing_sequences():
+@pytest.mark.parametrize("nh, S", [(4, 90), (16, 1801)])
+def test_recorded_and_replayed_with_growing_sequences(nh, S):
     """One graph serves a decoding loop: the lengths live on the device, the launch is sized by the longest."""
-    c = make("bf16", 6, 1, 4, 4, 64, 300, S=90, starts=[300] * 6)
+    c = make("bf16", 6, 1, nh, nh, 64, 300, S=S, starts=[300] * 6)
     for t in ("k", "v", "pk", "pv"):
         c[t] = torch.nan_to_num(c[t])
     d = on_device(c)
     side = torch.cuda.Stream()
     P_seq = torch.zeros(6, dtype=torch.int32, device=DEV)
     out = torch.empty_like(d["q"])
-    plan = mulo.make_attention(d["q"], out, d["k"], d["v"], 300, P_seq=P_seq, prefix_k=d["pk"], prefix_v=d["pv"], prefix_len=90)
+    plan = mulo.make_attention(d["q"], out, d["k"], d["v"], 300, P_seq=P_seq, prefix_k=d["pk"], prefix_v=d["pv"], prefix_len=S)
     ws, other = workspace(plan), torch.empty_like(out)
     with torch.cuda.stream(side):
         mulo.mulo_attention(plan, ws)
@@ -232,7 +336,7 @@ def test_recorded_and_replayed_with_growing_sequences():
             side.synchronize()
             c["starts"] = lens
             check(c, out, "replay %d" % rep)
-            eager = mulo.make_attention(d["q"], other, d["k"], d["v"], 300, P_seq=P_seq, prefix_k=d["pk"], prefix_v=d["pv"], prefix_len=90)
+            eager = mulo.make_attention(d["q"], other, d["k"], d["v"], 300, P_seq=P_seq, prefix_k=d["pk"], prefix_v=d["pv"], prefix_len=S)
             mulo.mulo_attention(eager, workspace(eager))
             side.synchronize()
             assert torch.equal(out, other)

@@ -63,6 +63,20 @@ def test_vocabularies(V):
     check(z, u, temperature=0.7, top_k=max(1, V // 3), top_p=0.8, min_p=0.01)
 
 
+@pytest.mark.parametrize("V", [1000, 4000, 16000, 20001])
+def test_more_rows_than_compute_units(V):
+    """Many rows are dealt otherwise than few: the first and last against the definition, all with the bits they have in small calls."""
+    R = torch.cuda.get_device_properties(0).multi_processor_count + 9
+    z, u = rows_of(R, V, seed=V)
+    for kw in (dict(top_k=700, top_p=0.9), dict(temperature=0.8, top_p=0.9, min_p=1e-3), dict(top_k=60)):
+        every = run(z, u, **kw)
+        for a, b in ((0, 3), (R // 2, R // 2 + 100), (R - 3, R)):
+            few = run(z[a:b], u[a:b].contiguous(), **kw)
+            for x, y in zip(every, few):
+                assert np.array_equal(x[a:b].view(np.int32), y.view(np.int32))
+        check(z[-2:], u[-2:].contiguous(), **kw)
+
+
 @pytest.mark.parametrize("V", [70000, 131072, 262144])
 def test_large_vocabularies(V):
     z, u = rows_of(2, V, seed=V, spread=3.0)
