@@ -342,7 +342,7 @@ MULO_API mulo_status mulo_resample_islands(mulo_ctx *ctx, mulo_kv *kv, int32_t B
  * not overlap.
  * Limits: head_dim 64 or 128; n_heads a multiple of n_kv_heads, B of n_prefix; rows, prefix_rows and every stride a multiple
  * of 16 bytes, pointers 16-byte aligned; rows, prefix_rows <= 2^24, k rows at most 2^22 and v channels 2^26 elements apart;
- * B * n_heads * L < 2^30. */
+ * B * n_heads <= 2^22, B * n_heads * L < 2^26. */
 typedef struct {
     int32_t dtype, B, L, n_heads, n_kv_heads, head_dim;
     const void *q;
@@ -426,10 +426,11 @@ typedef struct {
  *               entry above -inf
  *   probs       device float32 [rows, vocab] (out) or NULL: the filtered distribution (a row of zeros if there is none):
  *               what mulo_upsample_draft and the accept test take as a draft's
- *   logits_out  device float32 [rows, vocab] (out) or NULL: z / temperature where the entry stays (z with temperature 0;
- *               kept within float32's finite range), -inf elsewhere: what the accept test takes as the target's.  May be `logits` itself for float32 rows
- *               that lie next to each other; no other output may overlap an input or an output
- * Errors: no output -> MULO_ERR_NULL; vocab > 262144 -> MULO_ERR_UNSUPPORTED; row_stride < vocab -> MULO_ERR_SHAPE. */
+ *   logits_out  device float32 [rows, vocab] (out) or NULL: z / temperature where the entry stays (z with temperature 0; kept
+ *               within float32's finite range), -inf elsewhere: what the accept test takes as the target's.  May be
+ *               `logits` itself for float32 rows that lie next to each other; no other output may overlap an input or an
+ *               output
+ * Errors: no output -> MULO_ERR_NULL; vocab > 262144 or rows >= 2^22 -> MULO_ERR_UNSUPPORTED; row_stride < vocab -> MULO_ERR_SHAPE. */
 MULO_API mulo_status mulo_sample_filtered(void *hip_stream, const mulo_sample_params *p, int32_t rows, int32_t vocab,
                                  int32_t dtype, const void *logits, int64_t row_stride, const float *u,
                                  int32_t *tokens, float *probs, float *logits_out);

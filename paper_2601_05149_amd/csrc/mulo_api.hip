@@ -595,7 +595,9 @@ mulo_status mulo_check_attention(const mulo_attention_args* a) {
     if (!aligned16(a->q) || !aligned16(a->out) || !aligned16(a->k) || !aligned16(a->v) ||
         (prefix && (!aligned16(a->prefix_k) || !aligned16(a->prefix_v))))
         return MULO_ERR_UNSUPPORTED;
-    if ((int64_t)a->B * a->n_heads >= (1 << 30) || (int64_t)a->B * a->n_heads * a->L >= (1 << 30)) return MULO_ERR_UNSUPPORTED;
+    // fewer than 2^32 threads a launch: up to 512 for a workgroup of a (sequence, head), 64 for a joined row
+    const int64_t pairs = (int64_t)a->B * a->n_heads;
+    if (pairs > (1 << 22) || pairs * a->L >= (1 << 26)) return MULO_ERR_UNSUPPORTED;
     return MULO_OK;
 }
 
@@ -646,7 +648,7 @@ mulo_status mulo_sample_filtered(void* hip_stream, const mulo_sample_params* p, 
         !(p->temperature >= 0.0 && p->temperature <= 1e30) || (p->temperature > 0.0 && p->temperature < 1e-30) ||
         !(p->top_p > 0.0 && p->top_p <= 1.0) || !(p->min_p >= 0.0 && p->min_p <= 1.0) || !(p->cfg_scale >= 0.f && p->cfg_scale <= 1.0e6f))
         return MULO_ERR_RANGE;
-    if (vocab > 262144) return MULO_ERR_UNSUPPORTED;
+    if (vocab > 262144 || rows >= 1 << 22) return MULO_ERR_UNSUPPORTED;      // 1024 threads a row, fewer than 2^32 a launch
     if (row_stride < vocab || row_stride > ((int64_t)1 << 40)) return MULO_ERR_SHAPE;
     const size_t e = dtype == MULO_BF16 ? 2 : 4;
     if (((uintptr_t)logits & (e - 1)) || ((uintptr_t)probs & 3) || ((uintptr_t)logits_out & 3)) return MULO_ERR_UNSUPPORTED;

@@ -51,6 +51,8 @@ def attention_args(**changes):
     (UNSUPPORTED, dict(head_dim=32, q_row=64)), (UNSUPPORTED, dict(q_row=68)), (UNSUPPORTED, dict(k_batch=8193)), (UNSUPPORTED, dict(rows=62, P=0)),
     (UNSUPPORTED, dict(prefix_rows=63)), (UNSUPPORTED, dict(q=264)), (UNSUPPORTED, dict(out=8)), (UNSUPPORTED, dict(v=2052)),
     (UNSUPPORTED, dict(prefix_k=4100)), (UNSUPPORTED, dict(k_row=1 << 23)), (UNSUPPORTED, dict(B=1 << 28, n_prefix=1, out_batch=1024)),
+    (UNSUPPORTED, dict(B=1 << 20, n_prefix=1)), (0, dict(B=1 << 19, n_prefix=1)),
+    (UNSUPPORTED, dict(B=1 << 19, L=16, P=0, n_prefix=1, out_batch=8192)), (0, dict(B=1 << 18, L=16, P=0, n_prefix=1, out_batch=8192)),
     (0, dict(dtype=0)), (0, dict(dtype=0, q_row=68)), (UNSUPPORTED, dict(dtype=0, q_row=66)), (0, dict(dtype=0, rows=60, P=0)),
 ], ids=str)
 def test_attention_arguments(lib, status, changes):
@@ -90,6 +92,7 @@ def test_prefix_and_window_need_a_context(lib):
     (RANGE, dict(temperature=1e-31), {}), (RANGE, dict(top_k=-1), {}), (RANGE, dict(top_p=0.0), {}), (RANGE, dict(top_p=1.1), {}),
     (RANGE, dict(top_p=math.nan), {}), (RANGE, dict(min_p=-0.1), {}), (RANGE, dict(min_p=1.5), {}), (RANGE, dict(cfg_scale=-1.0), {}),
     (RANGE, dict(cfg_scale=math.nan), {}), (UNSUPPORTED, {}, dict(vocab=262145, stride=262145)), (SHAPE, {}, dict(stride=99)),
+    (UNSUPPORTED, {}, dict(rows=1 << 22)),
     (SHAPE, {}, dict(stride=1 << 41)), (UNSUPPORTED, {}, dict(logits=258)), (UNSUPPORTED, {}, dict(dtype=1, logits=257)),
     (UNSUPPORTED, {}, dict(probs=1025)), (SHAPE, {}, dict(kept=256, dtype=1)), (SHAPE, {}, dict(kept=256, stride=104)),
     (SHAPE, {}, dict(probs=256)), (SHAPE, {}, dict(probs=1024, kept=1024)),
