@@ -26,7 +26,7 @@ namespace {
 typedef unsigned long long u64;
 constexpr float MOST = 3.402823466e38f;   // the largest finite float32
 constexpr float NEG = -__builtin_huge_valf();
-constexpr int BINS = 1024, CAND = 512;    // bins of a histogram; entries of a bin that are ordered by comparing them all
+constexpr int CAND = 512;                 // entries of a bin that are ordered by comparing them all
 constexpr int DIGIT = 10;                 // bits of a rank that a histogram of them tells apart
 constexpr int LDS_ENTRIES = 32768;        // of a row that is kept in LDS (128 KB)
 constexpr int ONE = 44;                   // bits of the largest weight
@@ -128,6 +128,9 @@ __device__ __forceinline__ float wave_max(float v) {
 template <int NT, bool LDS, int PER>
 __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
     constexpr int NW = NT / 64;
+    // Bins of a histogram.  Long rows, which leave LDS free, have more, so that a bin near their middle holds no more than CAND entries
+    // (150000 normal ones 520 of 1024 bins, and the digits took over: 16 rows 245 us, so 118; 1 row of 131072 103 and 91).
+    constexpr int BINS = LDS ? 1024 : 4096;
     extern __shared__ __attribute__((aligned(16))) float4 kept_row[];      // [NW][runs][64]
     __shared__ __align__(16) u64 hist[BINS];       // then the entries of a bin, and their weights
     __shared__ double table[STEPS];
@@ -430,7 +433,7 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
                     bool here[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) here[e] = in[e] && bin_of(z[e]) == bin && short_rank(z[e], i + e) >> (shift + DIGIT) == known;
-                    add(z, here, [&](int e) { return BINS - 1 - (int)(short_rank(z[e], i + e) >> shift & (BINS - 1)); });
+                    add(z, here, [&](int e) { return BINS - 1 - (int)(short_rank(z[e], i + e) >> shift & ((1 << DIGIT) - 1)); });
                 });
                 __syncthreads();
                 cross(by_mass, front, [&](u64) { return target; });
@@ -442,7 +445,7 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
         }
         take_border();
     };
-    static_assert(BINS == 1 << DIGIT, "a bin for every digit");
+    static_assert(BINS >= 1 << DIGIT && BINS >= 2 * CAND, "a bin for every digit, and room for the entries of one");
     bool cleared = true;
     auto clear_hist = [&]() {
         if (!cleared) {
