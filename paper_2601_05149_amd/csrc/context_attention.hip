@@ -10,12 +10,26 @@
 // are already laid out as the second operand of the second product.  Tiles of K and V^T go from memory to LDS directly,
 // double buffered, and are shared by the wavefronts of a workgroup.
 //
-// What a workgroup's queries are (`role`):
-//   whole   one sequence; its tiles are those of its prefix that it sees, then its own
+// What a workgroup's queries are (make_plan chooses, with both sides measured):
+//   few     32 queries over few keys, all wavefronts with the same queries and tiles of keys of their own, joined in LDS: one launch
 //   stacked few queries per sequence behind a shared prefix: the rows of all sequences of a group go over the prefix
 //           together (prefix workgroups), each sequence's over its own rows (own workgroups, the same launch), and
 //           k_context_join joins the partial results.  The prefix is read once per 128 stacked rows.
-// Keys of few queries are dealt to several workgroups as well, whose shares k_context_join joins.
+//   whole   128 or 256 queries of one sequence; its tiles are those of its prefix that it sees, then its own.  Keys of few
+//           queries are dealt to several workgroups, whose shares k_context_join joins.
+//
+// bf16: the exponentials are rounded for the second product, whose matrix instruction takes bf16 (half a step of 2^-8 each, of either
+// sign, of positive terms; their sum l is taken of what was not rounded); scores, m, l, o and every partial result are float32.
+//
+// What bounds it, heads of 128, 32 of them, on a card that copies 5.05 TB/s and multiplies 8192^3 bf16 at 1.25 PFLOP/s:
+//   single tokens over thousands of rows: memory.  64 tokens, two prefixes of 2048 rows and 900 own rows 199 us, 5.1 TB/s; 32 through a
+//   window of 2048 with 128 sinks 196 us, 5.8 TB/s
+//   long blocks: the matrix instruction and the softmax's vector instructions one after the other at a clock that falls under the load
+//   (4 x 1024 queries, 1024 shared and 2048 own rows 247 us, 975 TFLOP/s, matrix pipes busy 45 %; through a window of 1024 with 128
+//   sinks 106 to 112 us, 700 TFLOP/s, 38 %: a fifth of the scores it computes are those of tiles that a window cuts)
+//   16 x 16 queries, 330 own and 4224 shared rows 52.6 us, 364 TFLOP/s: 42 in k_context, where the own rows' workgroups have one
+//   wavefront of four at work, and 25 MB of partial results each way
+//   everything smaller: launches and one chain of latencies (a tile some 1.2 us; one launch 5 to 9 us, two 9 to 14)
 #include <hip/hip_bf16.h>
 
 #include <utility>
@@ -701,7 +715,10 @@ Plan make_plan(const ContextAttn& a, int esz, int64_t part_floats) {
     p.n = p.by_kv ? group * a.L : a.L;
     p.tiles = (p.n + 127) / 128;
     p.split = 1;
-    const int TARGET = 512;           // workgroups: two per CU
+    // Workgroups that run at a time, two per CU, and to how many keys are dealt.  us, 256 / 512 / 1024, heads of 128: 8 tokens, 100 own and
+    // 1000 shared rows 15.8 / 14.9 / 19.4, 16 x 16 of 330 and 4224 74 / 58 / 70, 1 token of 4000 rows 23.3 / 20.7 / 25.5, 1 x 64 of
+    // 4000 27.4 / 29.9 / 38; 8 tokens of 16 heads of 64, 100 and 4000 15.5 / 13.9 / 15.0; float32 6 x 5 of 300 and 333 16.4 / 14.3 / 14.4.
+    const int TARGET = 512;
     const int64_t base = (int64_t)a.B * p.heads * p.tiles;
     const int n_own = own_tiles(a, bkv), n_pre = prefix_tiles(a, bkv);
     // One launch instead of two, as long as every (sequence, key head) has its place on a CU (128 KB of LDS; heads of 64 half) and

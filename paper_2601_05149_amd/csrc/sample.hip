@@ -12,7 +12,7 @@
 // border or a draw where sums in 64-bit floating point place it.
 //
 // What bounds it: one row, the chain of its passes and barriers (16384 entries, top-k 2000: 26 thousand cycles, 11.7 us, of which
-// the launch is 5; 32 guided rows 16.1); many rows, vector instructions: 61 an entry, the vector pipes busy 87 % (2048 rows of 16384,
+// the launch is 5; 32 guided rows 16.1); many rows, vector instructions: 60 an entry, the vector pipes busy 72 % (2048 rows of 16384,
 // top-p and min-p, logits out: 81 us, 3.3 TB/s of the 5.05 that a copy reaches).
 #include <hip/hip_bf16.h>
 
@@ -128,8 +128,9 @@ __device__ __forceinline__ float wave_max(float v) {
 template <int NT, bool LDS, int PER>
 __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
     constexpr int NW = NT / 64;
-    // Bins of a histogram.  Long rows, which leave LDS free, have more, so that a bin near their middle holds no more than CAND entries
-    // (150000 normal ones 520 of 1024 bins, and the digits took over: 16 rows 245 us, so 118; 1 row of 131072 103 and 91).
+    // Bins of a histogram.  Long rows, which leave LDS free, have more, so that a bin near their middle holds no more than CAND entries:
+    // of 150000 normal ones 520 fell into one of 1024 bins, and the digits took over (16 rows 245 us, with 4096 bins 118; 1 row of
+    // 131072 103 and 91).
     constexpr int BINS = LDS ? 1024 : 4096;
     extern __shared__ __attribute__((aligned(16))) float4 kept_row[];      // [NW][runs][64]
     __shared__ __align__(16) u64 hist[BINS];       // then the entries of a bin, and their weights
