@@ -50,7 +50,8 @@ def oracle(m, w, cos, sin, B, rows, round_bf16, sinks=0, window=0):
 
 @pytest.mark.parametrize("name, B, groups, S, sinks, window, copy", [
     ("tiny", 3, 1, 33, 0, 0, False), ("tiny", 4, 2, 50, 10, 37, False), ("small", 4, 2, 77, 0, 0, False), ("small", 3, 1, 40, 5, 30, False),
-    ("wide", 6, 1, 64, 0, 0, True), ("wide", 2, 2, 65, 70, 20, False)])
+    ("wide", 6, 1, 64, 0, 0, True), ("wide", 2, 2, 65, 70, 20, False),
+    ("wide", 16, 2, 1300, 0, 0, False), ("wide", 16, 1, 1300, 900, 1200, False)])      # long enough for the sequences to be stacked over it
 def test_forward_behind_a_shared_prefix(name, B, groups, S, sinks, window, copy):
     """Blocks and single tokens behind a shared prefix: what a decoder computes whose every sequence begins with the prefix."""
     m = MODELS[name]
@@ -117,12 +118,13 @@ def test_detached_and_without_a_window_nothing_is_left():
     assert np.array_equal(back, forward(plain, mulo.alloc_kv(plain, DEV), toks, 0)) and not np.array_equal(back, seen)
 
 
-def test_resampling_behind_a_prefix():
+@pytest.mark.parametrize("B, S", [(3, 41), (24, 1300)])
+def test_resampling_behind_a_prefix(B, S):
     """One pass over scattered islands, and single tokens in order, behind an attached prefix: the logits of a context whose
     sequences hold the prefix themselves (one layer: the same inputs up to the attention, whose sums are the same terms)."""
     m = WIDE
     w = G.make_weights(m, seed=0)
-    B, S, H, W = 3, 41, 4, 8
+    H, W = 4, 8
     L = H * W
     prefix = G.uniform_tokens((1, S), m["vocab"], 0, tag=0)
     toks, prev = G.uniform_tokens((B, L), m["vocab"], 1, tag=0), G.uniform_tokens((B,), m["vocab"], 2, tag=0)
@@ -130,9 +132,10 @@ def test_resampling_behind_a_prefix():
     mask[0, [3, 17, 30]] = 1
     mask[1, [9]] = 1
     mask[2, [0, 21]] = 1
+    mask[3:, [2, 28]] = 1
     ctx, kv, cos, sin, _ = with_prefix(m, w, prefix, B, L, L)
     rows = (S + L + 7) // 8 * 8
-    full, _, _ = make_ctx(m, w, B, rows, 48)
+    full, _, _ = make_ctx(m, w, B, rows, (S + 3) // 4 * 4 + 4)
     kvf = mulo.alloc_kv(full, DEV)
     forward(full, kvf, np.repeat(prefix, B, 0), 0)
     for window in (0, 20):
