@@ -125,7 +125,11 @@ __device__ __forceinline__ float wave_max(float v) {
 // (masses, top-p, the draw's sums, what is written of them) goes by the list: of 16384 entries 2000 cost an eighth (a row of 16384,
 // 512 threads, top-p 0.9 alone 19.6 us, behind top-k 200 13.6).  With 512 threads two entries a thread would take 8 KB
 // that the second row of a CU needs.
-template <int NT, bool LDS, int PER>
+// KIND: ANY_ROWS, or what the rows are (1: bf16, 2: guided), for the form that reads them in every pass: each pass holds the loads of its
+// kind alone (of all kinds the code took 152 KB, more than the instruction cache by far; now 97 to 112.
+// 1 row of 33000 28.4 and 25.8 us, 16 of 131072 56 and 53, bf16 59.5 and 55.3, guided 66 and 62.5).
+constexpr int ANY_ROWS = -1;
+template <int NT, bool LDS, int PER, int KIND>
 __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
     constexpr int NW = NT / 64;
     // Bins of a histogram.  Long rows, which leave LDS free, have more, so that a bin near their middle holds no more than CAND entries:
@@ -149,10 +153,10 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
     const int w_first = wave * runs * 256, w_runs = V - w_first <= 0 ? 0 : (V - w_first + 255) / 256 < runs ? (V - w_first + 255) / 256 : runs;
     const int first = w_first + lane * 4;
     float4* const mine = kept_row + wave * runs * 64 + lane;
-    const bool bf16 = a.dtype == 1;
+    const bool bf16 = KIND == ANY_ROWS ? a.dtype == 1 : KIND & 1, guided = KIND == ANY_ROWS ? a.logits_u != nullptr : KIND & 2;
     const size_t esz = bf16 ? 2 : 4;
     const char* const zc = (const char*)a.logits + r * a.row_stride * esz;
-    const char* const zu = a.logits_u ? (const char*)a.logits_u + r * a.row_stride * esz : nullptr;
+    const char* const zu = (const char*)a.logits_u + (guided ? r * a.row_stride * esz : 0);
     // Four entries an access, wherever the row begins (global memory takes vectors at any alignment of their elements).  Four
     // runs that lie in the row as a whole take one address; else an access that would pass the end moves back to it, and what it
     // then holds too early is shifted out.
@@ -177,7 +181,7 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
                     v[j] = make_float4(t.v[0], t.v[1], t.v[2], t.v[3]);
                 }
             }
-        } else if (V >= 4) {
+        } else if (!LDS || V >= 4) {
             int at[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) at[j] = i + j * 256 < V - 4 ? i + j * 256 : V - 4;
@@ -215,7 +219,7 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
         for (int j0 = 0; j0 < w_runs; j0 += 4) {
             float4 c[4];
             four_runs(zc, first + j0 * 256, c);
-            if (zu) {
+            if (guided) {
                 float4 u[4];
                 four_runs(zu, first + j0 * 256, u);
                 auto guide = [&](float x, float y) {
@@ -615,11 +619,11 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
     }
 }
 
-template <int NT, bool LDS, int PER>
+template <int NT, bool LDS, int PER, int KIND = ANY_ROWS>
 void run(const SampleArgs& a, hipStream_t st) {
     const int runs = (a.V + NT * 4 - 1) / (NT * 4);
     const int lds = LDS ? runs * NT * (int)sizeof(float4) : 0;
-    auto kern = k_sample<NT, LDS, PER>;
+    auto kern = k_sample<NT, LDS, PER, KIND>;
     if constexpr (LDS) {
         static int attr_state[MAX_DEVICES] = {};
         if (!ensure_dynamic_lds_here(reinterpret_cast<const void*>(kern), LDS_ENTRIES * 4, attr_state)) return;
@@ -642,7 +646,12 @@ void launch_sample_filtered(const SampleArgs& args, hipStream_t st) {
     if (a.V <= (many ? 4096 : 2048)) run<256, true, 2>(a, st);
     else if (many && a.V <= LDS_ENTRIES / 2) run<512, true, 1>(a, st);
     else if (a.V <= LDS_ENTRIES) run<1024, true, 2>(a, st);
-    else run<1024, false, 2>(a, st);
+    else switch ((a.dtype == 1 ? 1 : 0) + (a.logits_u ? 2 : 0)) {
+        case 0: run<1024, false, 2, 0>(a, st); break;
+        case 1: run<1024, false, 2, 1>(a, st); break;
+        case 2: run<1024, false, 2, 2>(a, st); break;
+        default: run<1024, false, 2, 3>(a, st);
+    }
 }
 
 }  // namespace mulo

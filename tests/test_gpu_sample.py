@@ -77,6 +77,15 @@ def test_more_rows_than_compute_units(V):
         check(z[-2:], u[-2:].contiguous(), **kw)
 
 
+@pytest.mark.parametrize("dtype, cfg", [(torch.bfloat16, 0.0), (torch.float32, 3.0), (torch.bfloat16, 1.7)])
+def test_large_vocabularies_of_every_kind(dtype, cfg):
+    for V in (32769, 60001):
+        z, u = rows_of(4, V, seed=V, spread=2.0, dtype=dtype)
+        u = u[:2].contiguous() if cfg else u
+        for kw in (dict(top_k=300, top_p=0.9), dict(temperature=0.7, top_p=0.95, min_p=1e-3), dict(top_k=5000), dict(temperature=0.0)):
+            check(z, u, cfg_scale=cfg, **kw)
+
+
 @pytest.mark.parametrize("V", [70000, 131072, 262144])
 def test_large_vocabularies(V):
     z, u = rows_of(2, V, seed=V, spread=3.0)
