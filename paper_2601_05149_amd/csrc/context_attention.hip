@@ -764,7 +764,7 @@ Plan make_plan(const ContextAttn& a, int esz, int64_t part_floats) {
             const int s = clamp_int((n_own + per - 1) / per, 1, MAX_SLOTS / 2), ps = clamp_int((n_pre + per - 1) / per, 1, MAX_SLOTS - s);
             const int64_t t = makespan(pbase * ps, (n_pre + ps - 1) / ps * prefix_cost, base * s, (n_own + s - 1) / s * own_cost, TARGET);
             if (t <= best) best = t, p.split = s, p.prefix_split = ps;
-            if (s == 1 && ps == 1) break;
+            if ((s == 1 && ps == 1) || per > best) break;      // some workgroup has more than half of `per` tiles, 2 each: no shorter one follows
         }
         const int64_t whole = (base * whole_split + TARGET - 1) / TARGET * ((n + whole_split - 1) / whole_split) * own_cost;
         const int more = p.split + p.prefix_split - (whole_split > 1 ? whole_split : 0);
