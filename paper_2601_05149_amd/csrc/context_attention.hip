@@ -598,17 +598,19 @@ __global__ __launch_bounds__(NTH, !FEW && DH * BKV * (int)sizeof(T) <= 16384 ? 2
         if (lh == 0) *reinterpret_cast<float2*>(a.ml + 2 * (slot * all_rows + out_row)) = make_float2(m_run, l_run);
         return;
     }
-    const float inv = active && l_run > 0.f ? 1.0f / l_run : 0.f;
+    const float inv = l_run > 0.f ? 1.0f / l_run : 0.f;
+    auto done = [&](float x) { return active ? x * inv : 0.f; };      // an unused slot's query may hold anything
 #pragma unroll
     for (int i = 0; i < NDB; ++i)
 #pragma unroll
         for (int g4 = 0; g4 < 4; ++g4)
-            store_out(i, g4, f32x4{o[i][g4 * 4] * inv, o[i][g4 * 4 + 1] * inv, o[i][g4 * 4 + 2] * inv, o[i][g4 * 4 + 3] * inv});
+            store_out(i, g4, f32x4{done(o[i][g4 * 4]), done(o[i][g4 * 4 + 1]), done(o[i][g4 * 4 + 2]), done(o[i][g4 * 4 + 3])});
 }
 
 // A wavefront joins the shares of a query: lane s takes the weight of share s, then every lane DH / 64 channels of all of them.
 // One memory round trip: the outputs of NS shares (those there are not re-read the first) are requested together with the weights.
-// Rows of absent sequences and unused slots are zeros.
+// Rows of absent sequences and unused slots are zeros, whatever the shares hold: workgroups of the prefix have gone over their
+// queries as well, which may be infinite or NaN.
 constexpr int JOIN_WAVES = 4;
 template <class T, int DH, int NS>
 __global__ __launch_bounds__(64 * JOIN_WAVES) void k_context_join(const Args a, int slots) {
@@ -649,11 +651,11 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void k_context_join(const Args a, 
         if (s0 >= slots) break;
         request(s0);
     }
-    const float inv = !absent && den > 0.f ? 1.0f / den : 0.f;
+    const float inv = den > 0.f ? 1.0f / den : 0.f;
     T* const op = reinterpret_cast<T*>(a.out) + (a.frag ? frag_index(b * a.L + j, h * DH + lane * C, a.nh * DH)
                                                         : (int64_t)b * a.out_batch + h * a.out_head + j * a.out_row + lane * C);
 #pragma unroll
-    for (int c = 0; c < C; ++c) op[c] = (T)(acc[c] * inv);
+    for (int c = 0; c < C; ++c) op[c] = (T)(absent ? 0.f : acc[c] * inv);
 }
 template <class T, int DH>
 void join(const Args& a, int slots, hipStream_t st) {

@@ -238,6 +238,35 @@ def test_dealt_keys_and_many_queries(case):
         check(c, out, "%d of %d results of a query" % (n // least, asked // least), reference=reference)
 
 
+ABSENT = [c for c in CASES + DEALT if any(p < 0 for p in c[7].get("starts", ()))] + [
+    # every row over the prefix together: 16 sequences, half of them absent
+    ("bf16", 16, 2, 8, 8, 64, 100, dict(S=4000, starts=[100, -1] * 8)),
+]
+
+
+@pytest.mark.parametrize("case", ABSENT, ids=name_of)
+def test_absent_sequences_are_zeros_whatever_their_queries_hold(case):
+    """A slot without a sequence may hold infinities, NaN, or numbers whose scores overflow: its outputs are zeros, and those of the
+    other sequences have the bits they have beside a slot of ordinary numbers."""
+    dtype, B, L, nh, nkv, dh, P, kw = case
+    c = make(dtype, B, L, nh, nkv, dh, P, **kw)
+    d = on_device(c)
+    absent = torch.tensor([p < 0 for p in c["starts"]])
+    ask = mulo.mulo_attention_workspace_bytes(plan_of(c, d, torch.empty_like(d["q"])))
+    for share in (1.0, 0.0):
+        ws = torch.full((int(ask * share),), 0xFF, dtype=torch.uint8, device=DEV) if int(ask * share) else None
+        want = torch.full_like(d["q"], NAN)
+        mulo.mulo_attention(plan_of(c, d, want), ws)
+        for bad in (float("inf"), float("-inf"), NAN, torch.finfo(DT[dtype]).max):
+            q = d["q"].clone()
+            q[absent.to(DEV)] = bad
+            out = torch.full_like(q, NAN)
+            mulo.mulo_attention(plan_of(c, dict(d, q=q), out), ws)
+            torch.cuda.synchronize()
+            assert (out[absent.to(DEV)] == 0).all(), "queries of %s, scratch %s" % (bad, ws is not None)
+            assert torch.equal(out, want), "queries of %s, scratch %s" % (bad, ws is not None)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_sharp_and_scaled_scores(dtype):
     """Scores of a hundred and more: nearly all of the mass on one key; and a scale of the caller's."""
