@@ -304,7 +304,13 @@ __global__ __launch_bounds__(NT) void k_sample(const SampleArgs a, int runs) {
     const bool none = hi == NEG;
     const float top = hi;
     const double per_z = a.temperature * 0.6931471805599453;
-    auto at_least = [&](double bits) { return (float)fmax((double)top - bits * per_z, -(double)MOST); };
+    // the least float32 that is at most `bits` below the maximum.  (A conversion alone may step below: where a step is hundreds
+    // of bits, part() would move the exponent of an entry there by more than there is.)
+    auto at_least = [&](double bits) {
+        const double limit = fmax((double)top - bits * per_z, -(double)MOST);
+        const float z = (float)limit;
+        return (double)z < limit ? of_key(key_of(z) + 1) : z;
+    };
     const Weights w{(double)top, greedy ? 0.0 : STEPS * 1.4426950408889634 / a.temperature, at_least(900.0), at_least(ONE + 2.0), table};
     // the border, so far: entries above b_z stay, and those at it up to index b_i
     float b_z = NEG;

@@ -209,6 +209,21 @@ def test_skewed_values():
         check(z, u, **kw)
 
 
+@pytest.mark.parametrize("top", [0.75, 1.5, 10.0, 100.0, 10000.0, -10.0])
+@pytest.mark.parametrize("T", [1e-6, 1e-8, 1e-9, 1e-10, 1e-20, 1e-30])
+def test_small_temperatures(top, T):
+    """Steps of float32 that are hundreds of bits and more: the entry a step below the largest weighs nothing, whichever way
+    a limit between the two would be rounded."""
+    z = torch.full((1, 300), top)
+    for i in range(1, 300):
+        z[0, i] = torch.nextafter(z[0, i - 1], torch.tensor(-INF)) if i % 3 else z[0, i - 1]
+    order = torch.randperm(300, generator=torch.Generator().manual_seed(12))
+    z = torch.cat([z, z[:, order], z.flip(1)]).to(DEV)
+    u = torch.tensor([0.0, 0.6, 0.9], device=DEV)
+    for kw in (dict(), dict(top_k=5), dict(top_k=250), dict(top_p=0.9), dict(min_p=1e-3), dict(top_k=7, top_p=0.5)):
+        check(z, u, temperature=T, **kw)
+
+
 def test_distribution_of_draws():
     """Uniforms on a grid land on every entry in proportion to its probability."""
     z, _ = rows_of(1, 50, seed=9)
