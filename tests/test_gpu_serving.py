@@ -7,7 +7,7 @@ import paper_2601_05149_amd as mulo
 from oracle import decoder as OD
 from oracle import sampling as OS
 from oracle import step as ST
-from tests.gpu_util import DEV, check_bf16_logits, decide_buffers, make_ctx, say
+from tests.gpu_util import DEV, check_bf16_logits, compare_decisions, decide_buffers, make_ctx, say, to_np
 from workloads import generators as G
 
 pytestmark = pytest.mark.gpu
@@ -158,6 +158,101 @@ def test_resampling_behind_a_prefix(B, S):
             assert np.abs(b).max() > 0.1
             say("  window %d, %s: %.3g" % (window, what, np.abs(a - b).max()))
             assert np.abs(a - b).max() <= 2e-2
+
+
+@pytest.mark.parametrize("name, B, S, sinks, window, cfg_scale", [
+    ("tiny", 2, 33, 0, 0, 0.0), ("tiny", 2, 50, 10, 37, 4.0), ("small", 3, 77, 0, 0, 0.0), ("small", 2, 40, 5, 30, 4.0),
+    ("wide", 4, 65, 70, 20, 0.0), ("wide", 2, 300, 0, 0, 4.0)])
+def test_verification_step_behind_a_prefix_and_through_a_window(name, B, S, sinks, window, cfg_scale):
+    """A whole step, plain and guided (the prompt and the empty prompt as two prefixes), in front of 8 committed rows: the logits of a
+    decoder whose every sequence begins with its prefix, the bits of its stages called one by one, and the decisions of the oracle on
+    those logits."""
+    m = MODELS[name]
+    w = G.make_weights(m, seed=0)
+    H, W, r, V, P = 16, 8, 2, m["vocab"], 8
+    L, n_lo = H * W, H * W // 4
+    Bz, groups = (2 * B, 2) if cfg_scale else (B, 1)
+    prefix = G.uniform_tokens((groups, S), V, 0, tag=0)
+    ctx, kv, cos, sin, _ = with_prefix(m, w, prefix, Bz, P + L, L)
+    mulo.mulo_set_window(ctx, sinks, window)
+    before = np.concatenate([G.uniform_tokens((B, P), V, 0, tag=1)] * (Bz // B))
+    forward(ctx, kv, before, 0)
+    dl = G.normal_logits((B, n_lo, V), 1.0, 0, tag=2)
+    dt, prev = dev(G.sample_categorical(dl, 0, tag=2)), dev(before[:B, -1])
+    dl = dev(dl)
+    p = mulo.make_params(H, W, 0, L, 1, seed=3, rng_counter=4, cfg_scale=cfg_scale)
+    i32 = lambda *shape: torch.empty(*shape, dtype=torch.int32, device=DEV)
+    out, toks, z = decide_buffers(B, L), i32(B, L), torch.empty(Bz, L, V, device=DEV)
+    mulo.mulo_verify_step(ctx, kv, B, P, p, H // r, W // r, r, dl, 0, dt, prev, out["tokens_out"], out["accept"], out["mask"], out["t0"],
+                          out["stats"], toks, z)
+    toks2, q, q_row, z2, out2 = i32(B, L), torch.empty(B, n_lo, V, device=DEV), i32(L), torch.empty(Bz, L, V, device=DEV), decide_buffers(B, L)
+    mulo.mulo_upsample_draft(ctx, B, H // r, W // r, r, dl, 0, dt, toks2, q, q_row, None)
+    rows = torch.cat([torch.cat([prev[:, None], toks2[:, :-1]], 1)] * (Bz // B))
+    mulo.mulo_verify_forward(ctx, kv, Bz, L, P, rows, None, z2)
+    mulo.mulo_accept_local_resample(ctx, B, p, z2, q, q_row, n_lo * V, toks2, **out2)
+    torch.cuda.synchronize()
+    assert torch.equal(z, z2) and torch.equal(toks, toks2)
+    for k in out:
+        assert torch.equal(out[k], out2[k]), k
+    bf16 = m["dtype"] == "bf16"
+    want = []
+    for rounded in ((True, False) if bf16 else (False,)):
+        d = oracle(m, w, cos, sin, Bz, S + P + L, rounded)
+        d.forward(np.repeat(prefix, Bz // groups, 0), 0)
+        d.sinks, d.window = sinks, window
+        d.forward(before, S)
+        want.append(d.forward(rows.cpu().numpy(), S + P).numpy())
+    zh = z.cpu().numpy()
+    if bf16:
+        check_bf16_logits("step, %s" % name, zh, *want)
+    else:
+        say("  step, %s: %.3g" % (name, np.abs(zh - want[0]).max()))
+        assert np.abs(zh - want[0]).max() <= 1e-4
+    guided = dict(logits_uncond=zh[B:], cfg_scale=cfg_scale) if cfg_scale else {}
+    ref = ST.decide(zh[:B], q.cpu().numpy(), q_row.cpu().numpy(), toks.cpu().numpy(), W=W, n0=0, radius=1, seed=3, rng_counter=4, **guided)
+    say("  %r" % compare_decisions(to_np(out), ref, toks.cpu().numpy(), q.cpu().numpy(), q_row.cpu().numpy(), label="step"))
+    assert 0 < ref["accept"].sum() < B * L
+
+
+def test_a_step_behind_a_prefix_recorded_and_replayed():
+    """One graph of a step behind a shared prefix and through a window, replayed over other drafts: the bits of an ordinary call."""
+    m = SMALL
+    w = G.make_weights(m, seed=0)
+    B, S, H, W, r, V, P = 8, 600, 8, 8, 2, m["vocab"], 8
+    L, n_lo = H * W, H * W // 4
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        ctx, kv, _, _, cp = with_prefix(m, w, G.uniform_tokens((1, S), V, 0, tag=0), B, P + L, L)
+        mulo.mulo_set_window(ctx, 5, 400)
+        before = G.uniform_tokens((B, P), V, 0, tag=1)
+        forward(ctx, kv, before, 0)
+        prev, dl, dt = dev(before[:, -1]), torch.zeros(B, n_lo, V, device=DEV), torch.zeros(B, n_lo, dtype=torch.int32, device=DEV)
+        out, z = decide_buffers(B, L), torch.empty(B, L, V, device=DEV)
+        p = mulo.make_params(H, W, 0, L, 1, seed=3, rng_counter=4)
+
+        def step():
+            mulo.mulo_verify_step(ctx, kv, B, P, p, H // r, W // r, r, dl, 0, dt, prev, logits=z, **out)
+
+        step()
+        side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    with torch.cuda.stream(side):
+        for tag in (2, 3, 4):
+            drawn = G.normal_logits((B, n_lo, V), 1.0, 0, tag=tag)
+            dl.copy_(torch.tensor(drawn))
+            dt.copy_(torch.tensor(G.sample_categorical(drawn, 0, tag=tag)))
+            got = []
+            for run in (graph.replay, step):
+                for t in list(out.values()) + [z]:
+                    t.fill_(77)
+                run()
+                side.synchronize()
+                got.append([t.clone() for t in list(out.values()) + [z]])
+            assert all(torch.equal(a, b) for a, b in zip(*got))
+            assert 0 < int(out["accept"].sum()) < B * L
+    del graph
 
 
 def test_groups_have_to_divide_the_batch():
