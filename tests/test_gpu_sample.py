@@ -86,6 +86,67 @@ def test_large_vocabularies_of_every_kind(dtype, cfg):
             check(z, u, cfg_scale=cfg, **kw)
 
 
+@pytest.mark.parametrize("V", [32765, 32768])
+def test_the_longest_rows_that_are_kept_in_lds(V):
+    """One row, and more rows than compute units, at the most LDS a workgroup takes."""
+    z, u = rows_of(3, V, seed=V, spread=2.0)
+    for kw in (dict(), dict(top_k=2048, top_p=0.9), dict(temperature=0.8, top_p=0.95, min_p=1e-3), dict(top_k=2049)):
+        check(z, u, **kw)
+    R = torch.cuda.get_device_properties(0).multi_processor_count + 3
+    z, u = rows_of(R, V, seed=V + 1, spread=2.0)
+    every = run(z, u, top_k=900, top_p=0.9)
+    for a, b in ((0, 2), (R - 2, R)):
+        for x, y in zip(every, run(z[a:b], u[a:b].contiguous(), top_k=900, top_p=0.9)):
+            assert np.array_equal(x[a:b].view(np.int32), y.view(np.int32))
+
+
+LONG = 40001       # a row that is read again in every pass
+
+
+@pytest.mark.parametrize("dtype, cfg", [(torch.float32, 0.0), (torch.bfloat16, 0.0), (torch.float32, 2.0), (torch.bfloat16, 2.0)])
+def test_long_rows_with_ties(dtype, cfg):
+    """Some 10000 entries of each value, all of them alike, and zeros of both signs: borders inside a tie, with more entries than the
+    list holds in front of them and with fewer."""
+    g = torch.Generator().manual_seed(31)
+    z = torch.randint(0, 4, (3, LONG), generator=g).float()
+    z[1] = 0.0
+    z[2, 100:] = -0.0
+    z[2, :100] = 0.0
+    if cfg:      # the guided row is z_u + 2 (z_c - z_u): of twins that are alike, themselves
+        z = torch.cat([z, z])
+    z, u = z.to(dtype).to(DEV), torch.rand(3, generator=g).to(DEV)
+    for kw in (dict(top_k=1), dict(top_k=2000), dict(top_k=2049), dict(top_k=11000), dict(top_p=0.3), dict(top_p=0.7, top_k=30000),
+               dict(top_k=2048, top_p=0.5), dict(temperature=0.0), dict(min_p=0.2, top_p=0.99)):
+        check(z, u, cfg_scale=cfg, **kw)
+
+
+def test_long_rows_with_masks_and_infinities():
+    z, u = rows_of(7, LONG, seed=33)
+    z[0] = -INF
+    z[1, 1:] = -INF
+    z[2, 5:] = float("nan")
+    z[3, 100:39000] = torch.finfo(torch.float32).min
+    z[4, ::2] = -INF
+    z[5, [7, 20001, LONG - 1]] = INF
+    z[6, 3:] = -3.0e38
+    for kw in (dict(), dict(top_k=20), dict(top_k=3000), dict(top_p=0.6), dict(min_p=0.2), dict(top_k=300, top_p=0.9, min_p=0.01), dict(temperature=0.0)):
+        tokens = check(z, u, **kw)
+        assert tokens[0] == -1 and tokens[1] == 0 and tokens[5] in (7, 20001, LONG - 1)
+
+
+@pytest.mark.parametrize("cfg", [0.0, 4.0])
+def test_long_rows_in_place(cfg):
+    """The filtered logits in the place of the logits, which every pass reads again."""
+    z, u = rows_of(4, LONG, seed=34)
+    u = u[:2].contiguous() if cfg else u
+    for kw in (dict(top_k=300, top_p=0.9), dict(top_k=2048), dict(temperature=0.7, top_k=5000), dict(temperature=0.8, top_p=0.9, min_p=1e-3), dict()):
+        want = run(z, u, cfg_scale=cfg, **kw)
+        again = z.clone()
+        got = run(again, u, in_place=True, cfg_scale=cfg, **kw)
+        assert all(np.array_equal(a, b) for a, b in zip(want, got))
+        assert torch.equal(again[len(u):], z[len(u):])                     # the twins stay as they were
+
+
 @pytest.mark.parametrize("V", [70000, 131072, 262144])
 def test_large_vocabularies(V):
     z, u = rows_of(2, V, seed=V, spread=3.0)
