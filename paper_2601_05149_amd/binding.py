@@ -369,7 +369,7 @@ def mulo_attach_prefix(ctx, kv=None, length=0, rope_cos=None, rope_sin=None, n_p
     n, rows = k.shape[1], k.shape[3]
     if k.shape != (c.n_layers, n, c.n_heads, rows, c.head_dim) or v.shape != (c.n_layers, n, c.n_heads, c.head_dim, rows):
         raise ValueError("the prefix is not a cache of this model")
-    if any(t.shape != (c.max_seq, c.head_dim // 2) for t in (rope_cos, rope_sin)):
+    if any(t is None or t.shape != (c.max_seq, c.head_dim // 2) for t in (rope_cos, rope_sin)):
         raise ValueError("the rotary tables of the prefix have a row for every cache row of the context")
     p = Prefix(KV(_ptr(k, ctx.tdtype), _ptr(v, ctx.tdtype)), n if n_prefix is None else n_prefix, n, rows, length,
                _ptr(rope_cos, torch.float32), _ptr(rope_sin, torch.float32))

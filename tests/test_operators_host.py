@@ -115,6 +115,16 @@ def test_binding_refuses_what_does_not_fit():
         mulo.mulo_sample_filtered(mulo.make_sample_params(), torch.zeros(2, 3, dtype=torch.float16))
 
 
+def test_a_prefix_without_its_rotary_tables_is_refused():
+    ctx = mulo.Ctx(None, mulo.make_cfg(dict(n_layers=1, d_model=128, n_heads=2, head_dim=64, d_ffn=128, vocab=64, dtype="bf16"), 2, 16, 8), [])
+    k, v, table = torch.zeros(1, 1, 2, 24, 64).bfloat16(), torch.zeros(1, 1, 2, 64, 24).bfloat16(), torch.zeros(16, 32)
+    for tables in ((None, None), (table, None), (None, table)):
+        with pytest.raises(ValueError):
+            mulo.mulo_attach_prefix(ctx, (k, v), 20, *tables)
+    with pytest.raises(ValueError):
+        mulo.mulo_attach_prefix(ctx, (k, v), 20, table, table)            # not on a GPU
+
+
 # ---- the oracle --------------------------------------------------------------------------------------------------------
 def test_oracle_attention_is_causal_softmax_attention():
     g = torch.Generator().manual_seed(0)
