@@ -339,7 +339,8 @@ MULO_API mulo_status mulo_resample_islands(mulo_ctx *ctx, mulo_kv *kv, int32_t B
  *   sinks, window   window == 0: every earlier key is seen, and sinks is not read
  *   scale        0: 1 / sqrt(head_dim); at most 1e6
  * Rows that no query of the call sees may hold anything, NaN included; what some query sees has to be finite.  q and out must
- * not overlap.
+ * not overlap.  A prefix is read once for several sequences unless it comes with a window and with P_seq: then each reads it for
+ * itself.
  * Limits: head_dim 64 or 128; n_heads a multiple of n_kv_heads, B of n_prefix; rows, prefix_rows and every stride a multiple
  * of 16 bytes, pointers 16-byte aligned; rows, prefix_rows <= 2^24, k rows at most 2^22 and v channels 2^26 elements apart;
  * B * n_heads <= 2^22, B * n_heads * L < 2^26. */
@@ -371,7 +372,7 @@ MULO_API uint64_t mulo_attention_workspace_bytes(const mulo_attention_args *a);
  * stream work has finished (calls that may overlap need one each, and so do graphs that may replay at the same time), or
  * NULL; with fewer bytes than mulo_attention_workspace_bytes says the keys are dealt to fewer workgroups.  The
  * number of shares follows from the sizes alone, so equal calls give equal bits.  (A recorded call needs an ordinary one of the
- * same sizes before it, as the compute entry points of a context do.)
+ * same sizes and workspace before it, as the compute entry points of a context do.)
  * Errors: as mulo_check_attention; a workspace that is not 16-byte aligned -> MULO_ERR_UNSUPPORTED. */
 MULO_API mulo_status mulo_attention(void *hip_stream, const mulo_attention_args *a, void *workspace, uint64_t workspace_bytes);
 
@@ -392,7 +393,8 @@ typedef struct {
 /* From the next call on every forward pass of the context (mulo_verify_forward, mulo_verify_step, mulo_resample_sequential,
  * mulo_resample_islands) attends to the attached prefix in front of its cache rows, as mulo_attention does: P counts the
  * context's own rows, and its cache row i is position len + i.  The struct is copied; the memory must stay valid and unchanged
- * while attached.  NULL detaches.  A call whose number of sequences (2 B with guidance) is not a multiple of
+ * while attached.  NULL detaches.  (A MULO_F32 context has no scratch for partial results: there every sequence reads the prefix
+ * for itself.)  A call whose number of sequences (2 B with guidance) is not a multiple of
  * n_prefix is MULO_ERR_SHAPE.
  * Errors: head_dim other than 64 or 128, or rows (or the context's max_seq) not a multiple of 16 bytes -> MULO_ERR_UNSUPPORTED. */
 MULO_API mulo_status mulo_attach_prefix(mulo_ctx *ctx, const mulo_prefix *prefix);
@@ -408,7 +410,10 @@ MULO_API mulo_status mulo_set_window(mulo_ctx *ctx, int32_t sinks, int32_t windo
  *   top_k        the top_k largest entries stay, of equal ones those with the lowest index; 0: all
  *   top_p        of those an entry stays iff the mass in front of it (larger ones, equal ones of lower index) is below top_p
  *                times the mass of all of them; in (0, 1], 1: all
- *   min_p        of those an entry stays iff w_x >= min_p; in [0, 1] */
+ *   min_p        of those an entry stays iff w_x >= min_p; in [0, 1]
+ * Masses are sums of integers, w_x in units of 2^-44 of the largest, to the nearest: an entry below 2^-45 of the largest weighs
+ * nothing.  It is never drawn, and a top_p below 1 leaves it out, also one so near 1 (1 - top_p < vocab 2^-45) that the exact
+ * masses would keep it. */
 typedef struct {
     double temperature, top_p, min_p;
     int32_t top_k;
@@ -422,7 +427,7 @@ typedef struct {
  *   u           device float32 [rows] in [0, 1) (what lies outside counts as the nearest in it, NaN as 0); NULL allowed
  *               without tokens
  *   tokens      device int32 [rows] (out) or NULL: the first entry, by index, up to which the mass that stays exceeds u times
- *               all of it (64-bit weights: the draw does not depend on an order of summation); -1 for a row without an
+ *               all of it (integer masses: the draw does not depend on an order of summation); -1 for a row without an
  *               entry above -inf
  *   probs       device float32 [rows, vocab] (out) or NULL: the filtered distribution (a row of zeros if there is none):
  *               what mulo_upsample_draft and the accept test take as a draft's
@@ -430,6 +435,7 @@ typedef struct {
  *               within float32's finite range), -inf elsewhere: what the accept test takes as the target's.  May be
  *               `logits` itself for float32 rows that lie next to each other; no other output may overlap an input or an
  *               output
+ * (A recorded call needs an ordinary one of the same rows, vocab, type and guidance before it.)
  * Errors: no output -> MULO_ERR_NULL; vocab > 262144 or rows >= 2^22 -> MULO_ERR_UNSUPPORTED; row_stride < vocab -> MULO_ERR_SHAPE. */
 MULO_API mulo_status mulo_sample_filtered(void *hip_stream, const mulo_sample_params *p, int32_t rows, int32_t vocab,
                                  int32_t dtype, const void *logits, int64_t row_stride, const float *u,

@@ -21,14 +21,15 @@
 // bf16: the exponentials are rounded for the second product, whose matrix instruction takes bf16 (half a step of 2^-8 each, of either
 // sign, of positive terms; their sum l is taken of what was not rounded); scores, m, l, o and every partial result are float32.
 //
-// What bounds it, heads of 128, 32 of them, on a card that copies 5.05 TB/s and multiplies 8192^3 bf16 at 1.25 PFLOP/s:
+// What bounds it, heads of 128, 32 of them, on a card that reads 6.2 TB/s, copies 5.05 and multiplies 8192^3 bf16 at 1.25 PFLOP/s:
 //   single tokens over thousands of rows: memory.  64 tokens, two prefixes of 2048 rows and 900 own rows 199 us, 5.1 TB/s; 32 through a
 //   window of 2048 with 128 sinks 196 us, 5.8 TB/s
 //   long blocks: the matrix instruction and the softmax's vector instructions one after the other at a clock that falls under the load
-//   (4 x 1024 queries, 1024 shared and 2048 own rows 247 us, 975 TFLOP/s, matrix pipes busy 45 %; through a window of 1024 with 128
-//   sinks 106 to 112 us, 700 TFLOP/s, 38 %: a fifth of the scores it computes are those of tiles that a window cuts)
+//   (4 x 1024 queries, 1024 shared and 2048 own rows 247 to 256 us, 940 to 975 TFLOP/s, matrix pipes busy 45 %; through a window of
+//   1024 with 128 sinks 106 to 113 us, 700 TFLOP/s, 38 %: a query sees nine tiles' worth of keys, a wavefront computes ten and its
+//   workgroup goes through eleven, and each of the two rounds has a prologue and an epilogue that nothing overlaps)
 //   16 x 16 queries, 330 own and 4224 shared rows 52.6 us, 364 TFLOP/s: 42 in k_context, where the own rows' workgroups have one
-//   wavefront of four at work, and 25 MB of partial results each way
+//   wavefront of four at work, and 21 MB of partial results each way
 //   everything smaller: launches and one chain of latencies (a tile some 1.2 us; one launch 5 to 9 us, two 9 to 14)
 #include <hip/hip_bf16.h>
 
@@ -73,7 +74,7 @@ template <> struct Chunk<float> {
     }
 };
 
-constexpr float LAZY_EXP = 8.0f;     // the reference of the exponentials moves once the maximum has outgrown it by 2^8 (bf16; see attention.hip)
+constexpr float LAZY_EXP = 8.0f;     // the reference of the exponentials moves once the maximum has outgrown it by 2^8 (see attention.hip)
 constexpr int MAX_SLOTS = 64;        // shares of a query that k_context_join joins: a lane each
 
 // How a launch is laid out (host).

@@ -123,8 +123,9 @@ __device__ __forceinline__ float wave_max(float v) {
 // A thread takes the same entries in every pass.
 // PER: entries of the list a thread takes.  Where top-k leaves at most PER NT entries they are listed, and everything behind it
 // (masses, top-p, the draw's sums, what is written of them) goes by the list: of 16384 entries 2000 cost an eighth (a row of 16384,
-// 512 threads, top-p 0.9 alone 19.6 us, behind top-k 200 13.6).  With 512 threads two entries a thread would take 8 KB
-// that the second row of a CU needs.
+// 512 threads, top-p 0.9 alone 19.6 us, behind top-k 200 13.6).  With 512 threads a thread takes one: two would serve top-k up to
+// 1024, but a list takes two passes of its own, which only masses win back, and a shorter top-k is slower with two.  2048 rows of 16384, us, one / two: top-k 200 and top-p 0.9, tokens 64.6 / 65.7, logits 72.7 / 73.5; top-k 1000,
+// tokens 78.4 / 62.9, logits 55.8 / 77.8; top-k 1000 and top-p 0.9, tokens 115 / 73, logits 88.6 / 83.7.
 // KIND: ANY_ROWS, or what the rows are (1: bf16, 2: guided), for the form that reads them in every pass: each pass holds the loads of its
 // kind alone (of all kinds the code took 152 KB, more than the instruction cache by far; now 97 to 112.
 // 1 row of 33000 28.4 and 25.8 us, 16 of 131072 56 and 53, bf16 59.5 and 55.3, guided 66 and 62.5).
