@@ -441,6 +441,93 @@ MULO_API mulo_status mulo_sample_filtered(void *hip_stream, const mulo_sample_pa
                                  int32_t dtype, const void *logits, int64_t row_stride, const float *u,
                                  int32_t *tokens, float *probs, float *logits_out);
 
+/* ---- a packed cache: keys and values in 4 or 8 bits ------------------------------------------------------------------
+ * A group of 32 consecutive channels of a row is numbers of a grid times 2^e, with one byte 127 + e a group:
+ *   MULO_FP4   4 bits: 0, 0.5, 1, 1.5, 2, 3, 4, 6 (codes 0 to 7) and their negatives (codes 8 to 15); 4.25 bits a number
+ *   MULO_FP8   8 bits: sign, 4 bits of exponent (bias 7), 3 bits: up to 448; 8.25 bits a number
+ * e is the smallest integer with max |x| <= 7 * 2^e (MULO_FP8: 464 * 2^e): then no number of the group is further off than half of the
+ * grid's widest step.  It is at least -117 and at most 125 (119).  A number goes to the nearest of the grid, halfway to the even
+ * code, beyond the grid's end to its largest.  A group with an infinity or a NaN has the byte 255 and reads as NaN.  All
+ * numbers that a cache can hold are exact in bf16 and in float32. */
+typedef enum { MULO_FP4 = 0, MULO_FP8 = 1 } mulo_packed_format;
+
+/* A packed cache of B sequences, device memory of the caller.  Rows lie in tiles of 64, mulo_packed_tile_bytes each:
+ *   k, v        tile t of (sequence b, head h) begins at batch b + head h + t * tile bytes (strides in bytes); rows / 64 tiles
+ *   rows        rows allocated per sequence, a multiple of 64
+ * Inside a tile (dh = head_dim, G = dh / 32 groups, u = dh / 16) come the codes, 64 dh of them (MULO_FP4: two a byte, the even one in the
+ * lower half), and behind them the scale bytes, 64 G.  Row r, channel c, group g:
+ *   k   code r dh + c                                                      scale ((r % 16) G + g) 4 + r / 16
+ *   v   code (r / 4) 4 dh + (c / u) 4 u + (r % 4) u + c % u                scale ((r / 4 % 4 G + g) 4 + r / 16) 4 + r % 4
+ * Limits: head_dim 64 or 128; pointers and strides multiples of 16 bytes; rows <= 2^24. */
+typedef struct {
+    int32_t format, B, n_kv_heads, head_dim, rows;
+    void *k, *v;
+    int64_t batch, head;
+} mulo_packed_kv;
+
+/* Bytes of a tile of 64 rows; 0 for a format or head size that there is not. */
+MULO_API uint64_t mulo_packed_tile_bytes(int32_t format, int32_t head_dim);
+
+/* L consecutive rows of every sequence as numbers, device memory; strides in elements.
+ *   dtype       mulo_dtype of k and v
+ *   k           element (b, h, j, c) at k_batch b + k_head h + k_row j + c
+ *   v           element (b, h, j, c) at v_batch b + v_head h + v_row j + v_chan c; v_chan == 1 (rows of channels), or v_row == 1
+ *               (channels of rows, as mulo_kv keeps its values)
+ *   P, P_seq    row j is row P + j of the packed cache, or, when P_seq (device int32 [B]) is given, row P_seq[b] + j of sequence b; P
+ *               is then the largest of them.  An entry above rows - L counts as rows - L; a negative one says that the
+ *               sequence is absent: nothing of it is read or written.
+ * k or v may be NULL: the call then leaves those alone.
+ * Limits: pointers and strides of 16 bytes (not of channels of rows: any); B * n_kv_heads <= 2^22, B * n_kv_heads * L <= 2^26. */
+typedef struct {
+    int32_t dtype, L;
+    void *k, *v;
+    int64_t k_batch, k_head, k_row, v_batch, v_head, v_row, v_chan;
+    int32_t P;
+    const int32_t *P_seq;
+} mulo_kv_rows;
+
+/* Host-side check of the arguments (no GPU needed), also run by the two calls below. */
+MULO_API mulo_status mulo_check_packed_rows(const mulo_packed_kv *kv, const mulo_kv_rows *r);
+
+/* Both run on the current HIP device and allocate nothing.
+ * mulo_pack_rows writes rows of numbers into the cache and leaves its other rows as they are; mulo_unpack_rows writes rows of the
+ * cache as numbers, exactly (-0 comes back as -0).  Memory that a call writes must not overlap what it reads.
+ * Errors: (sequence, head)s of the cache, or rows of numbers that are written, on top of each other -> MULO_ERR_SHAPE. */
+MULO_API mulo_status mulo_pack_rows(void *hip_stream, const mulo_packed_kv *kv, const mulo_kv_rows *r);
+MULO_API mulo_status mulo_unpack_rows(void *hip_stream, const mulo_packed_kv *kv, const mulo_kv_rows *r);
+
+/* Attention of a block of L queries per sequence over the rows of a packed cache: mulo_attention without a prefix, over the numbers that the
+ * cache stands for.  Query j of sequence b sits at row P_b + j and sees row t iff t <= P_b + j and (window == 0, or t < sinks, or
+ * P_b + j - t < window).  Scores, statistics and sums in float32; for MULO_BF16 the exponentials are rounded to bf16 in front of the
+ * product with v, and a query's channel counts to within 2^-21 of the largest of its group of 32 (a bf16 number above 2^-13 of it
+ * counts as it is).
+ *   dtype        mulo_dtype of q and out
+ *   q, out       element (b, h, j, c) at q_batch b + q_head h + q_row j + c, n_heads heads (head h reads n_kv_heads * h / n_heads)
+ *   P, P_seq, sinks, window, scale  as mulo_attention_args; rows P_b .. P_b + L-1 hold the block's own keys and values
+ * Rows that no query of the call sees may hold anything; what some query sees has to be finite.  q and out must not overlap.
+ * batch and head of the cache may be 0 (sequences or heads that share theirs).
+ * Limits: those of mulo_packed_kv; q, out and their strides of 16 bytes; n_heads a multiple of n_kv_heads; B * n_heads <= 2^22,
+ * B * n_heads * L < 2^26. */
+typedef struct {
+    mulo_packed_kv kv;
+    int32_t dtype, L, n_heads;
+    const void *q;
+    int64_t q_batch, q_head, q_row;
+    void *out;
+    int64_t out_batch, out_head, out_row;
+    int32_t P;
+    const int32_t *P_seq;
+    int32_t sinks, window;
+    float scale;
+} mulo_packed_attention_args;
+
+/* Host-side check of the arguments (no GPU needed), also run by mulo_packed_attention. */
+MULO_API mulo_status mulo_check_packed_attention(const mulo_packed_attention_args *a);
+
+/* Scratch and errors as of mulo_attention_workspace_bytes and mulo_attention. */
+MULO_API uint64_t mulo_packed_attention_workspace_bytes(const mulo_packed_attention_args *a);
+MULO_API mulo_status mulo_packed_attention(void *hip_stream, const mulo_packed_attention_args *a, void *workspace, uint64_t workspace_bytes);
+
 /* Test and debugging aid (not part of the method): copies the first `bytes` bytes of one of the context's
  * workspace buffers, as the last mulo_verify_forward (or step) left it, to dst on the context's stream.  With a
  * one-layer model these are that layer's intermediate tensors, which is how the tests compare every stage of a

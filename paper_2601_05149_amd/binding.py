@@ -19,7 +19,9 @@ EXPORTS = ["mulo_status_string", "mulo_check_model_cfg", "mulo_check_step_params
            "mulo_create", "mulo_destroy", "mulo_upsample_draft", "mulo_verify_forward",
            "mulo_accept_local_resample", "mulo_accept_local_resample_static", "mulo_verify_step", "mulo_resample_sequential", "mulo_rejection_islands", "mulo_resample_islands", "mulo_workspace_read", "mulo_profile",
            "mulo_profile_read", "mulo_check_attention", "mulo_attention_workspace_bytes", "mulo_attention",
-           "mulo_attach_prefix", "mulo_set_window", "mulo_sample_filtered"]
+           "mulo_attach_prefix", "mulo_set_window", "mulo_sample_filtered",
+           "mulo_packed_tile_bytes", "mulo_check_packed_rows", "mulo_pack_rows", "mulo_unpack_rows", "mulo_check_packed_attention",
+           "mulo_packed_attention_workspace_bytes", "mulo_packed_attention"]
 
 
 class MuloError(RuntimeError):
@@ -60,6 +62,24 @@ class AttentionArgs(C.Structure):
                 [(n, C.c_int64) for n in ("prefix_k_group", "prefix_k_head", "prefix_k_row", "prefix_v_group", "prefix_v_head",
                                           "prefix_v_chan")] +
                 [(n, C.c_int32) for n in ("n_prefix", "prefix_len", "prefix_rows", "sinks", "window")] + [("scale", C.c_float)])
+
+
+class PackedKV(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("format", "B", "n_kv_heads", "head_dim", "rows")] + [(n, C.c_void_p) for n in ("k", "v")] +
+                [(n, C.c_int64) for n in ("batch", "head")])
+
+
+class KVRows(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("dtype", "L")] + [(n, C.c_void_p) for n in ("k", "v")] +
+                [(n, C.c_int64) for n in ("k_batch", "k_head", "k_row", "v_batch", "v_head", "v_row", "v_chan")] +
+                [("P", C.c_int32), ("P_seq", C.c_void_p)])
+
+
+class PackedAttentionArgs(C.Structure):
+    _fields_ = ([("kv", PackedKV)] + [(n, C.c_int32) for n in ("dtype", "L", "n_heads")] + [("q", C.c_void_p)] +
+                [(n, C.c_int64) for n in ("q_batch", "q_head", "q_row")] + [("out", C.c_void_p)] +
+                [(n, C.c_int64) for n in ("out_batch", "out_head", "out_row")] +
+                [("P", C.c_int32), ("P_seq", C.c_void_p), ("sinks", C.c_int32), ("window", C.c_int32), ("scale", C.c_float)])
 
 
 class Prefix(C.Structure):
@@ -113,8 +133,17 @@ def load_library():
     lib.mulo_attach_prefix.argtypes = [P, C.POINTER(Prefix)]
     lib.mulo_set_window.argtypes = [P, I32, I32]
     lib.mulo_sample_filtered.argtypes = [P, C.POINTER(SampleParams), I32, I32, I32, P, I64, P, P, P, P]
+    lib.mulo_packed_tile_bytes.restype = C.c_uint64
+    lib.mulo_packed_tile_bytes.argtypes = [I32, I32]
+    lib.mulo_check_packed_rows.argtypes = [C.POINTER(PackedKV), C.POINTER(KVRows)]
+    lib.mulo_pack_rows.argtypes = lib.mulo_unpack_rows.argtypes = [P, C.POINTER(PackedKV), C.POINTER(KVRows)]
+    lib.mulo_check_packed_attention.argtypes = [C.POINTER(PackedAttentionArgs)]
+    lib.mulo_packed_attention_workspace_bytes.restype = C.c_uint64
+    lib.mulo_packed_attention_workspace_bytes.argtypes = [C.POINTER(PackedAttentionArgs)]
+    lib.mulo_packed_attention.argtypes = [P, C.POINTER(PackedAttentionArgs), P, C.c_uint64]
     for n in EXPORTS:
-        if n not in ("mulo_status_string", "mulo_workspace_bytes", "mulo_destroy", "mulo_attention_workspace_bytes"):
+        if n not in ("mulo_status_string", "mulo_workspace_bytes", "mulo_destroy", "mulo_attention_workspace_bytes",
+                     "mulo_packed_tile_bytes", "mulo_packed_attention_workspace_bytes"):
             getattr(lib, n).restype = C.c_int
     _lib = lib
     return lib
@@ -410,6 +439,142 @@ def mulo_sample_filtered(params, logits, u=None, tokens=None, probs=None, logits
     _check(_on_device(device, stream, lambda st: lib.mulo_sample_filtered(
         st, C.byref(params), rows, V, MULO_BF16 if logits.dtype == torch.bfloat16 else MULO_F32, ptr, stride if n > 1 else V,
         u, tokens, probs, out)), "mulo_sample_filtered")
+
+
+MULO_FP4, MULO_FP8 = 0, 1
+
+
+class Packed:
+    """A packed cache: the tensors of its tiles and the struct that points to them."""
+
+    def __init__(self, args, k, v):
+        self.args, self.k, self.v, self.device = args, k, v, k.device
+        self.ref = C.byref(args)
+
+
+def mulo_packed_tile_bytes(format, head_dim):
+    return load_library().mulo_packed_tile_bytes(format, head_dim)
+
+
+def make_packed_kv(k, v, format, head_dim):
+    """k, v uint8 [B, n_kv_heads, rows / 64, mulo_packed_tile_bytes], the last two dimensions contiguous, strides alike."""
+    size = mulo_packed_tile_bytes(format, head_dim)
+    if not size:
+        raise ValueError("no packed cache of format %s with heads of %s" % (format, head_dim))
+    for t in (k, v):
+        if t.dim() != 4 or not t.is_cuda or t.dtype != torch.uint8 or t.shape[3] != size or t.stride(3) != 1 or (t.shape[2] > 1 and t.stride(2) != size):
+            raise ValueError("expected tiles, a device tensor [B, heads, tiles, %d] of uint8, contiguous in the last two dimensions" % size)
+    if k.shape != v.shape or k.device != v.device:
+        raise ValueError("keys and values do not fit together")
+    strides = [[t.stride(i) if t.shape[i] > 1 else 0 for i in range(2)] for t in (k, v)]
+    if strides[0] != strides[1]:
+        raise ValueError("keys and values have the same strides")
+    B, nkv, tiles = k.shape[:3]
+    return Packed(PackedKV(format, B, nkv, head_dim, tiles * 64, k.data_ptr(), v.data_ptr(), *strides[0]), k, v)
+
+
+def alloc_packed_kv(B, n_kv_heads, rows, head_dim, format=MULO_FP4, device="cuda"):
+    """A packed cache of at least `rows` rows (whole tiles of 64) a sequence, zeros."""
+    size = mulo_packed_tile_bytes(format, head_dim)
+    k, v = (torch.zeros(B, n_kv_heads, (rows + 63) // 64, size, dtype=torch.uint8, device=device) for _ in range(2))
+    return make_packed_kv(k, v, format, head_dim)
+
+
+class Rows:
+    """Rows of numbers of a packed cache's sequences, with the tensors they point into."""
+
+    def __init__(self, args, keep, shape, device):
+        self.args, self._keep, self.shape, self.device = args, keep, shape, device
+        self.ref = C.byref(args)
+
+
+def make_kv_rows(k, v, P, P_seq=None):
+    """k, v [B, n_kv_heads, L, head_dim], each or None: k in any strides with a contiguous last dimension, v also with a contiguous
+    third one (a mulo_kv's values, transposed); P_seq int32 [B] or None."""
+    given = [t for t in (k, v) if t is not None]
+    if not given or any(t.dim() != 4 or t.shape != given[0].shape or t.dtype != given[0].dtype or t.device != given[0].device for t in given):
+        raise ValueError("k and v do not fit together")
+    dtype, (B, nkv, L, dh) = given[0].dtype, given[0].shape
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("expected bfloat16 or float32, got %s" % dtype)
+    r = KVRows(dtype=MULO_BF16 if dtype == torch.bfloat16 else MULO_F32, L=L, P=P)
+    if k is not None:
+        r.k, (r.k_batch, r.k_head, r.k_row) = _strided(k, dtype, "k", 4)
+    if v is not None:
+        if not v.is_cuda or (v.stride(3) != 1 and L > 1 and v.stride(2) != 1):
+            raise ValueError("v: expected a device tensor, contiguous in its rows or in its channels")
+        r.v = v.data_ptr()
+        r.v_batch, r.v_head, r.v_row = (v.stride(i) if v.shape[i] > 1 else 0 for i in range(3))
+        r.v_chan = v.stride(3)
+    keep = given
+    if P_seq is not None:
+        if P_seq.shape != (B,) or P_seq.device != given[0].device:
+            raise ValueError("P_seq has one entry per sequence, on the device of the rows")
+        r.P_seq = _ptr(P_seq, torch.int32)
+        keep = given + [P_seq]
+    return Rows(r, keep, (B, nkv, dh), given[0].device)
+
+
+def _packed_rows(name, packed, rows, stream):
+    if rows.shape != (packed.args.B, packed.args.n_kv_heads, packed.args.head_dim) or rows.device != packed.device:
+        raise ValueError("the rows are not those of this cache")
+    call = getattr(load_library(), name)
+    _check(_on_device(packed.device, stream, lambda st: call(st, packed.ref, rows.ref)), name)
+
+
+def mulo_pack_rows(packed, rows, stream=None):
+    """Writes the rows of make_kv_rows into the cache of make_packed_kv."""
+    _packed_rows("mulo_pack_rows", packed, rows, stream)
+
+
+def mulo_unpack_rows(packed, rows, stream=None):
+    """Writes rows of the cache into the tensors of make_kv_rows."""
+    _packed_rows("mulo_unpack_rows", packed, rows, stream)
+
+
+class PackedAttention:
+    """Arguments of mulo_packed_attention, checked, with the tensors they point into."""
+
+    def __init__(self, args, keep, device):
+        self.args, self._keep, self.device = args, keep, device
+        self.ref = C.byref(args)
+
+
+def make_packed_attention(packed, q, out, P, P_seq=None, sinks=0, window=0, scale=0.0):
+    """q, out [B, n_heads, L, head_dim], any strides with a contiguous last dimension; P_seq int32 [B] or None."""
+    if q.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("expected bfloat16 or float32, got %s" % q.dtype)
+    B, nh, L, dh = q.shape
+    if out.shape != q.shape or (B, dh) != (packed.args.B, packed.args.head_dim):
+        raise ValueError("q, out and the cache do not fit together")
+    a = PackedAttentionArgs(kv=packed.args, dtype=MULO_BF16 if q.dtype == torch.bfloat16 else MULO_F32, L=L, n_heads=nh, P=P, sinks=sinks,
+                            window=window, scale=scale)
+    a.q, (a.q_batch, a.q_head, a.q_row) = _strided(q, q.dtype, "q", 4)
+    a.out, (a.out_batch, a.out_head, a.out_row) = _strided(out, q.dtype, "out", 4)
+    tensors = [q, out, packed.k, packed.v]
+    if P_seq is not None:
+        if P_seq.shape != (B,):
+            raise ValueError("P_seq has one entry per sequence")
+        a.P_seq = _ptr(P_seq, torch.int32)
+        tensors.append(P_seq)
+    if any(t.device != q.device for t in tensors):
+        raise ValueError("the tensors of a call lie on one device")
+    _check(load_library().mulo_check_packed_attention(C.byref(a)), "mulo_check_packed_attention")
+    return PackedAttention(a, tensors, q.device)
+
+
+def mulo_packed_attention_workspace_bytes(attention):
+    with torch.cuda.device(attention.device):
+        return load_library().mulo_packed_attention_workspace_bytes(attention.ref)
+
+
+def mulo_packed_attention(attention, workspace=None, stream=None):
+    """Writes `out` of make_packed_attention; workspace: a contiguous device tensor or None."""
+    ptr, n = (None, 0) if workspace is None else (_ptr(workspace), workspace.numel() * workspace.element_size())
+    if workspace is not None and workspace.device != attention.device:
+        raise ValueError("the workspace lies on another device")
+    lib = load_library()
+    _check(_on_device(attention.device, stream, lambda st: lib.mulo_packed_attention(st, attention.ref, ptr, n)), "mulo_packed_attention")
 
 
 PROF_CLASSES = ["gemm_qkv", "gemm_out", "gemm_gate_up", "gemm_down", "gemm_lm_head", "attention", "norm_embed",

@@ -35,6 +35,7 @@
 
 #include <utility>
 
+#include "index_div.h"
 #include "mulo_internal.h"
 
 namespace mulo {
@@ -89,25 +90,6 @@ struct Plan {
     int split;         // shares of the keys (stacked: of the own rows)
     int prefix_split;  // stacked: shares of the prefix
     int prefix_wgs;    // workgroups of the prefix (the first ones of the grid)
-};
-// Division of x < 2^32 by a number that the host knows, by multiplication: with 2^(l - 1) < d <= 2^l and
-// m = floor(2^32 (2^l - d) / d) + 1, t = the high word of m x, the quotient is (t + (x - t) / 2^min(l, 1)) / 2^max(l - 1, 0)
-// (Granlund and Montgomery, "Division by invariant integers using multiplication").  A division by a kernel argument is
-// some 30 instructions in a row, and a workgroup has eight in front of its first load.
-struct Div {
-    uint32_t d, m, s1, s2;
-    Div() = default;
-    explicit Div(uint32_t by) : d(by) {
-        uint32_t l = 0;
-        while (((uint64_t)1 << l) < d) ++l;
-        m = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << l) - d)) / d + 1);
-        s1 = l < 1 ? l : 1;
-        s2 = l < 1 ? 0 : l - 1;
-    }
-    __device__ __forceinline__ int of(int x) const {
-        const uint32_t t = __umulhi(m, (uint32_t)x);
-        return (int)((t + (((uint32_t)x - t) >> s1)) >> s2);
-    }
 };
 struct Args : ContextAttn, Plan {
     float* ml;         // [slots][B nh L] pairs: maximum and sum, behind the [slots][B nh L][dh] outputs in part

@@ -527,6 +527,21 @@ bool context_sizes_ok(const mulo_ctx* ctx, int rows) {
            ctx->cfg.max_seq % (int)(16 / ctx->esz) == 0 && rows <= (1 << 24) && ctx->cfg.max_seq <= (1 << 24);
 }
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+// Are the places of an array apart?  Every dimension has to step over what lies inside it (runs of `extent` innermost), in one order or another.
+struct Dim { int64_t n, step; };
+bool apart(const Dim* dims, int n_dims, int64_t extent) {
+    Dim d[4];
+    for (int i = 0; i < n_dims; ++i) d[i] = dims[i];
+    for (int i = 0; i < n_dims; ++i)      // innermost first
+        for (int j = i + 1; j < n_dims; ++j)
+            if (d[j].n > 1 && (d[i].n == 1 || d[j].step < d[i].step)) { const Dim t = d[i]; d[i] = d[j]; d[j] = t; }
+    for (int i = 0; i < n_dims; ++i) {
+        if (d[i].n == 1) continue;
+        if (d[i].step < extent) return false;
+        extent += (d[i].n - 1) * d[i].step;
+    }
+    return true;
+}
 }  // namespace
 
 mulo_status mulo_attach_prefix(mulo_ctx* ctx, const mulo_prefix* p) {
@@ -572,19 +587,8 @@ mulo_status mulo_check_attention(const mulo_attention_args* a) {
     if (a->k_row < a->head_dim || a->v_chan < a->rows ||
         (prefix && (a->prefix_k_row < a->head_dim || a->prefix_v_chan < a->prefix_rows)))
         return MULO_ERR_SHAPE;
-    // no two outputs at one place: every dimension steps over what lies inside it, in one order or another
-    {
-        struct Dim { int64_t n, step; } d[3] = {{a->B, a->out_batch}, {a->n_heads, a->out_head}, {a->L, a->out_row}};
-        for (int i = 0; i < 3; ++i)      // innermost first
-            for (int j = i + 1; j < 3; ++j)
-                if (d[j].n > 1 && (d[i].n == 1 || d[j].step < d[i].step)) { const Dim t = d[i]; d[i] = d[j]; d[j] = t; }
-        int64_t extent = a->head_dim;
-        for (int i = 0; i < 3; ++i) {
-            if (d[i].n == 1) continue;
-            if (d[i].step < extent) return MULO_ERR_SHAPE;
-            extent += (d[i].n - 1) * d[i].step;
-        }
-    }
+    const Dim outs[] = {{a->B, a->out_batch}, {a->n_heads, a->out_head}, {a->L, a->out_row}};
+    if (!apart(outs, 3, a->head_dim)) return MULO_ERR_SHAPE;
     if (a->head_dim != 64 && a->head_dim != 128) return MULO_ERR_UNSUPPORTED;
     const int unit = a->dtype == MULO_BF16 ? 8 : 4;      // elements of 16 bytes
     for (int i = 0; i < n_strides; ++i)
@@ -637,6 +641,147 @@ mulo_status mulo_attention(void* hip_stream, const mulo_attention_args* p, void*
     a.part = (float*)workspace;
     a.part_floats = workspace ? (int64_t)((workspace_bytes < ((uint64_t)1 << 40) ? workspace_bytes : (uint64_t)1 << 40) / sizeof(float)) : 0;
     launch_context_attention(a, (hipStream_t)hip_stream);
+    return check_launch();
+}
+
+uint64_t mulo_packed_tile_bytes(int32_t format, int32_t head_dim) {
+    if ((format != MULO_FP4 && format != MULO_FP8) || (head_dim != 64 && head_dim != 128)) return 0;
+    return (uint64_t)packed_tile_bytes(format, head_dim);
+}
+
+namespace {
+constexpr int64_t MAX_STRIDE = (int64_t)1 << 40;
+// sizes, strides and what the kernels take of a packed cache; k, v: which of the two the call touches
+mulo_status check_packed_kv(const mulo_packed_kv* c, bool k, bool v) {
+    if ((k && !c->k) || (v && !c->v)) return MULO_ERR_NULL;
+    if ((c->format != MULO_FP4 && c->format != MULO_FP8) || c->B < 1 || c->n_kv_heads < 1 || c->head_dim < 1 || c->rows < 1 ||
+        c->batch < 0 || c->batch > MAX_STRIDE || c->head < 0 || c->head > MAX_STRIDE)
+        return MULO_ERR_RANGE;
+    if (k && v && c->k == c->v) return MULO_ERR_SHAPE;
+    if ((c->head_dim != 64 && c->head_dim != 128) || c->rows % PACKED_TILE || c->rows > (1 << 24) || c->batch % 16 || c->head % 16 ||
+        (k && !aligned16(c->k)) || (v && !aligned16(c->v)))
+        return MULO_ERR_UNSUPPORTED;
+    return MULO_OK;
+}
+// writes: 0 neither (the check on its own), 1 the packed cache, 2 the rows of numbers
+mulo_status check_packed_rows(const mulo_packed_kv* c, const mulo_kv_rows* r, int writes) {
+    if (!c || !r || (!r->k && !r->v)) return MULO_ERR_NULL;
+    if (r->dtype != MULO_F32 && r->dtype != MULO_BF16) return MULO_ERR_RANGE;
+    if (r->L < 1 || r->P < 0) return MULO_ERR_RANGE;
+    const mulo_status s = check_packed_kv(c, r->k != nullptr, r->v != nullptr);
+    if (s != MULO_OK) return s;
+    if ((int64_t)r->P + r->L > c->rows) return MULO_ERR_SHAPE;
+    const int unit = r->dtype == MULO_BF16 ? 8 : 4;      // elements of 16 bytes
+    if (r->k) {
+        const int64_t strides[] = {r->k_batch, r->k_head, r->k_row};
+        for (const int64_t x : strides)
+            if (x < 0 || x > MAX_STRIDE) return MULO_ERR_RANGE;
+        for (const int64_t x : strides)
+            if (x % unit) return MULO_ERR_UNSUPPORTED;
+        if (!aligned16(r->k)) return MULO_ERR_UNSUPPORTED;
+        const Dim d[] = {{c->B, r->k_batch}, {c->n_kv_heads, r->k_head}, {r->L, r->k_row}};
+        if (writes == 2 && !apart(d, 3, c->head_dim)) return MULO_ERR_SHAPE;
+    }
+    if (r->v) {
+        const int64_t strides[] = {r->v_batch, r->v_head, r->v_row, r->v_chan};
+        for (const int64_t x : strides)
+            if (x < 0 || x > MAX_STRIDE) return MULO_ERR_RANGE;
+        if (r->v_chan != 1 && r->v_row != 1 && r->L > 1) return MULO_ERR_UNSUPPORTED;
+        if (r->v_chan == 1) {
+            for (int i = 0; i < 3; ++i)
+                if (strides[i] % unit) return MULO_ERR_UNSUPPORTED;
+            if (!aligned16(r->v)) return MULO_ERR_UNSUPPORTED;
+        } else if ((uintptr_t)r->v % (r->dtype == MULO_BF16 ? 2 : 4)) {
+            return MULO_ERR_UNSUPPORTED;
+        }
+        const Dim d[] = {{c->B, r->v_batch}, {c->n_kv_heads, r->v_head}, {r->L, r->v_row}, {c->head_dim, r->v_chan}};
+        if (writes == 2 && !apart(d, 4, 1)) return MULO_ERR_SHAPE;
+        if (writes == 2 && r->k == r->v) return MULO_ERR_SHAPE;
+    }
+    if (writes == 1) {
+        const Dim d[] = {{c->B, c->batch}, {c->n_kv_heads, c->head}};
+        if (!apart(d, 2, c->rows / PACKED_TILE * packed_tile_bytes(c->format, c->head_dim))) return MULO_ERR_SHAPE;
+    }
+    const int64_t pairs = (int64_t)c->B * c->n_kv_heads;      // fewer than 2^32 threads a launch: 16 a row, 256 for 64 rows or fewer of a pair
+    if (pairs > (1 << 22) || pairs * r->L > (1 << 26)) return MULO_ERR_UNSUPPORTED;
+    return MULO_OK;
+}
+PackedRows packed_rows(const mulo_packed_kv* c, const mulo_kv_rows* r) {
+    PackedRows a{};
+    a.fmt = c->format; a.dtype = r->dtype; a.B = c->B; a.nkv = c->n_kv_heads; a.dh = c->head_dim; a.rows = c->rows; a.L = r->L; a.P = r->P;
+    a.P_seq = r->P_seq;
+    a.pk = (uint8_t*)c->k; a.pv = (uint8_t*)c->v; a.batch = c->batch; a.head = c->head;
+    a.k = r->k; a.v = r->v;
+    a.k_batch = r->k_batch; a.k_head = r->k_head; a.k_row = r->k_row;
+    a.v_batch = r->v_batch; a.v_head = r->v_head; a.v_row = r->v_row; a.v_chan = r->v_chan;
+    return a;
+}
+}  // namespace
+
+mulo_status mulo_check_packed_rows(const mulo_packed_kv* kv, const mulo_kv_rows* r) { return check_packed_rows(kv, r, 0); }
+
+mulo_status mulo_pack_rows(void* hip_stream, const mulo_packed_kv* kv, const mulo_kv_rows* r) {
+    const mulo_status s = check_packed_rows(kv, r, 1);
+    if (s != MULO_OK) return s;
+    launch_pack_rows(packed_rows(kv, r), (hipStream_t)hip_stream);
+    return check_launch();
+}
+
+mulo_status mulo_unpack_rows(void* hip_stream, const mulo_packed_kv* kv, const mulo_kv_rows* r) {
+    const mulo_status s = check_packed_rows(kv, r, 2);
+    if (s != MULO_OK) return s;
+    launch_unpack_rows(packed_rows(kv, r), (hipStream_t)hip_stream);
+    return check_launch();
+}
+
+mulo_status mulo_check_packed_attention(const mulo_packed_attention_args* a) {
+    if (!a || !a->q || !a->out) return MULO_ERR_NULL;
+    if (a->dtype != MULO_F32 && a->dtype != MULO_BF16) return MULO_ERR_RANGE;
+    if (a->L < 1 || a->n_heads < 1 || a->P < 0 || a->sinks < 0 || a->window < 0 || !(a->scale >= 0.f && a->scale <= 1.0e6f)) return MULO_ERR_RANGE;
+    const mulo_packed_kv* c = &a->kv;
+    const mulo_status s = check_packed_kv(c, true, true);
+    if (s != MULO_OK) return s;
+    const int64_t strides[] = {a->q_batch, a->q_head, a->q_row, a->out_batch, a->out_head, a->out_row};
+    for (const int64_t x : strides)
+        if (x < 0 || x > MAX_STRIDE) return MULO_ERR_RANGE;
+    if ((int64_t)a->P + a->L > c->rows || a->n_heads % c->n_kv_heads) return MULO_ERR_SHAPE;
+    const Dim outs[] = {{c->B, a->out_batch}, {a->n_heads, a->out_head}, {a->L, a->out_row}};
+    if (!apart(outs, 3, c->head_dim)) return MULO_ERR_SHAPE;
+    const int unit = a->dtype == MULO_BF16 ? 8 : 4;
+    for (const int64_t x : strides)
+        if (x % unit) return MULO_ERR_UNSUPPORTED;
+    if (!aligned16(a->q) || !aligned16(a->out)) return MULO_ERR_UNSUPPORTED;
+    const int64_t pairs = (int64_t)c->B * a->n_heads;      // fewer than 2^32 threads a launch
+    if (pairs > (1 << 22) || pairs * a->L >= (1 << 26)) return MULO_ERR_UNSUPPORTED;
+    return MULO_OK;
+}
+
+namespace {
+PackedAttn packed_attn(const mulo_packed_attention_args* p) {
+    PackedAttn a{};
+    a.fmt = p->kv.format; a.dtype = p->dtype; a.B = p->kv.B; a.L = p->L; a.nh = p->n_heads; a.nkv = p->kv.n_kv_heads; a.dh = p->kv.head_dim;
+    a.q = p->q; a.q_batch = p->q_batch; a.q_head = p->q_head; a.q_row = p->q_row;
+    a.out = p->out; a.out_batch = p->out_batch; a.out_head = p->out_head; a.out_row = p->out_row;
+    a.k = (const uint8_t*)p->kv.k; a.v = (const uint8_t*)p->kv.v; a.batch = p->kv.batch; a.head = p->kv.head;
+    a.rows = p->kv.rows; a.P = p->P; a.P_seq = p->P_seq; a.sinks = p->sinks; a.window = p->window;
+    a.scale_log2 = 1.4426950408889634f * (p->scale > 0.f ? p->scale : 1.0f / sqrtf((float)p->kv.head_dim));
+    return a;
+}
+}  // namespace
+
+uint64_t mulo_packed_attention_workspace_bytes(const mulo_packed_attention_args* p) {
+    if (mulo_check_packed_attention(p) != MULO_OK) return 0;
+    return (uint64_t)packed_attention_floats(packed_attn(p)) * sizeof(float);
+}
+
+mulo_status mulo_packed_attention(void* hip_stream, const mulo_packed_attention_args* p, void* workspace, uint64_t workspace_bytes) {
+    const mulo_status s = mulo_check_packed_attention(p);
+    if (s != MULO_OK) return s;
+    if (!aligned16(workspace)) return MULO_ERR_UNSUPPORTED;
+    PackedAttn a = packed_attn(p);
+    a.part = (float*)workspace;
+    a.part_floats = workspace ? (int64_t)((workspace_bytes < ((uint64_t)1 << 40) ? workspace_bytes : (uint64_t)1 << 40) / sizeof(float)) : 0;
+    launch_packed_attention(a, (hipStream_t)hip_stream);
     return check_launch();
 }
 

@@ -231,6 +231,37 @@ struct ContextAttn {
 size_t context_attention_floats(const ContextAttn& a);   // scratch it runs fastest with
 void launch_context_attention(const ContextAttn& a, hipStream_t st);
 
+// ---- a packed cache (packed.hip) ----
+constexpr int PACKED_TILE = 64, PACKED_GROUP = 32;      // rows of a tile, channels of a group
+inline int64_t packed_tile_bytes(int fmt, int dh) { return PACKED_TILE * (int64_t)(dh / (fmt == 0 ? 2 : 1) + dh / PACKED_GROUP); }
+struct PackedRows {
+    int fmt, dtype, B, nkv, dh, rows, L, P;
+    const int32_t* P_seq;   // [B] or nullptr; < 0: absent
+    uint8_t *pk, *pv;       // tiles
+    int64_t batch, head;    // bytes
+    void *k, *v;            // numbers; nullptr: not of this call
+    int64_t k_batch, k_head, k_row, v_batch, v_head, v_row, v_chan;
+};
+void launch_pack_rows(const PackedRows& a, hipStream_t st);
+void launch_unpack_rows(const PackedRows& a, hipStream_t st);
+struct PackedAttn {
+    int fmt, dtype, B, L, nh, nkv, dh;
+    const void* q;
+    int64_t q_batch, q_head, q_row;
+    void* out;
+    int64_t out_batch, out_head, out_row;
+    const uint8_t *k, *v;
+    int64_t batch, head;
+    int rows, P;
+    const int32_t* P_seq;
+    int sinks, window;
+    float scale_log2;
+    float* part;            // scratch of part_floats floats (0: none)
+    int64_t part_floats;
+};
+size_t packed_attention_floats(const PackedAttn& a);
+void launch_packed_attention(const PackedAttn& a, hipStream_t st);
+
 // ---- filtered draws (sample.hip) ----
 struct SampleArgs {
     const void *logits, *logits_u;   // rows of V entries row_stride apart; logits_u: the unconditional twins or nullptr

@@ -1,0 +1,349 @@
+// A cache in 4 or 8 bits: rows packed as they are written, read back, and attended to.  (The formats and the tiles: include/mulo.h.)
+#include <hip/hip_bf16.h>
+
+#include <type_traits>
+
+#include "index_div.h"
+#include "mulo_internal.h"
+
+namespace mulo {
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(2))) short i16x2;
+
+constexpr int FP4 = 0, FP8 = 1;
+
+// ---- places in a tile, in bytes behind its start --------------------------------------------------------------------
+template <int FMT, int DH> struct Tile {
+    static constexpr int ROW = FMT == FP4 ? DH / 2 : DH;                 // bytes of a row's codes
+    static constexpr int G = DH / PACKED_GROUP, CODES = PACKED_TILE * ROW, BYTES = CODES + PACKED_TILE * G;
+    static constexpr int UNIT = ROW / 16;                                // bytes of the values of one row that lie together
+    static __host__ __device__ constexpr int k_scale(int r, int g) { return CODES + ((r & 15) * G + g) * 4 + (r >> 4); }
+    static __host__ __device__ constexpr int v_code(int r, int unit) { return (r >> 2) * 4 * ROW + unit * 4 * UNIT + (r & 3) * UNIT; }
+    static __host__ __device__ constexpr int v_scale(int r, int g) { return CODES + (((r >> 2 & 3) * G + g) * 4 + (r >> 4)) * 4 + (r & 3); }
+};
+
+// ---- eight numbers and their codes ---------------------------------------------------------------------------------
+// The byte 127 + e of a group whose largest |x| has these bits: e is the smallest integer with |x| <= T 2^e, T = 7 = 1.75 2^2 or
+// 464 = 1.8125 2^8.  Infinities and NaN have the largest bits of all: 255.
+template <int FMT> __device__ __forceinline__ uint32_t scale_byte(uint32_t bits) {
+    constexpr int TE = FMT == FP4 ? 2 : 8, TOP = FMT == FP4 ? 252 : 246;
+    constexpr uint32_t TM = FMT == FP4 ? 0x600000u : 0x680000u;
+    if (bits >= 0x7F800000u) return 255;
+    const int b = (int)(bits >> 23) - TE + ((bits & 0x7FFFFFu) > TM ? 1 : 0);
+    return (uint32_t)(b < 10 ? 10 : b > TOP ? TOP : b);
+}
+template <int FMT> using Codes8 = std::conditional_t<FMT == FP4, uint32_t, uint2>;
+__device__ __forceinline__ Codes8<FP4> encode8(std::integral_constant<int, FP4>, const float* x, float s) {
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], s, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], s, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], s, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], s, 3);
+}
+// (The conversion to 8 bits takes what lies beyond the grid for NaN.)
+__device__ __forceinline__ Codes8<FP8> encode8(std::integral_constant<int, FP8>, const float* x, float s) {
+    const float top = 448.f * s;
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = __builtin_amdgcn_fmed3f(x[i], -top, top);
+    i16x2 a = {0, 0}, b = {0, 0};
+    a = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(a, y[0], y[1], s, false);
+    a = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(a, y[2], y[3], s, true);
+    b = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(b, y[4], y[5], s, false);
+    b = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(b, y[6], y[7], s, true);
+    return make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
+}
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+__device__ __forceinline__ void decode8(uint32_t w, float s, float* x) {
+    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 1),
+                c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 3);
+    x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y; x[4] = c.x; x[5] = c.y; x[6] = d.x; x[7] = d.y;
+}
+__device__ __forceinline__ void decode8(uint2 w, float s, float* x) {
+    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.x, s, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.x, s, true),
+                c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.y, s, false), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.y, s, true);
+    x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y; x[4] = c.x; x[5] = c.y; x[6] = d.x; x[7] = d.y;
+}
+__device__ __forceinline__ void load8(const __bf16* p, float* x) {
+    const bf16x8 v = *reinterpret_cast<const bf16x8*>(p);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
+}
+__device__ __forceinline__ void load8(const float* p, float* x) {
+    const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+__device__ __forceinline__ void store8(__bf16* p, const float* x) {
+    bf16x8 v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (__bf16)x[i];      // exact
+    *reinterpret_cast<bf16x8*>(p) = v;
+}
+__device__ __forceinline__ void store8(float* p, const float* x) {
+    *reinterpret_cast<f32x4*>(p) = f32x4{x[0], x[1], x[2], x[3]};
+    *reinterpret_cast<f32x4*>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+}
+template <int X> __device__ __forceinline__ uint32_t quad_swap(uint32_t v) {      // lane ^ 1 or ^ 2
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, X == 1 ? 0xB1 : 0x4E, 0xF, 0xF, true);
+}
+
+// ---- rows in, rows out ----------------------------------------------------------------------------------------------
+// A thread has eight channels of a row, four threads a group: 16 bytes of bf16 in, 4 or 8 bytes of codes out, or the other way round.
+// Values that come as channels of rows go through LDS, 64 rows a workgroup.
+constexpr int ROWS_THREADS = 256;
+struct RowsArgs : PackedRows {
+    Div by_L, by_nkv, by_chunks;
+    uint32_t k_blocks;      // the first ones of the grid
+    int total, chunks;      // rows of the call; workgroups of a (sequence, head) whose values are channels of rows
+    bool v_across;
+};
+template <int FMT, int DH> __device__ __forceinline__ void put(uint8_t* tile, int r, int t8, bool keys, Codes8<FMT> w, uint32_t byte) {
+    using TL = Tile<FMT, DH>;
+    constexpr int B8 = sizeof(w);      // bytes of eight channels
+    if (keys) {
+        *reinterpret_cast<Codes8<FMT>*>(tile + r * TL::ROW + t8 * B8) = w;
+    } else if constexpr (DH == 128) {
+        *reinterpret_cast<Codes8<FMT>*>(tile + TL::v_code(r, t8)) = w;
+    } else if constexpr (FMT == FP4) {
+        *reinterpret_cast<uint16_t*>(tile + TL::v_code(r, 2 * t8)) = (uint16_t)w;
+        *reinterpret_cast<uint16_t*>(tile + TL::v_code(r, 2 * t8 + 1)) = (uint16_t)(w >> 16);
+    } else {
+        *reinterpret_cast<uint32_t*>(tile + TL::v_code(r, 2 * t8)) = w.x;
+        *reinterpret_cast<uint32_t*>(tile + TL::v_code(r, 2 * t8 + 1)) = w.y;
+    }
+    if ((t8 & 3) == 0) tile[keys ? TL::k_scale(r, t8 >> 2) : TL::v_scale(r, t8 >> 2)] = (uint8_t)byte;
+}
+template <int FMT, int DH> __device__ __forceinline__ Codes8<FMT> get(const uint8_t* tile, int r, int t8, bool keys) {
+    using TL = Tile<FMT, DH>;
+    constexpr int B8 = sizeof(Codes8<FMT>);
+    if (keys) return *reinterpret_cast<const Codes8<FMT>*>(tile + r * TL::ROW + t8 * B8);
+    if constexpr (DH == 128) return *reinterpret_cast<const Codes8<FMT>*>(tile + TL::v_code(r, t8));
+    else if constexpr (FMT == FP4)
+        return *reinterpret_cast<const uint16_t*>(tile + TL::v_code(r, 2 * t8)) | (uint32_t)*reinterpret_cast<const uint16_t*>(tile + TL::v_code(r, 2 * t8 + 1)) << 16;
+    else return make_uint2(*reinterpret_cast<const uint32_t*>(tile + TL::v_code(r, 2 * t8)), *reinterpret_cast<const uint32_t*>(tile + TL::v_code(r, 2 * t8 + 1)));
+}
+template <int FMT, int DH> __device__ __forceinline__ void pack8(uint8_t* tile, int r, int t8, bool keys, const float* x) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t a = __float_as_uint(x[i]) & 0x7FFFFFFFu;
+        m = a > m ? a : m;
+    }
+    const uint32_t m1 = quad_swap<1>(m);
+    m = m1 > m ? m1 : m;
+    const uint32_t m2 = quad_swap<2>(m);
+    m = m2 > m ? m2 : m;
+    const uint32_t byte = scale_byte<FMT>(m);
+    Codes8<FMT> w = encode8(std::integral_constant<int, FMT>{}, x, scale_of(byte));
+    if (byte == 255) w = Codes8<FMT>{};
+    put<FMT, DH>(tile, r, t8, keys, w, byte);
+}
+template <int FMT, int DH> __device__ __forceinline__ void unpack8(const uint8_t* tile, int r, int t8, bool keys, float* x) {
+    using TL = Tile<FMT, DH>;
+    const uint32_t byte = tile[keys ? TL::k_scale(r, t8 >> 2) : TL::v_scale(r, t8 >> 2)];
+    decode8(get<FMT, DH>(tile, r, t8, keys), scale_of(byte), x);
+    if (byte == 255) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __builtin_nanf("");
+    }
+}
+__device__ __forceinline__ int first_row(const PackedRows& a, int b) {
+    if (!a.P_seq) return a.P;
+    const int P = a.P_seq[b];
+    return P < a.rows - a.L ? P : a.rows - a.L;
+}
+
+template <int FMT, class T, int DH, bool PACK>
+__global__ __launch_bounds__(ROWS_THREADS) void k_packed_rows(const RowsArgs a) {
+    using TL = Tile<FMT, DH>;
+    constexpr int TR = DH / 8, NR = ROWS_THREADS / TR;      // threads of a row, rows at a time
+    const int tid = threadIdx.x, t8 = tid % TR;
+    const bool keys = blockIdx.x < a.k_blocks;
+    const int id = (int)(blockIdx.x - (keys ? 0 : a.k_blocks));
+    uint8_t* const cache = keys ? a.pk : a.pv;
+    if (keys || !a.v_across) {
+        const int row = id * NR + tid / TR;
+        if (row >= a.total) return;
+        const int bh = a.by_L.of(row), j = row - bh * a.L, b = a.by_nkv.of(bh), h = bh - b * a.nkv;
+        const int P = first_row(a, b);
+        if (P < 0) return;
+        const int at = P + j, r = at % PACKED_TILE;
+        uint8_t* const tile = cache + b * a.batch + h * a.head + (int64_t)(at / PACKED_TILE) * TL::BYTES;
+        T* const src = reinterpret_cast<T*>(keys ? a.k : a.v) + (keys ? b * a.k_batch + h * a.k_head + j * a.k_row : b * a.v_batch + h * a.v_head + j * a.v_row) + t8 * 8;
+        float x[8];
+        if constexpr (PACK) {
+            load8(src, x);
+            pack8<FMT, DH>(tile, r, t8, keys, x);
+        } else {
+            unpack8<FMT, DH>(tile, r, t8, keys, x);
+            store8(src, x);
+        }
+        return;
+    }
+    // rows of this workgroup: 64 of a (sequence, head), next to each other in memory; LDS holds them as rows of channels
+    constexpr int PITCH = DH + (sizeof(T) == 2 ? 2 : 1);      // odd words: neither the rows nor the channels of a wavefront share a bank
+    __shared__ T lds[PACKED_TILE * PITCH];
+    const int bh = a.by_chunks.of(id), j0 = (id - bh * a.chunks) * PACKED_TILE, b = a.by_nkv.of(bh), h = bh - b * a.nkv;
+    const int P = first_row(a, b);
+    if (P < 0) return;      // the whole workgroup
+    const int n = a.L - j0 < PACKED_TILE ? a.L - j0 : PACKED_TILE;
+    T* const src = reinterpret_cast<T*>(a.v) + b * a.v_batch + h * a.v_head + j0;
+    uint8_t* const head = cache + b * a.batch + h * a.head;
+    const int lane = tid & 63, wave = tid >> 6;
+    if constexpr (PACK) {
+        for (int c = wave; c < DH; c += ROWS_THREADS / 64)
+            if (lane < n) lds[lane * PITCH + c] = src[c * a.v_chan + lane];
+        __syncthreads();
+    }
+    for (int j = tid / TR; j < n; j += NR) {
+        const int at = P + j0 + j;
+        uint8_t* const tile = head + (int64_t)(at / PACKED_TILE) * TL::BYTES;
+        T* const mine = lds + j * PITCH + t8 * 8;
+        float x[8];
+        if constexpr (PACK) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = (float)mine[i];
+            pack8<FMT, DH>(tile, at % PACKED_TILE, t8, false, x);
+        } else {
+            unpack8<FMT, DH>(tile, at % PACKED_TILE, t8, false, x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) mine[i] = (T)x[i];
+        }
+    }
+    if constexpr (!PACK) {
+        __syncthreads();
+        for (int c = wave; c < DH; c += ROWS_THREADS / 64)
+            if (lane < n) src[c * a.v_chan + lane] = lds[lane * PITCH + c];
+    }
+}
+template <int FMT, class T, int DH, bool PACK> void run_rows(const PackedRows& p, hipStream_t st) {
+    constexpr int NR = ROWS_THREADS / (DH / 8);
+    RowsArgs a{};
+    static_cast<PackedRows&>(a) = p;
+    a.total = p.B * p.nkv * p.L;
+    a.chunks = (p.L + PACKED_TILE - 1) / PACKED_TILE;
+    a.v_across = p.v_chan != 1;
+    a.by_L = Div(p.L); a.by_nkv = Div(p.nkv); a.by_chunks = Div(a.chunks);
+    const uint32_t flat = (uint32_t)((a.total + NR - 1) / NR);
+    a.k_blocks = p.k ? flat : 0;
+    const uint32_t v_blocks = !p.v ? 0 : a.v_across ? (uint32_t)(p.B * p.nkv * a.chunks) : flat;
+    hipLaunchKernelGGL((k_packed_rows<FMT, T, DH, PACK>), dim3(a.k_blocks + v_blocks), dim3(ROWS_THREADS), 0, st, a);
+}
+template <bool PACK> void rows_launch(const PackedRows& a, hipStream_t st) {
+    auto with = [&](auto fmt, auto dh) {
+        constexpr int F = decltype(fmt)::value, D = decltype(dh)::value;
+        if (a.dtype == 1) run_rows<F, __bf16, D, PACK>(a, st);
+        else run_rows<F, float, D, PACK>(a, st);
+    };
+    auto with_dh = [&](auto fmt) {
+        if (a.dh == 128) with(fmt, std::integral_constant<int, 128>{});
+        else with(fmt, std::integral_constant<int, 64>{});
+    };
+    if (a.fmt == FP4) with_dh(std::integral_constant<int, FP4>{});
+    else with_dh(std::integral_constant<int, FP8>{});
+}
+
+// ---- attention ------------------------------------------------------------------------------------------------------
+// A wavefront a query: a lane a key for the scores, a lane DH / 64 channels for the output.
+template <int FMT, class T, int DH>
+__global__ __launch_bounds__(256) void k_packed_attention(const PackedAttn a) {
+    using TL = Tile<FMT, DH>;
+    constexpr int C = DH / 64;
+    __shared__ float qs[4][DH], ps[4][PACKED_TILE];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t row = (int64_t)blockIdx.x * 4 + wave;
+    if (row >= (int64_t)a.B * a.nh * a.L) return;
+    const int j = (int)(row % a.L), h = (int)(row / a.L % a.nh), b = (int)(row / a.L / a.nh), kvh = h / (a.nh / a.nkv);
+    int P = a.P;
+    if (a.P_seq) {
+        P = a.P_seq[b];
+        P = P < a.rows - a.L ? P : a.rows - a.L;
+    }
+    T* const out = reinterpret_cast<T*>(a.out) + b * a.out_batch + h * a.out_head + j * a.out_row;
+    if (P < 0) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) out[lane * C + c] = (T)0.f;
+        return;
+    }
+    const int p = P + j;
+    const T* const q = reinterpret_cast<const T*>(a.q) + b * a.q_batch + h * a.q_head + j * a.q_row;
+#pragma unroll
+    for (int c = 0; c < C; ++c) qs[wave][lane * C + c] = (float)q[lane * C + c];
+    __builtin_amdgcn_wave_barrier();
+    const uint8_t *const k = a.k + b * a.batch + kvh * a.head, *const v = a.v + b * a.batch + kvh * a.head;
+    const int lo = a.window ? (p - a.window + 1 > 0 ? p - a.window + 1 : 0) : 0;      // rows below: the sinks only
+    float m = -__builtin_huge_valf(), l = 0.f, o[C] = {};
+    for (int t = 0; t * PACKED_TILE <= p; ++t) {
+        if (t * PACKED_TILE >= a.sinks && t < lo / PACKED_TILE) t = lo / PACKED_TILE;
+        const int key = t * PACKED_TILE + lane;
+        const uint8_t* const kt = k + (int64_t)t * TL::BYTES;
+        const uint8_t* const vt = v + (int64_t)t * TL::BYTES;
+        float s = -__builtin_huge_valf();
+        if (key <= p && (key < a.sinks || key >= lo)) {
+            s = 0.f;
+            for (int t8 = 0; t8 < DH / 8; ++t8) {
+                float x[8];
+                decode8(get<FMT, DH>(kt, lane, t8, true), scale_of(kt[TL::k_scale(lane, t8 >> 2)]), x);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s = __builtin_fmaf(x[i], qs[wave][t8 * 8 + i], s);
+            }
+            s *= a.scale_log2;
+        }
+        float mx = s;
+        for (int x = 32; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor(mx, x));
+        const float m_new = fmaxf(m, mx), ref = m_new == -__builtin_huge_valf() ? 0.f : m_new, alpha = __builtin_amdgcn_exp2f(m - ref);
+        const float e = __builtin_amdgcn_exp2f(s - ref);
+        m = m_new;
+        l = l * alpha + e;
+        ps[wave][lane] = e;
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int c = 0; c < C; ++c) o[c] *= alpha;
+        for (int r = 0; r < PACKED_TILE; ++r) {
+            const float w = ps[wave][r];
+            if (w == 0.f) continue;      // hidden rows may hold anything
+            float x[8];
+            decode8(get<FMT, DH>(vt, r, lane * C / 8, false), scale_of(vt[TL::v_scale(r, lane * C / 32)]), x);
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                float y = x[0];
+#pragma unroll
+                for (int i = 1; i < 8; ++i) y = (lane * C + c) % 8 == i ? x[i] : y;
+                o[c] = __builtin_fmaf(w, y, o[c]);
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+    for (int x = 32; x > 0; x >>= 1) l += __shfl_xor(l, x);
+#pragma unroll
+    for (int c = 0; c < C; ++c) out[lane * C + c] = (T)(l > 0.f ? o[c] / l : 0.f);
+}
+
+}  // namespace
+
+void launch_pack_rows(const PackedRows& a, hipStream_t st) { rows_launch<true>(a, st); }
+void launch_unpack_rows(const PackedRows& a, hipStream_t st) { rows_launch<false>(a, st); }
+
+size_t packed_attention_floats(const PackedAttn&) { return 0; }
+
+void launch_packed_attention(const PackedAttn& a, hipStream_t st) {
+    const dim3 grid((unsigned)(((int64_t)a.B * a.nh * a.L + 3) / 4)), block(256);
+    auto with = [&](auto fmt, auto dh) {
+        constexpr int F = decltype(fmt)::value, D = decltype(dh)::value;
+        if (a.dtype == 1) hipLaunchKernelGGL((k_packed_attention<F, __bf16, D>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((k_packed_attention<F, float, D>), grid, block, 0, st, a);
+    };
+    auto with_dh = [&](auto fmt) {
+        if (a.dh == 128) with(fmt, std::integral_constant<int, 128>{});
+        else with(fmt, std::integral_constant<int, 64>{});
+    };
+    if (a.fmt == FP4) with_dh(std::integral_constant<int, FP4>{});
+    else with_dh(std::integral_constant<int, FP8>{});
+}
+
+}  // namespace mulo
