@@ -9,14 +9,19 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmulo.so")
 SOURCES = ["mulo_api.hip", "decide.hip", "elementwise.hip", "gemm.hip", "attention.hip", "forward_f32.hip",
-           "context_attention.hip", "packed.hip", "sample.hip"]
+           "context_attention.hip", "packed.hip", "packed_attention.hip", "sample.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument"]
+
+# The compiler's pass that folds a shift of a byte into an instruction (SDWA) has read that byte behind another instruction's overwriting
+# of its register here (a word whose four bytes become four scales): these sources are built without it.
+NO_SDWA = ["-mllvm", "-amdgpu-sdwa-peephole=0"]
+MORE_FLAGS = {"packed.hip": NO_SDWA, "packed_attention.hip": NO_SDWA}
 
 
 def _compile(src):
     out = os.path.join(OBJ, src.replace(".hip", ".o"))
-    cmd = ["hipcc", *FLAGS, "-c", os.path.join(CSRC, src), "-o", out]
+    cmd = ["hipcc", *FLAGS, *MORE_FLAGS.get(src, []), "-c", os.path.join(CSRC, src), "-o", out]
     r = subprocess.run(cmd, capture_output=True, text=True)
     err = "\n".join(l for l in r.stderr.splitlines() if "packed-fp32-ops" not in l)
     if r.returncode != 0:

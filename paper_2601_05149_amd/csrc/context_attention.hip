@@ -76,7 +76,7 @@ template <> struct Chunk<float> {
 };
 
 constexpr float LAZY_EXP = 8.0f;     // the reference of the exponentials moves once the maximum has outgrown it by 2^8 (see attention.hip)
-constexpr int MAX_SLOTS = 64;        // shares of a query that k_context_join joins: a lane each
+constexpr int MAX_SLOTS = MAX_SHARES;      // shares of a query that k_context_join joins: a lane each
 
 // How a launch is laid out (host).
 struct Plan {
@@ -827,6 +827,19 @@ size_t context_attention_floats(const ContextAttn& a) {
     const Plan p = make_plan(a, a.dtype == 1 ? 2 : 4, MAX_SLOTS * slot_floats);
     const int slots = p.split + (p.stacked ? p.prefix_split : 0);
     return slots > 1 ? (size_t)(slots * slot_floats) : 0;
+}
+
+void launch_join_shares(const ContextAttn& c, int shares, hipStream_t st) {
+    Args a{};
+    static_cast<ContextAttn&>(a) = c;
+    a.ml = c.part + (int64_t)shares * c.B * c.nh * c.L * c.dh;
+    if (c.dtype == 1) {
+        if (c.dh == 128) join<__bf16, 128>(a, shares, st);
+        else join<__bf16, 64>(a, shares, st);
+    } else {
+        if (c.dh == 128) join<float, 128>(a, shares, st);
+        else join<float, 64>(a, shares, st);
+    }
 }
 
 void launch_context_attention(const ContextAttn& a, hipStream_t st) {

@@ -230,6 +230,10 @@ struct ContextAttn {
 };
 size_t context_attention_floats(const ContextAttn& a);   // scratch it runs fastest with
 void launch_context_attention(const ContextAttn& a, hipStream_t st);
+// Joins `shares` partial results of every query, part [shares][B nh L][dh] (not normalised) and behind them [shares][B nh L] pairs of
+// maximum and sum, into out; of `a` it takes dtype, B, L, nh, dh, out, P_seq and part.
+constexpr int MAX_SHARES = 64;
+void launch_join_shares(const ContextAttn& a, int shares, hipStream_t st);
 
 // ---- a packed cache (packed.hip) ----
 constexpr int PACKED_TILE = 64, PACKED_GROUP = 32;      // rows of a tile, channels of a group

@@ -1,10 +1,11 @@
-// A cache in 4 or 8 bits: rows packed as they are written, read back, and attended to.  (The formats and the tiles: include/mulo.h.)
+// A cache in 4 or 8 bits: rows packed as they are written, and read back.  (The formats and the tiles: include/mulo.h.)
 #include <hip/hip_bf16.h>
 
 #include <type_traits>
 
 #include "index_div.h"
 #include "mulo_internal.h"
+#include "packed_tile.h"
 
 namespace mulo {
 namespace {
@@ -14,18 +15,6 @@ typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(2))) short i16x2;
-
-constexpr int FP4 = 0, FP8 = 1;
-
-// ---- places in a tile, in bytes behind its start --------------------------------------------------------------------
-template <int FMT, int DH> struct Tile {
-    static constexpr int ROW = FMT == FP4 ? DH / 2 : DH;                 // bytes of a row's codes
-    static constexpr int G = DH / PACKED_GROUP, CODES = PACKED_TILE * ROW, BYTES = CODES + PACKED_TILE * G;
-    static constexpr int UNIT = ROW / 16;                                // bytes of the values of one row that lie together
-    static __host__ __device__ constexpr int k_scale(int r, int g) { return CODES + ((r & 15) * G + g) * 4 + (r >> 4); }
-    static __host__ __device__ constexpr int v_code(int r, int unit) { return (r >> 2) * 4 * ROW + unit * 4 * UNIT + (r & 3) * UNIT; }
-    static __host__ __device__ constexpr int v_scale(int r, int g) { return CODES + (((r >> 2 & 3) * G + g) * 4 + (r >> 4)) * 4 + (r & 3); }
-};
 
 // ---- eight numbers and their codes ---------------------------------------------------------------------------------
 // The byte 127 + e of a group whose largest |x| has these bits: e is the smallest integer with |x| <= T 2^e, T = 7 = 1.75 2^2 or
@@ -248,102 +237,9 @@ template <bool PACK> void rows_launch(const PackedRows& a, hipStream_t st) {
     else with_dh(std::integral_constant<int, FP8>{});
 }
 
-// ---- attention ------------------------------------------------------------------------------------------------------
-// A wavefront a query: a lane a key for the scores, a lane DH / 64 channels for the output.
-template <int FMT, class T, int DH>
-__global__ __launch_bounds__(256) void k_packed_attention(const PackedAttn a) {
-    using TL = Tile<FMT, DH>;
-    constexpr int C = DH / 64;
-    __shared__ float qs[4][DH], ps[4][PACKED_TILE];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t row = (int64_t)blockIdx.x * 4 + wave;
-    if (row >= (int64_t)a.B * a.nh * a.L) return;
-    const int j = (int)(row % a.L), h = (int)(row / a.L % a.nh), b = (int)(row / a.L / a.nh), kvh = h / (a.nh / a.nkv);
-    int P = a.P;
-    if (a.P_seq) {
-        P = a.P_seq[b];
-        P = P < a.rows - a.L ? P : a.rows - a.L;
-    }
-    T* const out = reinterpret_cast<T*>(a.out) + b * a.out_batch + h * a.out_head + j * a.out_row;
-    if (P < 0) {
-#pragma unroll
-        for (int c = 0; c < C; ++c) out[lane * C + c] = (T)0.f;
-        return;
-    }
-    const int p = P + j;
-    const T* const q = reinterpret_cast<const T*>(a.q) + b * a.q_batch + h * a.q_head + j * a.q_row;
-#pragma unroll
-    for (int c = 0; c < C; ++c) qs[wave][lane * C + c] = (float)q[lane * C + c];
-    __builtin_amdgcn_wave_barrier();
-    const uint8_t *const k = a.k + b * a.batch + kvh * a.head, *const v = a.v + b * a.batch + kvh * a.head;
-    const int lo = a.window ? (p - a.window + 1 > 0 ? p - a.window + 1 : 0) : 0;      // rows below: the sinks only
-    float m = -__builtin_huge_valf(), l = 0.f, o[C] = {};
-    for (int t = 0; t * PACKED_TILE <= p; ++t) {
-        if (t * PACKED_TILE >= a.sinks && t < lo / PACKED_TILE) t = lo / PACKED_TILE;
-        const int key = t * PACKED_TILE + lane;
-        const uint8_t* const kt = k + (int64_t)t * TL::BYTES;
-        const uint8_t* const vt = v + (int64_t)t * TL::BYTES;
-        float s = -__builtin_huge_valf();
-        if (key <= p && (key < a.sinks || key >= lo)) {
-            s = 0.f;
-            for (int t8 = 0; t8 < DH / 8; ++t8) {
-                float x[8];
-                decode8(get<FMT, DH>(kt, lane, t8, true), scale_of(kt[TL::k_scale(lane, t8 >> 2)]), x);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) s = __builtin_fmaf(x[i], qs[wave][t8 * 8 + i], s);
-            }
-            s *= a.scale_log2;
-        }
-        float mx = s;
-        for (int x = 32; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor(mx, x));
-        const float m_new = fmaxf(m, mx), ref = m_new == -__builtin_huge_valf() ? 0.f : m_new, alpha = __builtin_amdgcn_exp2f(m - ref);
-        const float e = __builtin_amdgcn_exp2f(s - ref);
-        m = m_new;
-        l = l * alpha + e;
-        ps[wave][lane] = e;
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int c = 0; c < C; ++c) o[c] *= alpha;
-        for (int r = 0; r < PACKED_TILE; ++r) {
-            const float w = ps[wave][r];
-            if (w == 0.f) continue;      // hidden rows may hold anything
-            float x[8];
-            decode8(get<FMT, DH>(vt, r, lane * C / 8, false), scale_of(vt[TL::v_scale(r, lane * C / 32)]), x);
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-                float y = x[0];
-#pragma unroll
-                for (int i = 1; i < 8; ++i) y = (lane * C + c) % 8 == i ? x[i] : y;
-                o[c] = __builtin_fmaf(w, y, o[c]);
-            }
-        }
-        __builtin_amdgcn_wave_barrier();
-    }
-    for (int x = 32; x > 0; x >>= 1) l += __shfl_xor(l, x);
-#pragma unroll
-    for (int c = 0; c < C; ++c) out[lane * C + c] = (T)(l > 0.f ? o[c] / l : 0.f);
-}
-
 }  // namespace
 
 void launch_pack_rows(const PackedRows& a, hipStream_t st) { rows_launch<true>(a, st); }
 void launch_unpack_rows(const PackedRows& a, hipStream_t st) { rows_launch<false>(a, st); }
-
-size_t packed_attention_floats(const PackedAttn&) { return 0; }
-
-void launch_packed_attention(const PackedAttn& a, hipStream_t st) {
-    const dim3 grid((unsigned)(((int64_t)a.B * a.nh * a.L + 3) / 4)), block(256);
-    auto with = [&](auto fmt, auto dh) {
-        constexpr int F = decltype(fmt)::value, D = decltype(dh)::value;
-        if (a.dtype == 1) hipLaunchKernelGGL((k_packed_attention<F, __bf16, D>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((k_packed_attention<F, float, D>), grid, block, 0, st, a);
-    };
-    auto with_dh = [&](auto fmt) {
-        if (a.dh == 128) with(fmt, std::integral_constant<int, 128>{});
-        else with(fmt, std::integral_constant<int, 64>{});
-    };
-    if (a.fmt == FP4) with_dh(std::integral_constant<int, FP4>{});
-    else with_dh(std::integral_constant<int, FP8>{});
-}
 
 }  // namespace mulo
