@@ -50,14 +50,15 @@ constexpr int NW = 4;                // wavefronts of a workgroup
 
 struct Plan {
     int nq;            // blocks of 16 queries of a wavefront
-    bool shared;       // the wavefronts of a workgroup have the same queries, and tiles of keys in turn; else queries of their own
+    int waves;         // k_packed_few: wavefronts of a workgroup; 0: k_packed_block
     int tiles;         // workgroups of the queries of a (sequence, key head)
     int split;         // shares of the keys
 };
 struct Args : PackedAttn, Plan {
     float* ml;         // [split][B nh L] pairs of maximum and sum, behind the [split][B nh L][dh] outputs in part
     int group, n, shares;      // heads of a key head, queries of a (sequence, key head), workgroups of a share
-    Div by_nkv, by_L, by_tiles, by_shares;
+    int round;
+    Div by_nkv, by_L, by_round, by_in_round, by_shares;
 };
 
 // 16 codes bytes a lane feeds the instruction; two codes at once as bf16.  SEL: which pair of the word
@@ -74,158 +75,88 @@ __device__ __forceinline__ float max_of_groups(float x) {      // over the four 
     return fmaxf(x, __shfl_xor(x, 32));
 }
 
-constexpr int waves_per_simd(int fmt, int esz, int dh, int nq) { return esz == 4 && dh == 128 ? (nq == 1 ? 2 : 1) : nq == 1 && fmt == FP4 ? 3 : 2; }
-
-// Blocks of 16 rows that a wavefront goes over at a time: a tile, or half of one where the codes would take more registers than there are.
-constexpr int blocks_of_step(int fmt, int esz, int dh, int nq) { return esz == 2 && fmt == FP8 && dh == 128 && nq > 1 ? 2 : 4; }
-
-template <int FMT, class T, int DH, int NQ, bool SHARED>
-__global__ __launch_bounds__(64 * NW, waves_per_simd(FMT, sizeof(T), DH, NQ)) void k_packed_attention(const Args a) {
+// ---- what a lane holds of a step of 16 NX rows -----------------------------------------------------------------------
+constexpr int key_words(int fmt, int esz, int dh) { return esz == 2 ? (fmt == FP8 && dh == 128 ? 8 : 4) : (fmt == FP4 ? dh / 2 : dh) / 16; }
+template <int N> __device__ __forceinline__ void load_words(uint32_t* w, const uint8_t* p, int apart) {      // 8 bytes, or 16-byte pieces `apart` bytes apart
+    if constexpr (N == 2) {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+        w[0] = x.x; w[1] = x.y;
+    } else {
+#pragma unroll
+        for (int e = 0; e < N / 4; ++e) {
+            const u32x4 x = *reinterpret_cast<const u32x4*>(p + e * apart);
+            w[4 * e] = x.x; w[4 * e + 1] = x.y; w[4 * e + 2] = x.z; w[4 * e + 3] = x.w;
+        }
+    }
+}
+// Keys: row 16 x + c of the codes that the lane's quarter of the contraction takes.  bf16: as the scaled instruction has them (of 8 bits,
+// 16 g .. and, heads of 128, 64 + 16 g ..; of 4 bits 32 g ..; heads of 64 repeat their channels for the query's second term); float32:
+// d_h / 4 channels next to each other.
+template <int FMT, class T, int DH, int NX> struct Keys {
     using TL = Tile<FMT, DH>;
-    constexpr bool BF16 = sizeof(T) == 2;
-    constexpr int U = DH / 16;                        // channels of the output that a lane's rows of O^T step over, instructions of the second product
-    constexpr int VW = TL::UNIT;                      // words of four rows' values of a lane: 4 UNIT bytes
-    constexpr int KW = BF16 ? (FMT == FP8 && DH == 128 ? 8 : 4) : TL::ROW / 16;      // words of a key's codes of a lane
-    constexpr int NC = DH / 32;                       // float32: chunks of 8 channels of a lane
-    constexpr int NX = blocks_of_step(FMT, sizeof(T), DH, NQ), ROWS = 16 * NX;      // blocks of 16 rows, rows of a step
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c16 = lane & 15, lg = lane >> 4;
-
-    // ---- which queries, which share of which keys.  All query tiles of a (sequence, key head) on one XCD, next to each other; long ones first
-    const int id = blockIdx.x, split = a.by_shares.of(id), bid = id - split * a.shares;
-    const int nbh = a.B * a.nkv, by8 = (nbh & 7) == 0, sq = by8 ? bid >> 3 : bid, s_bh = a.by_tiles.of(sq);
-    const int qt = a.tiles - 1 - (sq - s_bh * a.tiles), bh = by8 ? s_bh * 8 + (bid & 7) : s_bh;
-    const int b = a.by_nkv.of(bh), kvh = bh - b * a.nkv;
-    const int r0 = (SHARED ? qt : qt * NW + wave) * (16 * NQ), n = a.n;
-    if (!SHARED && r0 >= n) return;
-    int P = a.P;
-    if (a.P_seq) {
-        P = a.P_seq[b];
-        P = P < a.rows - a.L ? P : a.rows - a.L;
-    }
-    int row_h[NQ], row_j[NQ];      // of this lane's queries (past the end the last one again: not stored)
-    bool live[NQ];
+    static constexpr bool BF16 = sizeof(T) == 2;
+    static constexpr int KW = key_words(FMT, sizeof(T), DH), SUB = 4 / NX;      // words of a row, steps of a tile
+    uint32_t w[NX][KW], scale;
+    __device__ __forceinline__ void load(const uint8_t* base, int t, int c16, int lg) {
+        const uint8_t* const at = base + (int64_t)(t / SUB) * TL::BYTES;
+        const int sub = t % SUB;
+        const uint32_t off = c16 * TL::ROW + (!BF16 ? lg * (TL::ROW / 4) : FMT == FP4 && DH == 64 ? (lg & 1) * 16 : lg * 16);
 #pragma unroll
-    for (int q = 0; q < NQ; ++q) {
-        const int r = r0 + q * 16 + c16, rc = r < n ? r : n - 1, h = a.by_L.of(rc);
-        live[q] = r < n;
-        row_h[q] = kvh * a.group + h;
-        row_j[q] = rc - h * a.L;
+        for (int x = 0; x < NX; ++x) load_words<KW>(w[x], at + off + (sub * NX + x) * 16 * TL::ROW, BF16 ? 64 : 16);
+        const uint32_t s_off = TL::k_scale(0, 0) + (c16 * TL::G + (DH == 128 ? lg : BF16 ? lg & 1 : lg >> 1)) * 4;
+        if constexpr (SUB == 1) scale = *reinterpret_cast<const uint32_t*>(at + s_off);
+        else scale = *reinterpret_cast<const uint16_t*>(at + s_off + 2 * sub);
     }
-    const int64_t all_rows = (int64_t)a.B * a.nh * a.L;
-    const bool partial = a.split > 1;
-    auto out_row = [&](int h, int j) { return ((int64_t)b * a.nh + h) * a.L + j; };
-    auto store4 = [&](int h, int j, int c, f32x4 w) {      // channels c .. c + 3 of a query
-        T* const op = reinterpret_cast<T*>(a.out) + b * a.out_batch + h * a.out_head + j * a.out_row + c;
-        if constexpr (BF16) {
-            bf16x4 t;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) t[e] = (__bf16)w[e];
-            *reinterpret_cast<bf16x4*>(op) = t;
-        } else {
-            *reinterpret_cast<f32x4*>(op) = w;
-        }
-    };
-
-    // ---- which steps: the head [0, n1) of the sinks and from t2 on the window
-    int p_min, p_max;
-    {
-        const int rb = (r0 + 16 * NQ < n ? r0 + 16 * NQ : n) - 1, ha = a.by_L.of(r0), hb = a.by_L.of(rb);      // within a head the queries are consecutive
-        p_min = P + (ha == hb ? r0 - ha * a.L : 0);
-        p_max = P + (ha == hb ? rb - hb * a.L : a.L - 1);
-    }
-    int lo = 0, n1 = 0;
-    if (a.window) {
-        lo = p_min - a.window + 1 > 0 ? p_min - a.window + 1 : 0;
-        n1 = ((a.sinks < lo ? a.sinks : lo) + ROWS - 1) / ROWS;
-    }
-    const int t2 = lo / ROWS > n1 ? lo / ROWS : n1, more = p_max / ROWS + 1 - t2;
-    const int n_steps = P < 0 ? 0 : n1 + (more > 0 ? more : 0);
-    const int per = (n_steps + a.split - 1) / a.split, t_begin = split * per, t_end = t_begin + per < n_steps ? t_begin + per : n_steps;
-    if (t_begin >= t_end) {      // the whole workgroup (SHARED) or wavefront: nothing to see
-        if (!SHARED || wave == 0) {
-#pragma unroll
-            for (int q = 0; q < NQ; ++q)
-                if (live[q]) {
-                    if (partial) {
-                        if (lg == 0) *reinterpret_cast<float2*>(a.ml + 2 * (split * all_rows + out_row(row_h[q], row_j[q]))) = make_float2(MINUS_INF, 0.f);
-                    } else {
-#pragma unroll
-                        for (int c = 0; c < DH / 4; c += 4) store4(row_h[q], row_j[q], lg * (DH / 4) + c, f32x4{0.f, 0.f, 0.f, 0.f});
-                    }
-                }
-        }
-        return;
-    }
-    auto step_of = [&](int i) { return i < n1 ? i : t2 + i - n1; };
-
-    // ---- loads of a step
-    const uint8_t* const kb = a.k + b * a.batch + kvh * a.head;
-    const uint8_t* const vb = a.v + b * a.batch + kvh * a.head;
-    const uint32_t k_off = c16 * TL::ROW + (!BF16 ? lg * (TL::ROW / 4) : FMT == FP4 && DH == 64 ? (lg & 1) * 16 : lg * 16);
-    const uint32_t ks_off = TL::k_scale(0, 0) + (c16 * TL::G + (DH == 128 ? lg : BF16 ? lg & 1 : lg >> 1)) * 4;
-    const uint32_t v_off = lg * (4 * TL::ROW) + c16 * (4 * TL::UNIT);
-    const uint32_t vs_off = TL::v_scale(0, 0) + (lg * TL::G + c16 * U / PACKED_GROUP) * 16;
-    uint32_t kw[NX][KW], vw[NX][VW], ks, vs[NX];
-    constexpr int SUB = 4 / NX;      // steps of a tile
-    auto load_k = [&](int t) {
-        const uint8_t* const at = kb + (int64_t)(t / SUB) * TL::BYTES;
+};
+// Values: of rows 16 x + 4 g .. + 3 the channels c u .. + u - 1 (words r UNIT / 4 .. of row r; UNIT 2: two rows a word), and those rows' scales
+template <int FMT, int DH, int NX> struct Values {
+    using TL = Tile<FMT, DH>;
+    static constexpr int VW = TL::UNIT, SUB = 4 / NX;
+    uint32_t w[NX][VW], scale[NX];
+    static __device__ __forceinline__ uint32_t offset(int c16, int lg) { return lg * (4 * TL::ROW) + c16 * (4 * TL::UNIT); }
+    static __device__ __forceinline__ uint32_t scale_offset(int c16, int lg) { return TL::v_scale(0, 0) + (lg * TL::G + c16 * (DH / 16) / PACKED_GROUP) * 16; }
+    __device__ __forceinline__ void load(const uint8_t* base, int t, int c16, int lg) {
+        const uint8_t* const at = base + (int64_t)(t / SUB) * TL::BYTES;
         const int sub = t % SUB;
 #pragma unroll
-        for (int x = 0; x < NX; ++x) {
-            const uint8_t* const p = at + k_off + (sub * NX + x) * 16 * TL::ROW;
-            if constexpr (KW == 2) {
-                const u32x2 w = *reinterpret_cast<const u32x2*>(p);
-                kw[x][0] = w.x; kw[x][1] = w.y;
-            } else {
-#pragma unroll
-                for (int e = 0; e < KW / 4; ++e) {
-                    const u32x4 w = *reinterpret_cast<const u32x4*>(p + e * (BF16 ? 64 : 16));
-                    kw[x][4 * e] = w.x; kw[x][4 * e + 1] = w.y; kw[x][4 * e + 2] = w.z; kw[x][4 * e + 3] = w.w;
-                }
-            }
-        }
-        if constexpr (SUB == 1) ks = *reinterpret_cast<const uint32_t*>(at + ks_off);
-        else ks = *reinterpret_cast<const uint16_t*>(at + ks_off + 2 * sub);
-    };
-    auto load_v = [&](int t) {
-        const uint8_t* const at = vb + (int64_t)(t / SUB) * TL::BYTES;
-        const int sub = t % SUB;
-#pragma unroll
-        for (int x = 0; x < NX; ++x) {
-            const uint8_t* const p = at + v_off + (sub * NX + x) * 16 * TL::ROW;
-            if constexpr (VW == 2) {
-                const u32x2 w = *reinterpret_cast<const u32x2*>(p);
-                vw[x][0] = w.x; vw[x][1] = w.y;
-            } else {
-#pragma unroll
-                for (int e = 0; e < VW / 4; ++e) {
-                    const u32x4 w = *reinterpret_cast<const u32x4*>(p + e * 16);
-                    vw[x][4 * e] = w.x; vw[x][4 * e + 1] = w.y; vw[x][4 * e + 2] = w.z; vw[x][4 * e + 3] = w.w;
-                }
-            }
-        }
-        if constexpr (NX == 4) {
-            const u32x4 w = *reinterpret_cast<const u32x4*>(at + vs_off);
-            vs[0] = w.x; vs[1] = w.y; vs[2] = w.z; vs[3] = w.w;
-        } else {
-            const u32x2 w = *reinterpret_cast<const u32x2*>(at + vs_off + 8 * sub);
-            vs[0] = w.x; vs[1] = w.y;
-        }
-    };
-    const int step = SHARED ? NW : 1, i0 = t_begin + (SHARED ? wave : 0);
-    if (i0 < t_end) {
-        load_k(step_of(i0));
-        load_v(step_of(i0));
+        for (int x = 0; x < NX; ++x) load_words<VW>(w[x], at + offset(c16, lg) + (sub * NX + x) * 16 * TL::ROW, 16);
+        if constexpr (NX == 4) load_words<4>(scale, at + scale_offset(c16, lg), 16);
+        else load_words<2>(scale, at + scale_offset(c16, lg) + 8 * sub, 16);
     }
-
-    // ---- the queries
-    i32x8 qh[NQ], ql[NQ];         // bf16: the two terms; heads of 64: both in qh
-    int qs[NQ];                   // their scales, bytes 0 and 1
-    bf16x8 q3[NQ][3][NC];         // float32: three terms
+    __device__ __forceinline__ void load_block(const uint8_t* base, int t, int x, int c16, int lg) {      // NX == 1: block x of tile t
+        const uint8_t* const at = base + (int64_t)t * TL::BYTES;
+        load_words<VW>(w[0], at + offset(c16, lg) + x * 16 * TL::ROW, 16);
+        scale[0] = *reinterpret_cast<const uint32_t*>(at + scale_offset(c16, lg) + 4 * x);
+    }
+    __device__ __forceinline__ void clear(int x, int r, bool keep) {      // row r of the four becomes zeros
+        if constexpr (TL::UNIT == 2) {
+            w[x][r >> 1] &= keep ? 0xFFFFFFFFu : (r & 1) ? 0x0000FFFFu : 0xFFFF0000u;
+        } else {
 #pragma unroll
-    for (int q = 0; q < NQ; ++q) {
-        const T* const qp = reinterpret_cast<const T*>(a.q) + b * a.q_batch + row_h[q] * a.q_head + row_j[q] * a.q_row;
-        if constexpr (BF16) {
+            for (int e = 0; e < VW / 4; ++e) w[x][r * (VW / 4) + e] = keep ? w[x][r * (VW / 4) + e] : 0u;
+        }
+        scale[x] = keep ? scale[x] : (scale[x] & ~(0xFFu << (8 * r))) | 0x7Fu << (8 * r);
+    }
+    // channels 2 PR and 2 PR + 1 of the lane's, of row R of block x
+    template <int PR, int R> __device__ __forceinline__ uint32_t two(int x) const {
+        const float s = scale_of(scale[x], R);
+        if constexpr (FMT == FP4) {
+            if constexpr (DH == 128) return pair<FMT, PR>(w[x][R], s);
+            else return pair<FMT, 2 * (R & 1) + PR>(w[x][R / 2], s);
+        } else {
+            if constexpr (DH == 128) return pair<FMT, PR & 1>(w[x][2 * R + PR / 2], s);
+            else return pair<FMT, PR>(w[x][R], s);
+        }
+    }
+};
+// 16 queries, one a lane: the terms of its channels
+template <class T, int DH> struct Query {
+    static constexpr int NC = DH / 32;      // float32: chunks of 8 channels of a lane
+    i32x8 hi, lo;                // bf16: the two terms; heads of 64: both in hi
+    int scale;                   // bytes 0 and 1: theirs
+    bf16x8 term[3][NC];          // float32: three terms
+    __device__ __forceinline__ void load(const T* qp, int c16, int lg) {
+        if constexpr (sizeof(T) == 2) {
             // a lane's codes are channels 16 g .. + 15, of heads of 128 also 64 + 16 g .. + 15: halves of the groups g / 2 and 2 + g / 2
             constexpr int NP = DH / 64;
             uint32_t most[NP];
@@ -257,27 +188,27 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(FMT, sizeof(T), DH, NQ)) vo
                     i16x2 w = {0, 0}, z = {0, 0};
                     w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, v[0], v[1], s_hi, false);
                     w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, v[2], v[3], s_hi, true);
-                    const uint32_t hi = __builtin_bit_cast(uint32_t, w);
-                    const f32x2 d0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, s_hi, false), d1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, s_hi, true);
+                    const uint32_t h = __builtin_bit_cast(uint32_t, w);
+                    const f32x2 d0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(h, s_hi, false), d1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(h, s_hi, true);
                     z = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(z, v[0] - d0.x, v[1] - d0.y, s_lo, false);
                     z = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(z, v[2] - d1.x, v[3] - d1.y, s_lo, true);
-                    codes[0][4 * y + e] = (int)hi;
+                    codes[0][4 * y + e] = (int)h;
                     codes[1][4 * y + e] = (int)__builtin_bit_cast(uint32_t, z);
                 }
             }
             if constexpr (DH == 128) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) { qh[q][e] = codes[0][e]; ql[q][e] = codes[1][e]; }
+                for (int e = 0; e < 8; ++e) { hi[e] = codes[0][e]; lo[e] = codes[1][e]; }
                 // the instruction takes the scale of group g from the lanes g
                 const int s1 = __shfl((int)most[0], c16 + 32), s2 = __shfl((int)most[1], c16);
                 const int s = lg == 0 ? (int)most[0] : lg == 1 ? s1 : lg == 2 ? s2 : (int)most[1];
-                qs[q] = s | (s - 4) << 8;
+                scale = s | (s - 4) << 8;
             } else {
                 // ... which are here those of the two groups' first terms, then of their second ones
 #pragma unroll
-                for (int e = 0; e < 4; ++e) { qh[q][e] = codes[0][e]; qh[q][4 + e] = codes[1][e]; }
+                for (int e = 0; e < 4; ++e) { hi[e] = codes[0][e]; hi[4 + e] = codes[1][e]; }
                 const int s = __shfl((int)most[0], c16 + 32 * (lg & 1));
-                qs[q] = lg < 2 ? s : s - 4;
+                scale = lg < 2 ? s : s - 4;
             }
         } else {
 #pragma unroll
@@ -288,14 +219,238 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(FMT, sizeof(T), DH, NQ)) vo
                     float x = e < 4 ? x0[e & 3] : x1[e & 3];
 #pragma unroll
                     for (int y = 0; y < 3; ++y) {
-                        q3[q][y][c][e] = (__bf16)x;
-                        x -= (float)q3[q][y][c][e];
+                        term[y][c][e] = (__bf16)x;
+                        x -= (float)term[y][c][e];
                     }
                 }
             }
         }
     }
+};
+// scores of a step: s[x][q][i] of key 16 x + 4 g + i
+template <int FMT, class T, int DH, int NX, int NQ>
+__device__ __forceinline__ void scores(f32x4 (&s)[NX][NQ], const Keys<FMT, T, DH, NX>& k, const Query<T, DH> (&query)[NQ]) {
+    static_for<NX>([&](auto xc) {
+        constexpr int x = decltype(xc)::value;
+        if constexpr (sizeof(T) == 2) {
+            constexpr int KW = Keys<FMT, T, DH, NX>::KW, CODE = FMT == FP4 ? 4 : 0;
+            i32x8 kf;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) kf[e] = (int)k.w[x][e & (KW - 1)];      // (of 4 bits the instruction takes four words)
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) {
+                s[x][q] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, query[q].hi, f32x4{0.f, 0.f, 0.f, 0.f}, CODE, 0, x, (int)k.scale, 0, query[q].scale);
+                if constexpr (DH == 128) s[x][q] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, query[q].lo, s[x][q], CODE, 0, x, (int)k.scale, 1, query[q].scale);
+            }
+        } else {
+            const float sc = scale_of(k.scale, x);
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) s[x][q] = f32x4{0.f, 0.f, 0.f, 0.f};
+            static_for<DH / 32>([&](auto cc) {
+                constexpr int c = decltype(cc)::value;
+                u32x4 w;
+                static_for<4>([&](auto ec) {
+                    constexpr int e = decltype(ec)::value;
+                    if constexpr (FMT == FP4) w[e] = pair<FMT, e>(k.w[x][c], sc);
+                    else w[e] = pair<FMT, e & 1>(k.w[x][2 * c + e / 2], sc);
+                });
+#pragma unroll
+                for (int q = 0; q < NQ; ++q)
+#pragma unroll
+                    for (int y = 0; y < 3; ++y) s[x][q] = mma(__builtin_bit_cast(bf16x8, w), query[q].term[y][c], s[x][q]);
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        }
+    });
+}
+// The compiler may move these instructions to where their results are used, also behind a branch that not all lanes take; all lanes' operands
+// are needed.
+template <int N, int NQ> __device__ __forceinline__ void stay(f32x4 (&s)[N][NQ]) {
+#pragma unroll
+    for (int x = 0; x < N; ++x)
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) asm volatile("" : "+v"(s[x][q]));
+}
+// -inf for the keys of a step (first key k0) that a lane's query (at row p) does not see
+template <int NX> __device__ __forceinline__ bool sees(int key, int p, int before, int head) { return (key <= p) & ((key > before) | (key < head)); }
+template <int NX, int NQ> __device__ __forceinline__ void hide(f32x4 (&s)[NX][NQ], const PackedAttn& a, const int (&row)[NQ], int k0, int lg) {
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+        const int p = row[q] - k0 - 4 * lg, before = a.window ? p - a.window : -1 - 16 * NX, head = a.sinks - k0 - 4 * lg;
+#pragma unroll
+        for (int x = 0; x < NX; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[x][q][e] = sees<NX>(16 * x + e, p, before, head) ? s[x][q][e] : MINUS_INF;
+    }
+}
+// Moves the reference of the exponentials where some query's maximum has outgrown it, and what has been added up with it
+template <int NX, int NQ, int U> __device__ __forceinline__ void refer(const f32x4 (&s)[NX][NQ], float scale_log2, float (&m_run)[NQ], float (&l_run)[NQ], f32x4 (&o)[U][NQ]) {
+    float mx[NQ];
+    bool up = false;
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+        mx[q] = s[0][q][0];
+#pragma unroll
+        for (int x = 0; x < NX; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mx[q] = fmaxf(mx[q], s[x][q][e]);
+        mx[q] *= scale_log2;
+        up |= mx[q] > m_run[q] + LAZY_EXP;
+    }
+    if (__any(up)) {
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            const float most = max_of_groups(mx[q]), m_new = most > m_run[q] + LAZY_EXP ? most : m_run[q];
+            const float alpha = m_new == MINUS_INF ? 1.f : __builtin_amdgcn_exp2f(m_run[q] - m_new);
+            m_run[q] = m_new;
+            l_run[q] *= alpha;
+#pragma unroll
+            for (int m = 0; m < U; ++m) o[m][q] *= alpha;
+        }
+    }
+}
+// Exponential e of keys 32 half .. + 31 of a lane, as the terms of the second product's operand
+template <bool PIN, int NX, int NQ, int NT> __device__ __forceinline__ void exponential(bf16x8 (&pf)[NQ][NT], const f32x4 (&s)[NX][NQ], int half, int e, float scale_log2, const float (&m_run)[NQ], float (&l_run)[NQ]) {
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+        const float ref = m_run[q] == MINUS_INF ? 0.f : m_run[q];      // no key seen yet: every exponential is 0
+        float x = s[2 * half + (e >> 2)][q][e & 3];
+        if (PIN) asm volatile("" : "+v"(x));      // here, among the matrix instructions of its slice
+        float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x, scale_log2, -ref));
+        l_run[q] += p;
+#pragma unroll
+        for (int y = 0; y < NT; ++y) {
+            pf[q][y][e] = (__bf16)p;
+            if (y + 1 < NT) p -= (float)pf[q][y][e];
+        }
+    }
+}
+template <int NX, int NQ, int NT> __device__ __forceinline__ void exponentials(bf16x8 (&pf)[NQ][NT], const f32x4 (&s)[NX][NQ], int half, float scale_log2, const float (&m_run)[NQ], float (&l_run)[NQ]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) exponential<false>(pf, s, half, e, scale_log2, m_run, l_run);
+}
 
+// ---- where a workgroup is --------------------------------------------------------------------------------------------
+struct Place { int split, qt, b, kvh, P; };
+// All query tiles of a (sequence, key head) on one XCD, next to each other; long ones first
+__device__ __forceinline__ Place place(const Args& a) {
+    Place w;
+    const int id = blockIdx.x;
+    w.split = a.by_shares.of(id);
+    const int bid = id - w.split * a.shares, nbh = a.B * a.nkv, by8 = (nbh & 7) == 0, sq = by8 ? bid >> 3 : bid, n_bh = by8 ? nbh >> 3 : nbh;
+    const int grp = a.by_round.of(sq), in = sq - grp * (a.round * a.tiles), first = grp * a.round, left = n_bh - first;
+    int t, x;
+    if (left >= a.round) { t = a.by_in_round.of(in); x = in - t * a.round; } else { t = in / left; x = in - t * left; }
+    w.qt = a.tiles - 1 - t;
+    const int s_bh = first + x, bh = by8 ? s_bh * 8 + (bid & 7) : s_bh;
+    w.b = a.by_nkv.of(bh);
+    w.kvh = bh - w.b * a.nkv;
+    w.P = a.P;
+    if (a.P_seq) {
+        const int P = a.P_seq[w.b];
+        w.P = P < a.rows - a.L ? P : a.rows - a.L;
+    }
+    return w;
+}
+// rows of the first and the last of queries r0 .. r0 + n - 1 (within a head they are consecutive)
+__device__ __forceinline__ void span(const Args& a, int P, int r0, int n, int& p_min, int& p_max) {
+    const int rb = (r0 + n < a.n ? r0 + n : a.n) - 1, ha = a.by_L.of(r0), hb = a.by_L.of(rb);
+    p_min = P + (ha == hb ? r0 - ha * a.L : 0);
+    p_max = P + (ha == hb ? rb - hb * a.L : a.L - 1);
+}
+// The steps of ROWS rows that queries at p_min .. p_max see: the head [0, head) of the sinks and from `from` on the window; of them a share
+struct Steps {
+    int head, from, begin, end;
+    __device__ __forceinline__ int of(int i) const { return i < head ? i : from + i - head; }
+};
+template <int ROWS> __device__ __forceinline__ Steps steps(const Args& a, int P, int p_min, int p_max, int split) {
+    Steps w;
+    int lo = 0;
+    w.head = 0;
+    if (a.window) {
+        lo = p_min - a.window + 1 > 0 ? p_min - a.window + 1 : 0;
+        w.head = ((a.sinks < lo ? a.sinks : lo) + ROWS - 1) / ROWS;
+    }
+    w.from = lo / ROWS > w.head ? lo / ROWS : w.head;
+    const int more = p_max / ROWS + 1 - w.from, n = P < 0 ? 0 : w.head + (more > 0 ? more : 0), per = (n + a.split - 1) / a.split;
+    w.begin = split * per;
+    w.end = w.begin + per < n ? w.begin + per : n;
+    return w;
+}
+// some query at p_min .. p_max does not see some key of k0 .. k0 + n - 1
+__device__ __forceinline__ bool cut(const Args& a, int k0, int n, int p_min, int p_max) {
+    return k0 + n - 1 > p_min || (a.window && k0 + n > a.sinks && k0 <= p_max - a.window);
+}
+template <class T> __device__ __forceinline__ void store4(const Args& a, int b, int h, int j, int c, f32x4 w) {      // channels c .. c + 3 of a query
+    T* const op = reinterpret_cast<T*>(a.out) + b * a.out_batch + h * a.out_head + j * a.out_row + c;
+    if constexpr (sizeof(T) == 2) {
+        bf16x4 t;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t[e] = (__bf16)w[e];
+        *reinterpret_cast<bf16x4*>(op) = t;
+    } else {
+        *reinterpret_cast<f32x4*>(op) = w;
+    }
+}
+// a query's result: 4 channels of it, or of its share, and its share's maximum and sum
+struct Result {
+    const Args& a;
+    int b, h, j, split;
+    __device__ __forceinline__ int64_t row() const { return split * ((int64_t)a.B * a.nh * a.L) + ((int64_t)b * a.nh + h) * a.L + j; }
+    template <class T, int DH> __device__ __forceinline__ void put(int c, f32x4 w, float inv) const {
+        if (a.split > 1) *reinterpret_cast<f32x4*>(a.part + row() * DH + c) = w;
+        else store4<T>(a, b, h, j, c, w * inv);
+    }
+    __device__ __forceinline__ void put_ml(float m, float l) const {
+        if (a.split > 1) *reinterpret_cast<float2*>(a.ml + 2 * row()) = make_float2(m, l);
+    }
+};
+// Queries r0 .. r0 + n - 1 see nothing: zeros, or an empty share
+template <class T, int DH> __device__ __forceinline__ void nothing(const Args& a, const Place& w, int r0, int n, int tid, int threads) {
+    for (int x = tid; x < n * (DH / 4); x += threads) {
+        const int r = r0 + x / (DH / 4), c = x % (DH / 4) * 4;
+        if (r >= a.n) return;
+        const int hg = a.by_L.of(r);
+        const Result y{a, w.b, w.kvh * a.group + hg, r - hg * a.L, w.split};
+        if (a.split == 1) store4<T>(a, w.b, y.h, y.j, c, f32x4{0.f, 0.f, 0.f, 0.f});
+        else if (c == 0) y.put_ml(MINUS_INF, 0.f);
+    }
+}
+
+// ---- few queries: the wavefronts of a workgroup have the same ones, and steps in turn; joined in LDS --------------------
+// Blocks of 16 rows that a wavefront goes over at a time: a tile, or half of one where the codes would take more registers than there are.
+constexpr int blocks_of_step(int fmt, int esz, int dh, int nq) { return esz == 2 && fmt == FP8 && dh == 128 && nq > 1 ? 2 : 4; }
+constexpr int waves_per_simd(int fmt, int esz, int dh, int nq) { return esz == 4 && dh == 128 ? (nq == 1 ? 2 : 1) : nq == 1 && fmt == FP4 ? 3 : 2; }
+
+template <int FMT, class T, int DH, int NQ, int W>
+__global__ __launch_bounds__(64 * W, W == 8 ? 2 : waves_per_simd(FMT, sizeof(T), DH, NQ)) void k_packed_few(const Args a) {
+    constexpr int U = DH / 16, NT = sizeof(T) == 2 ? 1 : 3;
+    constexpr int NX = blocks_of_step(FMT, sizeof(T), DH, NQ), ROWS = 16 * NX;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c16 = lane & 15, lg = lane >> 4;
+    const Place w = place(a);
+    const int r0 = w.qt * (16 * NQ);
+    int p_min, p_max;
+    span(a, w.P, r0, 16 * NQ, p_min, p_max);
+    const Steps st = steps<ROWS>(a, w.P, p_min, p_max, w.split);
+    if (st.begin >= st.end) return nothing<T, DH>(a, w, r0, 16 * NQ, tid, 64 * W);
+
+    const uint8_t* const kb = a.k + w.b * a.batch + w.kvh * a.head;
+    const uint8_t* const vb = a.v + w.b * a.batch + w.kvh * a.head;
+    Keys<FMT, T, DH, NX> keys;
+    Values<FMT, DH, NX> values;
+    const int i0 = st.begin + wave;
+    if (i0 < st.end) {
+        keys.load(kb, st.of(i0), c16, lg);
+        values.load(vb, st.of(i0), c16, lg);
+    }
+    Query<T, DH> query[NQ];
+    int at[NQ];      // rows of this lane's queries (past the end the last one again: not stored)
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+        const int r = r0 + q * 16 + c16, rc = r < a.n ? r : a.n - 1, hg = a.by_L.of(rc), j = rc - hg * a.L;
+        at[q] = w.P + j;
+        query[q].load(reinterpret_cast<const T*>(a.q) + w.b * a.q_batch + (w.kvh * a.group + hg) * a.q_head + j * a.q_row, c16, lg);
+    }
     f32x4 o[U][NQ];
     float m_run[NQ], l_run[NQ];      // l: of this lane's keys
 #pragma unroll
@@ -305,145 +460,33 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(FMT, sizeof(T), DH, NQ)) vo
 #pragma unroll
         for (int m = 0; m < U; ++m) o[m][q] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-
-    for (int i = i0; i < t_end; i += step) {
-        const int t = step_of(i), k0 = t * ROWS;
-        const bool next = i + step < t_end;
-        const int t_next = step_of(i + step);
-        // ---- scores
+    for (int i = i0; i < st.end; i += W) {
+        const int k0 = st.of(i) * ROWS, t_next = st.of(i + W);
+        const bool next = i + W < st.end;
         f32x4 s[NX][NQ];
-        static_for<NX>([&](auto xc) {
-            constexpr int x = decltype(xc)::value;
-            if constexpr (BF16) {
-                i32x8 kf;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) kf[e] = (int)kw[x][FMT == FP4 ? e & 3 : DH == 64 ? e & 3 : e & (KW - 1)];
-#pragma unroll
-                for (int q = 0; q < NQ; ++q) {
-                    s[x][q] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, qh[q], f32x4{0.f, 0.f, 0.f, 0.f}, FMT == FP4 ? 4 : 0, 0, x, (int)ks, 0, qs[q]);
-                    if constexpr (DH == 128)
-                        s[x][q] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, ql[q], s[x][q], FMT == FP4 ? 4 : 0, 0, x, (int)ks, 1, qs[q]);
-                }
-            } else {
-                const float sc = scale_of(ks, x);
-#pragma unroll
-                for (int q = 0; q < NQ; ++q) s[x][q] = f32x4{0.f, 0.f, 0.f, 0.f};
-                static_for<NC>([&](auto cc) {
-                    constexpr int c = decltype(cc)::value;
-                    u32x4 w;
-                    static_for<4>([&](auto ec) {
-                        constexpr int e = decltype(ec)::value;
-                        if constexpr (FMT == FP4) w[e] = pair<FMT, e>(kw[x][c], sc);
-                        else w[e] = pair<FMT, e & 1>(kw[x][2 * c + e / 2], sc);
-                    });
-                    const bf16x8 kf = __builtin_bit_cast(bf16x8, w);
-#pragma unroll
-                    for (int q = 0; q < NQ; ++q)
-#pragma unroll
-                        for (int y = 0; y < 3; ++y) s[x][q] = mma(kf, q3[q][y][c], s[x][q]);
-                    __builtin_amdgcn_sched_barrier(0);
-                });
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        });
-        // The compiler may move these instructions to where their results are used, also behind a branch that not all lanes take;
-        // all lanes' operands are needed.
-#pragma unroll
-        for (int x = 0; x < NX; ++x)
-#pragma unroll
-            for (int q = 0; q < NQ; ++q) asm volatile("" : "+v"(s[x][q]));
-        if (next) load_k(t_next);
-        // ---- rows that some query does not see
-        const bool cut = k0 + ROWS - 1 > p_min || (a.window && k0 + ROWS > a.sinks && k0 <= p_max - a.window);
-        if (cut) {
-#pragma unroll
-            for (int q = 0; q < NQ; ++q) {
-                const int p = P + row_j[q] - k0 - 4 * lg, before = a.window ? p - a.window : -1 - ROWS, head = a.sinks - k0 - 4 * lg;
-#pragma unroll
-                for (int x = 0; x < NX; ++x)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int key = 16 * x + e;
-                        s[x][q][e] = (key <= p) & ((key > before) | (key < head)) ? s[x][q][e] : MINUS_INF;
-                    }
-            }
-            // Rows that no query of the wavefront sees may hold anything, and 0 * NaN must not reach the sums: their codes become zeros.
-            const int last = p_max - k0, first = a.window ? p_min - a.window - k0 : -1 - ROWS, head = a.sinks - k0;
+        scores<FMT, T, DH, NX, NQ>(s, keys, query);
+        stay(s);
+        if (next) keys.load(kb, t_next, c16, lg);
+        if (cut(a, k0, ROWS, p_min, p_max)) {
+            hide(s, a, at, k0, lg);
+            // Rows that no query of the workgroup sees may hold anything, and 0 * NaN must not reach the sums.
+            const int last = p_max - k0 - 4 * lg, first = a.window ? p_min - a.window - k0 - 4 * lg : -1 - ROWS, head = a.sinks - k0 - 4 * lg;
 #pragma unroll
             for (int x = 0; x < NX; ++x)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int key = 16 * x + 4 * lg + e;
-                    const bool seen = (key <= last) & ((key > first) | (key < head));
-                    if constexpr (TL::UNIT == 2) {
-                        vw[x][e >> 1] &= seen ? 0xFFFFFFFFu : (e & 1) ? 0x0000FFFFu : 0xFFFF0000u;
-                    } else {
-#pragma unroll
-                        for (int w = 0; w < VW / 4; ++w) vw[x][e * (VW / 4) + w] = seen ? vw[x][e * (VW / 4) + w] : 0u;
-                    }
-                    vs[x] = seen ? vs[x] : (vs[x] & ~(0xFFu << (8 * e))) | 0x7Fu << (8 * e);
-                }
+                for (int e = 0; e < 4; ++e) values.clear(x, e, sees<NX>(16 * x + e, last, first, head));
         }
-        // ---- the reference of the exponentials
-        float mx[NQ];
-        bool up = false;
-#pragma unroll
-        for (int q = 0; q < NQ; ++q) {
-            mx[q] = s[0][q][0];
-#pragma unroll
-            for (int x = 0; x < NX; ++x)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) mx[q] = fmaxf(mx[q], s[x][q][e]);
-            mx[q] *= a.scale_log2;
-            up |= mx[q] > m_run[q] + LAZY_EXP;
-        }
-        if (__any(up)) {
-#pragma unroll
-            for (int q = 0; q < NQ; ++q) {
-                const float most = max_of_groups(mx[q]), m_new = most > m_run[q] + LAZY_EXP ? most : m_run[q];
-                const float alpha = m_new == MINUS_INF ? 1.f : __builtin_amdgcn_exp2f(m_run[q] - m_new);
-                m_run[q] = m_new;
-                l_run[q] *= alpha;
-#pragma unroll
-                for (int m = 0; m < U; ++m) o[m][q] *= alpha;
-            }
-        }
-        // ---- exponentials and the second product, 32 keys at a time
+        refer(s, a.scale_log2, m_run, l_run, o);
         static_for<NX / 2>([&](auto hc) {
             constexpr int half = decltype(hc)::value;
-            constexpr int NT = BF16 ? 1 : 3;
             bf16x8 pf[NQ][NT];
-#pragma unroll
-            for (int q = 0; q < NQ; ++q) {
-                const float ref = m_run[q] == MINUS_INF ? 0.f : m_run[q];      // no key seen yet: every exponential is 0
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * half + (e >> 2)][q][e & 3], a.scale_log2, -ref));
-                    l_run[q] += p;
-#pragma unroll
-                    for (int y = 0; y < NT; ++y) {
-                        pf[q][y][e] = (__bf16)p;
-                        if (y + 1 < NT) p -= (float)pf[q][y][e];
-                    }
-                }
-            }
+            exponentials(pf, s, half, a.scale_log2, m_run, l_run);
             static_for<U / 2>([&](auto bc) {
                 constexpr int pr = decltype(bc)::value;      // channels 2 pr and 2 pr + 1 of the lane's
                 u32x4 even, odd;
                 static_for<4>([&](auto kc) {
                     constexpr int k2 = decltype(kc)::value, x = 2 * half + k2 / 2, e = 2 * (k2 & 1);      // rows e and e + 1 of block x
-                    auto value = [&](auto rc) {
-                        constexpr int r = decltype(rc)::value;
-                        const float sc = scale_of(vs[x], r);
-                        if constexpr (FMT == FP4) {
-                            if constexpr (DH == 128) return pair<FMT, pr>(vw[x][r], sc);
-                            else return pair<FMT, 2 * (r & 1) + pr>(vw[x][r / 2], sc);
-                        } else {
-                            if constexpr (DH == 128) return pair<FMT, pr & 1>(vw[x][2 * r + pr / 2], sc);
-                            else return pair<FMT, pr>(vw[x][r], sc);
-                        }
-                    };
-                    const uint32_t w0 = value(std::integral_constant<int, e>{}), w1 = value(std::integral_constant<int, e + 1>{});
+                    const uint32_t w0 = values.template two<pr, e>(x), w1 = values.template two<pr, e + 1>(x);
                     even[k2] = __builtin_amdgcn_perm(w1, w0, 0x05040100u);
                     odd[k2] = __builtin_amdgcn_perm(w1, w0, 0x07060302u);
                 });
@@ -457,119 +500,281 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(FMT, sizeof(T), DH, NQ)) vo
                 __builtin_amdgcn_sched_barrier(0);
             });
         });
-        if (next) load_v(t_next);
+        if (next) values.load(vb, t_next, c16, lg);
     }
-#pragma unroll
-    for (int m = 0; m < U; ++m)
-#pragma unroll
-        for (int q = 0; q < NQ; ++q) asm volatile("" : "+v"(o[m][q]));
-
+    stay(o);
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
         l_run[q] += __shfl_xor(l_run[q], 16);
         l_run[q] += __shfl_xor(l_run[q], 32);
     }
-    auto mine = [&](int q, int e, int k4) { return f32x4{o[4 * k4][q][e], o[4 * k4 + 1][q][e], o[4 * k4 + 2][q][e], o[4 * k4 + 3][q][e]}; };      // channels (4 g + e) U + 4 k4 ..
-    auto leave = [&](int h, int j, int c, f32x4 w, float inv) {
-        if (partial) *reinterpret_cast<f32x4*>(a.part + (split * all_rows + out_row(h, j)) * DH + c) = w;
-        else store4(h, j, c, w * inv);
-    };
-    if constexpr (!SHARED) {
-        int first = r0;
-        asm volatile("" : "+s"(first));      // heads and rows of the queries once more: kept over the loop they would take registers
+    // the wavefronts' results, 16 queries at a time: 16-byte chunk c of row r sits at c ^ r, so that 16 rows' chunks touch every bank once
+    __shared__ f32x4 acc[W][16 * (DH / 4)];
+    __shared__ float2 stat[W][16];
+    for (int q = 0; q < NQ; ++q) {
+        if (q) __syncthreads();
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) {
-            const int r = first + q * 16 + c16, hg = a.by_L.of(r), h = kvh * a.group + hg, j = r - hg * a.L;
-            if (r >= n) continue;
-            const float inv = l_run[q] > 0.f ? 1.0f / l_run[q] : 0.f;
+        for (int y = 0; y < NQ; ++y)
+            if (y == q) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
+                for (int e = 0; e < 4; ++e)
 #pragma unroll
-                for (int k4 = 0; k4 < U / 4; ++k4) leave(h, j, (4 * lg + e) * U + 4 * k4, mine(q, e, k4), inv);
-            if (partial && lg == 0) *reinterpret_cast<float2*>(a.ml + 2 * (split * all_rows + out_row(h, j))) = make_float2(m_run[q], l_run[q]);
-        }
-    } else {
-        // the wavefronts' results, 16 queries at a time: 16-byte chunk c of row r sits at c ^ r, so that 16 rows' chunks touch every bank once
-        __shared__ f32x4 acc[NW][16 * (DH / 4)];
-        __shared__ float2 stat[NW][16];
-        for (int q = 0; q < NQ; ++q) {
-            if (q) __syncthreads();
-#pragma unroll
-            for (int y = 0; y < NQ; ++y)
-                if (y == q) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-#pragma unroll
-                        for (int k4 = 0; k4 < U / 4; ++k4) acc[wave][c16 * (DH / 4) + ((((4 * lg + e) * U) / 4 + k4) ^ c16)] = mine(y, e, k4);
-                    if (lg == 0) stat[wave][c16] = make_float2(m_run[y], l_run[y]);
-                }
-            __syncthreads();
-            const int row = tid >> 4, r = r0 + q * 16 + row;
-            if (r < n) {
-                const int hg = a.by_L.of(r), h = kvh * a.group + hg, j = r - hg * a.L;
-                float M = MINUS_INF, f[NW], den = 0.f;
-#pragma unroll
-                for (int w = 0; w < NW; ++w) M = fmaxf(M, stat[w][row].x);
-#pragma unroll
-                for (int w = 0; w < NW; ++w) {
-                    f[w] = stat[w][row].x == MINUS_INF ? 0.f : __builtin_amdgcn_exp2f(stat[w][row].x - M);
-                    den += f[w] * stat[w][row].y;
-                }
-                const float inv = den > 0.f ? 1.0f / den : 0.f;
-#pragma unroll
-                for (int x = 0; x < DH / 64; ++x) {
-                    const int c4 = (tid & 15) + x * 16;
-                    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int w = 0; w < NW; ++w) sum += f[w] * acc[w][row * (DH / 4) + (c4 ^ row)];
-                    leave(h, j, c4 * 4, sum, inv);
-                }
-                if (partial && (tid & 15) == 0) *reinterpret_cast<float2*>(a.ml + 2 * (split * all_rows + out_row(h, j))) = make_float2(M, den);
+                    for (int k4 = 0; k4 < U / 4; ++k4)      // channels (4 g + e) u + 4 k4 ..
+                        acc[wave][c16 * (DH / 4) + (((4 * lg + e) * (U / 4) + k4) ^ c16)] = f32x4{o[4 * k4][y][e], o[4 * k4 + 1][y][e], o[4 * k4 + 2][y][e], o[4 * k4 + 3][y][e]};
+                if (lg == 0) stat[wave][c16] = make_float2(m_run[y], l_run[y]);
             }
+        __syncthreads();
+        const int row = tid >> 4 & 15, r = r0 + q * 16 + row;
+        if (r >= a.n || tid >= 256) continue;
+        const int hg = a.by_L.of(r);
+        const Result y{a, w.b, w.kvh * a.group + hg, r - hg * a.L, w.split};
+        float M = MINUS_INF, f[W], den = 0.f;
+#pragma unroll
+        for (int x = 0; x < W; ++x) M = fmaxf(M, stat[x][row].x);
+#pragma unroll
+        for (int x = 0; x < W; ++x) {
+            f[x] = stat[x][row].x == MINUS_INF ? 0.f : __builtin_amdgcn_exp2f(stat[x][row].x - M);
+            den += f[x] * stat[x][row].y;
         }
+        const float inv = den > 0.f ? 1.0f / den : 0.f;
+#pragma unroll
+        for (int z = 0; z < DH / 64; ++z) {
+            const int c4 = (tid & 15) + z * 16;
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int x = 0; x < W; ++x) sum += f[x] * acc[x][row * (DH / 4) + (c4 ^ row)];
+            y.put<T, DH>(c4 * 4, sum, inv);
+        }
+        if ((tid & 15) == 0) y.put_ml(M, den);
+    }
+}
+
+// ---- many queries: the wavefronts have queries of their own and share a tile's values ------------------------------------
+// Every wavefront unpacks a quarter of a tile's values into LDS, where all of them read the second product's operand: with values unpacked by
+// every wavefront for itself they were a third of the vector instructions.  Two buffers, one barrier a tile.
+template <int FMT, class T, int DH, int NQ>
+__global__ __launch_bounds__(64 * NW, sizeof(T) == 4 && DH == 128 ? 1 : 2) void k_packed_block(const Args a) {
+    constexpr int U = DH / 16, NT = sizeof(T) == 2 ? 1 : 3;
+    // bf16 operands of either half of a tile: [half][channel of a lane][lane], 8 keys, 4 of each of the half's blocks
+    __shared__ u32x2 lds[2][2][U][64][2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c16 = lane & 15, lg = lane >> 4;
+    const Place w = place(a);
+    const int g0 = w.qt * (NW * 16 * NQ), r0 = g0 + wave * (16 * NQ);
+    int g_min, g_max, p_min = 0, p_max = -1;      // of the workgroup, of the wavefront
+    span(a, w.P, g0, NW * 16 * NQ, g_min, g_max);
+    if (r0 < a.n) span(a, w.P, r0, 16 * NQ, p_min, p_max);
+    const Steps st = steps<PACKED_TILE>(a, w.P, g_min, g_max, w.split);
+    if (st.begin >= st.end) return nothing<T, DH>(a, w, g0, NW * 16 * NQ, tid, 64 * NW);
+
+    const uint8_t* const kb = a.k + w.b * a.batch + w.kvh * a.head;
+    const uint8_t* const vb = a.v + w.b * a.batch + w.kvh * a.head;
+    Keys<FMT, T, DH, 4> keys;
+    Values<FMT, DH, 1> values;
+    values.load_block(vb, st.of(st.begin), wave, c16, lg);
+    keys.load(kb, st.of(st.begin), c16, lg);
+    Query<T, DH> query[NQ];
+    int at[NQ];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+        const int r = r0 + q * 16 + c16, rc = r < a.n ? r : a.n - 1, hg = a.by_L.of(rc), j = rc - hg * a.L;
+        at[q] = w.P + j;
+        query[q].load(reinterpret_cast<const T*>(a.q) + w.b * a.q_batch + (w.kvh * a.group + hg) * a.q_head + j * a.q_row, c16, lg);
+    }
+    auto clear = [&](int i) {      // rows that no query of the workgroup sees may hold anything
+        const int k0 = st.of(i) * PACKED_TILE;
+        if (cut(a, k0, PACKED_TILE, g_min, g_max)) {
+            const int off = k0 + 16 * wave + 4 * lg, last = g_max - off, first = a.window ? g_min - a.window - off : -1 - PACKED_TILE, head = a.sinks - off;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) values.clear(0, e, sees<4>(e, last, first, head));
+        }
+    };
+    // channels 2 PR and 2 PR + 1 of this wavefront's block of 16 rows, in two steps
+    uint32_t two[4];
+    auto unpack = [&](auto pc, int i, bool second) {
+        constexpr int pr = decltype(pc)::value;
+        if (!second) {
+#pragma unroll
+            for (int x = 0; x < Values<FMT, DH, 1>::VW; ++x) asm volatile("" : "+v"(values.w[0][x]));      // here, not in front of the loop's other steps
+            two[0] = values.template two<pr, 0>(0); two[1] = values.template two<pr, 1>(0); two[2] = values.template two<pr, 2>(0); two[3] = values.template two<pr, 3>(0);
+        } else {
+            u32x2* const to = &lds[i & 1][wave >> 1][2 * pr][lane][wave & 1];
+            to[0] = u32x2{__builtin_amdgcn_perm(two[1], two[0], 0x05040100u), __builtin_amdgcn_perm(two[3], two[2], 0x05040100u)};
+            to[128] = u32x2{__builtin_amdgcn_perm(two[1], two[0], 0x07060302u), __builtin_amdgcn_perm(two[3], two[2], 0x07060302u)};
+        }
+    };
+    auto unpack_all = [&](int i) {
+        static_for<U / 2>([&](auto pc) {
+            unpack(pc, i, false);
+            unpack(pc, i, true);
+        });
+    };
+    clear(st.begin);
+    unpack_all(st.begin);
+    if (st.begin + 1 < st.end) values.load_block(vb, st.of(st.begin + 1), wave, c16, lg);
+    f32x4 o[U][NQ];
+    float m_run[NQ], l_run[NQ];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+        m_run[q] = MINUS_INF;
+        l_run[q] = 0.f;
+#pragma unroll
+        for (int m = 0; m < U; ++m) o[m][q] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    for (int i = st.begin; i < st.end; ++i) {
+        const int k0 = st.of(i) * PACKED_TILE;
+        const bool next = i + 1 < st.end;
+        // the buffer is full, and everybody has read the other one
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (next) clear(i + 1);
+        f32x4 s[4][NQ];
+        __builtin_amdgcn_s_setprio(1);
+        scores<FMT, T, DH, 4, NQ>(s, keys, query);
+        __builtin_amdgcn_s_setprio(0);
+        stay(s);
+        if (next) keys.load(kb, st.of(i + 1), c16, lg);
+        if (r0 < a.n && cut(a, k0, PACKED_TILE, p_min, p_max)) hide(s, a, at, k0, lg);      // (what a wavefront without queries computes is not stored)
+        refer(s, a.scale_log2, m_run, l_run, o);
+        // The second product, the operand of an instruction requested four channels in front of it; beside the first half's the exponentials
+        // of the second, beside the second half's the unpacking of the next tile (behind the last one: the old values once more, which
+        // nobody reads).
+        constexpr int AHEAD = 2;
+        bf16x8 pf[2][NQ][NT], vf[AHEAD];
+        auto fragment = [&](int half, int m) { return *reinterpret_cast<const bf16x8*>(&lds[i & 1][half][m][lane][0]); };
+#pragma unroll
+        for (int x = 0; x < AHEAD; ++x) vf[x] = fragment(0, x);
+        exponentials(pf[0], s, 0, a.scale_log2, m_run, l_run);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+        static_for<2 * U>([&](auto mc) {
+            constexpr int half = decltype(mc)::value / U, m = decltype(mc)::value % U;
+            const bf16x8 v = vf[m % AHEAD];
+            if constexpr (half == 0 || m + AHEAD < U) vf[m % AHEAD] = m + AHEAD < U ? fragment(half, m + AHEAD) : fragment(1, m + AHEAD - U);
+#pragma unroll
+            for (int q = 0; q < NQ; ++q)
+#pragma unroll
+                for (int y = 0; y < NT; ++y) o[m][q] = mma(v, pf[half][q][y], o[m][q]);
+            if constexpr (half == 0) {
+#pragma unroll
+                for (int e = m * 8 / U; e < (m + 1) * 8 / U; ++e) exponential<true>(pf[1], s, 1, e, a.scale_log2, m_run, l_run);
+            } else {
+                unpack(std::integral_constant<int, m / 2>{}, i + 1, m & 1);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        __builtin_amdgcn_s_setprio(0);
+        if (i + 2 < st.end) values.load_block(vb, st.of(i + 2), wave, c16, lg);
+    }
+    stay(o);
+    int first = r0;
+    asm volatile("" : "+s"(first));      // heads and rows of the queries once more: kept over the loop they would take registers
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+        l_run[q] += __shfl_xor(l_run[q], 16);
+        l_run[q] += __shfl_xor(l_run[q], 32);
+        const int r = first + q * 16 + c16, hg = a.by_L.of(r);
+        const Result y{a, w.b, w.kvh * a.group + hg, r - hg * a.L, w.split};
+        if (r >= a.n) continue;
+        const float inv = l_run[q] > 0.f ? 1.0f / l_run[q] : 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int k4 = 0; k4 < U / 4; ++k4) y.put<T, DH>((4 * lg + e) * U + 4 * k4, f32x4{o[4 * k4][q][e], o[4 * k4 + 1][q][e], o[4 * k4 + 2][q][e], o[4 * k4 + 3][q][e]}, inv);
+        if (lg == 0) y.put_ml(m_run[q], l_run[q]);
     }
 }
 
 int clamp_int(int64_t v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : (int)v; }
 
-// part_floats: the scratch there is (packed_attention_floats asks with as much as can be wanted)
-Plan make_plan(const PackedAttn& a, int64_t part_floats) {
-    Plan p{};
-    const int64_t n = (int64_t)(a.nh / a.nkv) * a.L, slot_floats = (int64_t)a.B * a.nh * a.L * (a.dh + 2);
-    const int slots = clamp_int(part_floats / slot_floats, 0, MAX_SHARES);
-    p.shared = n <= 32;
-    p.nq = n <= 16 ? 1 : 2;
-    const int rows = 16 * p.nq * (p.shared ? 1 : NW);
-    p.tiles = (int)((n + rows - 1) / rows);
-    // tiles of keys that a workgroup sees at most
-    const int64_t end = (int64_t)a.P + a.L;
-    int64_t seen = (end + PACKED_TILE - 1) / PACKED_TILE;
+// What a call costs in microseconds, fitted to the times in make_plan's comment: a round of workgroups has START; a wavefront's step of
+// 64 rows takes LATENCY by itself, and a SIMD gets through one in WORK; the cache comes in at READ bytes a microsecond, into a CU at INTO_CU.
+struct Cost { double start, latency, work; };
+constexpr double READ = 5.9e6, INTO_CU = 45e3, JOIN = 4.5, JOIN_SHARE = 0.08, JOIN_BYTES = 5e6;
+Cost cost_few(int esz, int dh, int nq) {
+    if (esz == 4) return dh == 128 ? Cost{4.5, 2.0, 1.6} : nq == 1 ? Cost{4.5, 1.3, 0.93} : Cost{5.5, 2.2, 1.8};
+    return nq == 1 ? (dh == 128 ? Cost{4.5, 1.05, 0.55} : Cost{4.5, 0.8, 0.35}) : (dh == 128 ? Cost{5.5, 1.5, 0.98} : Cost{5.5, 1.1, 0.62});
+}
+// 64-row tiles that a workgroup with `rows` queries of a (sequence, key head) sees at most, and on average
+void tiles_seen(const PackedAttn& a, int64_t n, int64_t rows, double& most, double& mean) {
+    const double last = a.P + a.L, first = a.P, span = n < rows ? a.L : rows < a.L ? rows : a.L;      // rows of its queries
+    most = last;
+    mean = (first + last + span) / 2;
     if (a.window) {
-        const int64_t w = ((int64_t)a.window + (p.shared || n < rows ? a.L : rows) + PACKED_TILE - 1) / PACKED_TILE + 1 + ((int64_t)a.sinks + PACKED_TILE - 1) / PACKED_TILE;
-        seen = w < seen ? w : seen;
+        const double w = (double)a.window + span + (a.sinks ? a.sinks + 32.0 : 0.0);
+        most = w < most ? w : most;
+        mean = w < mean ? w : mean;
     }
-    const int64_t base = (int64_t)a.B * a.nkv * p.tiles, places = 3 * cu_count();
-    p.split = clamp_int(places / base, 1, clamp_int(seen / (p.shared ? 8 : 4), 1, slots > 1 ? slots : 1));
-    return p;
+    most = most / PACKED_TILE + (a.window ? 1 : 0.5);
+    mean = mean / PACKED_TILE + (a.window ? 1 : 0.5);
 }
 
-template <int FMT, class T, int DH, int NQ, bool SHARED>
+// part_floats: the scratch there is (packed_attention_floats asks with as much as can be wanted)
+Plan make_plan(const PackedAttn& a, int64_t part_floats) {
+    const int64_t n = (int64_t)(a.nh / a.nkv) * a.L, pairs = (int64_t)a.B * a.nkv, slot_floats = (int64_t)a.B * a.nh * a.L * (a.dh + 2);
+    const int slots = clamp_int(part_floats / slot_floats, 1, MAX_SHARES), esz = a.dtype == 1 ? 2 : 4, cus = cu_count();
+    const double tile_bytes = 2.0 * packed_tile_bytes(a.fmt, a.dh);
+    Plan best{};
+    double best_time = 0;
+    auto offer = [&](const Plan& p, double time) {
+        if (best.nq && time >= best_time) return;
+        best = p;
+        best_time = time;
+    };
+    double most, mean;
+    for (int nq = 1; nq <= 2; ++nq) {
+        if (nq == 2 && (n <= 16 || (esz == 4 && a.dh == 128))) break;
+        const Cost c = cost_few(esz, a.dh, nq);
+        const int64_t tiles = (n + 16 * nq - 1) / (16 * nq), base = pairs * tiles;
+        tiles_seen(a, n, 16 * nq, most, mean);
+        const double bytes = pairs * most * tile_bytes;
+        for (int waves = NW; waves <= (nq == 1 ? 2 * NW : NW); waves += NW) {
+            const int places = cus * (waves > NW ? 1 : esz == 2 && nq == 1 && a.fmt == FP4 ? 3 : 2);
+            for (int split = 1; split <= slots && (split == 1 || split * waves <= most + waves); split += 1 + split / 4) {
+                const int64_t rounds = (base * split + places - 1) / places;
+                const int steps = (int)(most / (split * waves)) + 1;
+                const double alone = rounds * steps * c.latency, work = base * split * (mean / split) / (4.0 * cus) * c.work, most_of = alone > work ? alone : work;
+                const double into_cu = rounds * (most / split) * tile_bytes / INTO_CU, read = bytes / READ > into_cu ? bytes / READ : into_cu;
+                offer({nq, waves, (int)tiles, split}, rounds * c.start + sqrt(most_of * most_of + read * read) + (split > 1 ? JOIN + split * (JOIN_SHARE + slot_floats * 8.0 / JOIN_BYTES) : 0.0));
+            }
+        }
+    }
+    if (esz == 2) {
+        // a tile's time in a workgroup that has its CU to itself, that shares it with another one, with two others (heads of 64); a round's START
+        // again; the last round is as long as its longest
+        const double alone[3] = {a.dh == 128 ? 1.5 : 1.0, a.dh == 128 ? 2.0 : 1.25, 1.7}, codes = a.fmt == FP8 && a.dh == 128 ? 1.15 : 1.0, start = 6.0;
+        const int per_cu = a.dh == 128 ? 2 : 3;
+        const int64_t rows = 32 * NW, tiles = (n + rows - 1) / rows, wgs = pairs * tiles, places = (int64_t)per_cu * cus, rounds = (wgs + places - 1) / places;
+        const int64_t beside = (wgs - (rounds - 1) * places + cus - 1) / cus;
+        tiles_seen(a, n, rows, most, mean);
+        offer({2, 0, (int)tiles, 1}, rounds * start + codes * ((rounds - 1) * mean * alone[per_cu - 1] + (rounds > 1 ? mean : most) * alone[beside - 1]));
+    }
+    return best;
+}
+
+template <int FMT, class T, int DH, int NQ, int W>
 void run_cfg(Args a, hipStream_t st) {
     a.group = a.nh / a.nkv;
     a.n = a.group * a.L;
     a.shares = a.tiles * a.nkv * a.B;
-    a.by_nkv = Div(a.nkv); a.by_L = Div(a.L); a.by_tiles = Div(a.tiles); a.by_shares = Div(a.shares);
+    a.by_nkv = Div(a.nkv); a.by_L = Div(a.L); a.round = a.tiles < 64 ? 64 / a.tiles : 1; a.by_round = Div(a.round * a.tiles); a.by_in_round = Div(a.round); a.by_shares = Div(a.shares);
     a.ml = a.part ? a.part + (int64_t)a.split * a.B * a.nh * a.L * DH : nullptr;
-    hipLaunchKernelGGL((k_packed_attention<FMT, T, DH, NQ, SHARED>), dim3((unsigned)((int64_t)a.shares * a.split)), dim3(64 * NW), 0, st, a);
+    if constexpr (W == 0) hipLaunchKernelGGL((k_packed_block<FMT, T, DH, NQ>), dim3((unsigned)((int64_t)a.shares * a.split)), dim3(64 * NW), 0, st, a);
+    else hipLaunchKernelGGL((k_packed_few<FMT, T, DH, NQ, W>), dim3((unsigned)((int64_t)a.shares * a.split)), dim3(64 * W), 0, st, a);
 }
 template <int FMT, class T, int DH>
 void run(const PackedAttn& c, hipStream_t st) {
     Args a{};
     static_cast<PackedAttn&>(a) = c;
     static_cast<Plan&>(a) = make_plan(a, c.part ? c.part_floats : 0);
-    if (!a.shared) run_cfg<FMT, T, DH, 2, false>(a, st);
-    else if (a.nq == 2) run_cfg<FMT, T, DH, 2, true>(a, st);
-    else run_cfg<FMT, T, DH, 1, true>(a, st);
+    if (a.waves > NW) {
+        run_cfg<FMT, T, DH, 1, 2 * NW>(a, st);
+    } else if (a.nq == 1) {
+        run_cfg<FMT, T, DH, 1, NW>(a, st);
+    } else if constexpr (sizeof(T) == 2) {
+        if (a.waves) run_cfg<FMT, T, DH, 2, NW>(a, st);
+        else run_cfg<FMT, T, DH, 2, 0>(a, st);
+    } else if constexpr (DH == 64) {
+        run_cfg<FMT, T, DH, 2, NW>(a, st);
+    }
     if (a.split > 1) {
         ContextAttn j{};
         j.dtype = c.dtype; j.B = c.B; j.L = c.L; j.nh = c.nh; j.nkv = c.nkv; j.dh = c.dh;
