@@ -15,6 +15,7 @@ typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(2))) short i16x2;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 // ---- eight numbers and their codes ---------------------------------------------------------------------------------
 // The byte 127 + e of a group whose largest |x| has these bits: e is the smallest integer with |x| <= T 2^e, T = 7 = 1.75 2^2 or
@@ -71,11 +72,11 @@ __device__ __forceinline__ void store8(__bf16* p, const float* x) {
     bf16x8 v;
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = (__bf16)x[i];      // exact
-    *reinterpret_cast<bf16x8*>(p) = v;
+    __builtin_nontemporal_store(v, reinterpret_cast<bf16x8*>(p));
 }
 __device__ __forceinline__ void store8(float* p, const float* x) {
-    *reinterpret_cast<f32x4*>(p) = f32x4{x[0], x[1], x[2], x[3]};
-    *reinterpret_cast<f32x4*>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+    __builtin_nontemporal_store(f32x4{x[0], x[1], x[2], x[3]}, reinterpret_cast<f32x4*>(p));
+    __builtin_nontemporal_store(f32x4{x[4], x[5], x[6], x[7]}, reinterpret_cast<f32x4*>(p + 4));
 }
 template <int X> __device__ __forceinline__ uint32_t quad_swap(uint32_t v) {      // lane ^ 1 or ^ 2
     return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, X == 1 ? 0xB1 : 0x4E, 0xF, 0xF, true);
@@ -85,11 +86,12 @@ template <int X> __device__ __forceinline__ uint32_t quad_swap(uint32_t v) {    
 // A thread has eight channels of a row, four threads a group: 16 bytes of bf16 in, 4 or 8 bytes of codes out, or the other way round.
 // Values that come as channels of rows go through LDS, 64 rows a workgroup.
 constexpr int ROWS_THREADS = 256;
+struct __attribute__((packed, aligned(2))) Piece { u32x4 v; };
 struct RowsArgs : PackedRows {
     Div by_L, by_nkv, by_chunks;
     uint32_t k_blocks;      // the first ones of the grid
     int total, chunks;      // rows of the call; workgroups of a (sequence, head) whose values are channels of rows
-    bool v_across;
+    bool v_across, v_whole;      // values are channels of rows; in whole pieces of 16 bytes
 };
 template <int FMT, int DH> __device__ __forceinline__ void put(uint8_t* tile, int r, int t8, bool keys, Codes8<FMT> w, uint32_t byte) {
     using TL = Tile<FMT, DH>;
@@ -147,78 +149,122 @@ __device__ __forceinline__ int first_row(const PackedRows& a, int b) {
     return P < a.rows - a.L ? P : a.rows - a.L;
 }
 
+// Rows of a thread.  us, one / two, 4 x 4224 rows of 32 heads of 128 read back 76 / 72; float32, 4 x 1024 40.6 / 42.9.
+constexpr int rows_each(int esz) { return esz == 2 ? 2 : 1; }
+
 template <int FMT, class T, int DH, bool PACK>
 __global__ __launch_bounds__(ROWS_THREADS) void k_packed_rows(const RowsArgs a) {
     using TL = Tile<FMT, DH>;
     constexpr int TR = DH / 8, NR = ROWS_THREADS / TR;      // threads of a row, rows at a time
+    constexpr int ROWS_EACH = rows_each(sizeof(T));
     const int tid = threadIdx.x, t8 = tid % TR;
     const bool keys = blockIdx.x < a.k_blocks;
     const int id = (int)(blockIdx.x - (keys ? 0 : a.k_blocks));
     uint8_t* const cache = keys ? a.pk : a.pv;
     if (keys || !a.v_across) {
-        const int row = id * NR + tid / TR;
-        if (row >= a.total) return;
-        const int bh = a.by_L.of(row), j = row - bh * a.L, b = a.by_nkv.of(bh), h = bh - b * a.nkv;
-        const int P = first_row(a, b);
-        if (P < 0) return;
-        const int at = P + j, r = at % PACKED_TILE;
-        uint8_t* const tile = cache + b * a.batch + h * a.head + (int64_t)(at / PACKED_TILE) * TL::BYTES;
-        T* const src = reinterpret_cast<T*>(keys ? a.k : a.v) + (keys ? b * a.k_batch + h * a.k_head + j * a.k_row : b * a.v_batch + h * a.v_head + j * a.v_row) + t8 * 8;
-        float x[8];
-        if constexpr (PACK) {
-            load8(src, x);
-            pack8<FMT, DH>(tile, r, t8, keys, x);
-        } else {
-            unpack8<FMT, DH>(tile, r, t8, keys, x);
-            store8(src, x);
+        T* src[ROWS_EACH];
+        uint8_t* tile[ROWS_EACH];
+        int r[ROWS_EACH];
+        bool there[ROWS_EACH];
+        float x[ROWS_EACH][8];
+#pragma unroll
+        for (int y = 0; y < ROWS_EACH; ++y) {
+            const int row = (id * ROWS_EACH + y) * NR + tid / TR, bh = a.by_L.of(row), j = row - bh * a.L, b = a.by_nkv.of(bh), h = bh - b * a.nkv;
+            const int P = row < a.total ? first_row(a, b) : -1, at = P + j;
+            there[y] = P >= 0;
+            r[y] = at % PACKED_TILE;
+            tile[y] = cache + b * a.batch + h * a.head + (int64_t)(at / PACKED_TILE) * TL::BYTES;
+            src[y] = reinterpret_cast<T*>(keys ? a.k : a.v) + (keys ? b * a.k_batch + h * a.k_head + j * a.k_row : b * a.v_batch + h * a.v_head + j * a.v_row) + t8 * 8;
         }
+#pragma unroll
+        for (int y = 0; y < ROWS_EACH; ++y)
+            if (there[y]) {
+                if constexpr (PACK) load8(src[y], x[y]);
+                else unpack8<FMT, DH>(tile[y], r[y], t8, keys, x[y]);
+            }
+#pragma unroll
+        for (int y = 0; y < ROWS_EACH; ++y)
+            if (there[y]) {
+                if constexpr (PACK) pack8<FMT, DH>(tile[y], r[y], t8, keys, x[y]);
+                else store8(src[y], x[y]);
+            }
         return;
     }
-    // rows of this workgroup: 64 of a (sequence, head), next to each other in memory; LDS holds them as rows of channels
-    constexpr int PITCH = DH + (sizeof(T) == 2 ? 2 : 1);      // odd words: neither the rows nor the channels of a wavefront share a bank
-    __shared__ T lds[PACKED_TILE * PITCH];
+    // 64 rows of a (sequence, head), next to each other in memory: 16-byte pieces of E rows of a channel, in LDS at piece ^ (channel / 8), and of
+    // two-byte numbers with the upper channels' pairs exchanged, so that neither the pieces nor the eight channels of 16 threads share a bank.
+    constexpr int E = 16 / sizeof(T), CH = PACKED_TILE / E, PER = DH * CH / ROWS_THREADS;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[DH * PACKED_TILE * sizeof(T)];
+    auto piece = [&](int c, int e) { return lds + (sizeof(T) == 2 ? c ^ (c >> 6) : c) * (PACKED_TILE * (int)sizeof(T)) + (e ^ (c >> 3 & (CH - 1))) * 16; };
+    auto number = [&](int c, int j) { return reinterpret_cast<T*>(piece(c, j / E)) + j % E; };
     const int bh = a.by_chunks.of(id), j0 = (id - bh * a.chunks) * PACKED_TILE, b = a.by_nkv.of(bh), h = bh - b * a.nkv;
     const int P = first_row(a, b);
     if (P < 0) return;      // the whole workgroup
     const int n = a.L - j0 < PACKED_TILE ? a.L - j0 : PACKED_TILE;
     T* const src = reinterpret_cast<T*>(a.v) + b * a.v_batch + h * a.v_head + j0;
     uint8_t* const head = cache + b * a.batch + h * a.head;
-    const int lane = tid & 63, wave = tid >> 6;
     if constexpr (PACK) {
-        for (int c = wave; c < DH; c += ROWS_THREADS / 64)
-            if (lane < n) lds[lane * PITCH + c] = src[c * a.v_chan + lane];
+        Piece x[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int c = (tid + i * ROWS_THREADS) / CH, e = tid % CH;
+            const T* const from = src + c * a.v_chan + e * E;
+            if (e * E + E <= n) {
+                if (a.v_whole) x[i].v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from));
+                else x[i] = *reinterpret_cast<const Piece*>(from);      // at any alignment of its numbers
+            } else {
+#pragma unroll
+                for (int y = 0; y < E; ++y)
+                    if (e * E + y < n) reinterpret_cast<T*>(&x[i])[y] = from[y];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) *reinterpret_cast<u32x4*>(piece((tid + i * ROWS_THREADS) / CH, tid % CH)) = x[i].v;
         __syncthreads();
     }
     for (int j = tid / TR; j < n; j += NR) {
         const int at = P + j0 + j;
         uint8_t* const tile = head + (int64_t)(at / PACKED_TILE) * TL::BYTES;
-        T* const mine = lds + j * PITCH + t8 * 8;
         float x[8];
         if constexpr (PACK) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = (float)mine[i];
+            for (int i = 0; i < 8; ++i) x[i] = (float)*number(t8 * 8 + i, j);
             pack8<FMT, DH>(tile, at % PACKED_TILE, t8, false, x);
         } else {
             unpack8<FMT, DH>(tile, at % PACKED_TILE, t8, false, x);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) mine[i] = (T)x[i];
+            for (int i = 0; i < 8; ++i) *number(t8 * 8 + i, j) = (T)x[i];
         }
     }
     if constexpr (!PACK) {
         __syncthreads();
-        for (int c = wave; c < DH; c += ROWS_THREADS / 64)
-            if (lane < n) src[c * a.v_chan + lane] = lds[lane * PITCH + c];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int c = (tid + i * ROWS_THREADS) / CH, e = tid % CH;
+            T* const to = src + c * a.v_chan + e * E;
+            Piece x;
+            x.v = *reinterpret_cast<const u32x4*>(piece(c, e));
+            if (e * E + E <= n) {
+                if (a.v_whole) __builtin_nontemporal_store(x.v, reinterpret_cast<u32x4*>(to));
+                else *reinterpret_cast<Piece*>(to) = x;
+            } else {
+#pragma unroll
+                for (int y = 0; y < E; ++y)
+                    if (e * E + y < n) to[y] = reinterpret_cast<const T*>(&x)[y];
+            }
+        }
     }
 }
 template <int FMT, class T, int DH, bool PACK> void run_rows(const PackedRows& p, hipStream_t st) {
-    constexpr int NR = ROWS_THREADS / (DH / 8);
+    constexpr int NR = ROWS_THREADS / (DH / 8), ROWS_EACH = rows_each(sizeof(T));
     RowsArgs a{};
     static_cast<PackedRows&>(a) = p;
     a.total = p.B * p.nkv * p.L;
     a.chunks = (p.L + PACKED_TILE - 1) / PACKED_TILE;
     a.v_across = p.v_chan != 1;
+    constexpr int64_t E = 16 / sizeof(T);
+    a.v_whole = ((uintptr_t)p.v & 15) == 0 && p.v_batch % E == 0 && p.v_head % E == 0 && p.v_chan % E == 0;
     a.by_L = Div(p.L); a.by_nkv = Div(p.nkv); a.by_chunks = Div(a.chunks);
-    const uint32_t flat = (uint32_t)((a.total + NR - 1) / NR);
+    const uint32_t flat = (uint32_t)((a.total + ROWS_EACH * NR - 1) / (ROWS_EACH * NR));
     a.k_blocks = p.k ? flat : 0;
     const uint32_t v_blocks = !p.v ? 0 : a.v_across ? (uint32_t)(p.B * p.nkv * a.chunks) : flat;
     hipLaunchKernelGGL((k_packed_rows<FMT, T, DH, PACK>), dim3(a.k_blocks + v_blocks), dim3(ROWS_THREADS), 0, st, a);
