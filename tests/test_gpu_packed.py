@@ -327,6 +327,37 @@ CASES = [
     ("fp4", "bf16", 1, 300, 4, 4, 64, 2000, {}),
     ("fp8", "f32", 1, 70, 4, 4, 64, 1500, dict(starts=[1111])),
 ]
+# Sizes at which keys are dealt to several workgroups or to eight wavefronts, and those of more queries
+MANY = [
+    # blocks whose wavefronts share a tile's values: whole and ragged tiles of 128 queries, queries that span heads, windows and sinks,
+    # sequences of unequal length, absent ones
+    ("fp4", "bf16", 5, 150, 32, 32, 128, 33, {}),
+    ("fp8", "bf16", 5, 150, 32, 32, 128, 90, dict(starts=[90, 0, -1, 64, 17])),
+    ("fp4", "bf16", 8, 128, 32, 32, 128, 0, {}),
+    ("fp4", "bf16", 8, 70, 64, 32, 128, 100, dict(window=60, sinks=70)),
+    ("fp8", "bf16", 6, 260, 32, 32, 128, 60, dict(window=100, sinks=10)),
+    ("fp4", "bf16", 8, 140, 32, 32, 128, 200, dict(window=1, starts=[200, 3, -1, 64, 63, 0, 150, 199])),
+    ("fp4", "bf16", 8, 33, 128, 32, 128, 150, dict(starts=[150, -1, 0, 1, 63, 64, 65, 5])),
+    ("fp8", "bf16", 16, 150, 32, 32, 64, 40, dict(window=150, sinks=9)),
+    ("fp4", "bf16", 16, 128, 32, 32, 64, 70, {}),
+    ("fp4", "bf16", 16, 200, 32, 32, 64, 5, dict(starts=[5, -1] * 8)),
+    # a few queries over many keys
+    ("fp4", "bf16", 2, 1, 8, 8, 128, 3000, {}),
+    ("fp8", "bf16", 1, 3, 8, 4, 128, 5000, dict(window=4500, sinks=100)),
+    ("fp8", "bf16", 3, 1, 8, 8, 64, 2500, dict(starts=[2500, -1, 700])),
+    ("fp4", "bf16", 4, 1, 32, 32, 128, 1100, {}),
+    ("fp8", "bf16", 8, 1, 32, 32, 64, 1300, {}),
+    ("fp4", "f32", 4, 1, 16, 16, 128, 900, {}),
+    ("fp8", "f32", 2, 2, 8, 8, 64, 2100, {}),
+    ("fp8", "f32", 4, 40, 8, 8, 64, 600, {}),
+    ("fp4", "f32", 6, 90, 16, 16, 64, 200, dict(window=150, sinks=3)),
+    ("fp8", "bf16", 12, 40, 32, 32, 128, 300, {}),
+    ("fp8", "bf16", 4, 90, 16, 16, 64, 700, {}),
+]
+# every kernel of every format, type and head size: 32 and 16 queries of a wavefront, four and eight wavefronts, shared values, shares of the keys
+EACH = [(fmt, dtype, B, L, nh, nkv, dh, P, dict(kw, starts=[P] + [17] * (B - 1)) if kw else {}) for fmt in ("fp4", "fp8") for dtype in ("bf16", "f32")
+        for dh in (64, 128) for B, L, nh, nkv, P in ((2, 200, 32, 8, 30), (4, 200, 32, 8, 30), (1, 200, 4, 1, 30), (1, 17, 4, 1, 1500), (1, 200, 16, 4, 2500))
+        for kw in ({}, dict(window=70, sinks=5))]
 name_of = lambda c: "%s-%s-%dx%d-h%d.%d-%d-P%d%s" % (c[:8] + ("".join("-%s%s" % (k, v) for k, v in c[8].items() if k != "starts"),))
 
 
@@ -345,7 +376,7 @@ def test_plain_form_is_the_oracle(case):
     assert torch.equal(keys, want[3])
 
 
-@pytest.mark.parametrize("case", CASES, ids=name_of)
+@pytest.mark.parametrize("case", CASES + MANY + EACH, ids=name_of)
 def test_attention(case):
     fmt, dtype, B, L, nh, nkv, dh, P, kw = case
     c = make(fmt, dtype, B, L, nh, nkv, dh, P, **kw)
@@ -358,7 +389,7 @@ def test_attention(case):
         check(c, out, "scratch %g" % share, reference)
 
 
-@pytest.mark.parametrize("case", [c for c in CASES if any(p < 0 for p in c[8].get("starts", ()))], ids=name_of)
+@pytest.mark.parametrize("case", [c for c in CASES + MANY if any(p < 0 for p in c[8].get("starts", ()))], ids=name_of)
 def test_absent_sequences_are_zeros_whatever_their_queries_hold(case):
     fmt, dtype, B, L, nh, nkv, dh, P, kw = case
     c = make(fmt, dtype, B, L, nh, nkv, dh, P, **kw)
