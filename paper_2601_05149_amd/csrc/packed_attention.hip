@@ -4,15 +4,17 @@
 // o = o 2^(m - m') + sum 2^(s - m') v, l likewise; out = o / l; partial results join the same way.  A wavefront goes over tiles of 64
 // rows with 16 NQ queries, which are rows of all the heads that share a key head.  S^T = K Q^T and O^T = V^T P^T in 16 x 16 blocks: a
 // lane (query c = lane % 16, g = lane / 16) has the scores of keys 16 x + 4 g + i, which are the operand that the second product takes
-// of it, and channels (4 g + i) u + m of the output, u = d_h / 16.  Nothing of the cache passes through LDS: a lane loads the codes that
-// its instructions take.
+// of it, and channels (4 g + i) u + m of the output, u = d_h / 16.  Nothing of the cache passes through LDS on its way to an instruction
+// of the wavefront that loads it: a lane loads the codes that its instructions take, 16 bytes at a time.
 //
 // bf16: the keys' codes and scales feed the scaled matrix instruction as they lie.  A query enters as two terms of four
 // significant bits, q = hi + lo, with a power of two per group of 32 channels each: bf16's eight bits, exactly, but for channels below 2^-13 of
-// their group's largest (2^-21 of it).  Heads of 64 have both terms side by side in one instruction.  float32: codes become
-// bf16, exactly, and a query (and an exponential) three bf16 terms.
+// their group's largest (2^-21 of it).  Heads of 64 have both terms side by side in one instruction.  Against keys made bf16 first the scores
+// take no conversions at all: of a tile of 64 rows of heads of 128, 64 of them a lane.  The exponentials are rounded to bf16, at most 2^-8 of
+// each, as the weights of context_attention.hip are.
+// float32: codes become bf16, exactly, and a query (and an exponential) three bf16 terms, all its 24 bits; the products are exact in float32.
 // Values become bf16 with their own scale, two channels of a row an instruction, and pairs of rows are put together by a byte
-// permutation.
+// permutation: exact, so that only the exponentials' rounding and the sums' are left.
 #include <hip/hip_bf16.h>
 
 #include <type_traits>
@@ -27,7 +29,6 @@ namespace {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
@@ -61,7 +62,7 @@ struct Args : PackedAttn, Plan {
     Div by_nkv, by_L, by_round, by_in_round, by_shares;
 };
 
-// 16 codes bytes a lane feeds the instruction; two codes at once as bf16.  SEL: which pair of the word
+// two codes times their scale as bf16.  SEL: which pair of the word
 template <int FMT, int SEL> __device__ __forceinline__ uint32_t pair(uint32_t w, float s) {
     if constexpr (FMT == FP4) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, SEL));
     else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, SEL != 0));
@@ -271,8 +272,9 @@ template <int N, int NQ> __device__ __forceinline__ void stay(f32x4 (&s)[N][NQ])
 #pragma unroll
         for (int q = 0; q < NQ; ++q) asm volatile("" : "+v"(s[x][q]));
 }
+// key (of a step, as p, before and head are) seen by a query at row p: behind the window's last unseen row, or of the sinks
+__device__ __forceinline__ bool sees(int key, int p, int before, int head) { return (key <= p) & ((key > before) | (key < head)); }
 // -inf for the keys of a step (first key k0) that a lane's query (at row p) does not see
-template <int NX> __device__ __forceinline__ bool sees(int key, int p, int before, int head) { return (key <= p) & ((key > before) | (key < head)); }
 template <int NX, int NQ> __device__ __forceinline__ void hide(f32x4 (&s)[NX][NQ], const PackedAttn& a, const int (&row)[NQ], int k0, int lg) {
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
@@ -280,7 +282,7 @@ template <int NX, int NQ> __device__ __forceinline__ void hide(f32x4 (&s)[NX][NQ
 #pragma unroll
         for (int x = 0; x < NX; ++x)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[x][q][e] = sees<NX>(16 * x + e, p, before, head) ? s[x][q][e] : MINUS_INF;
+            for (int e = 0; e < 4; ++e) s[x][q][e] = sees(16 * x + e, p, before, head) ? s[x][q][e] : MINUS_INF;
     }
 }
 // Moves the reference of the exponentials where some query's maximum has outgrown it, and what has been added up with it
@@ -348,7 +350,7 @@ __device__ __forceinline__ Place place(const Args& a) {
     w.P = a.P;
     if (a.P_seq) {
         const int P = a.P_seq[w.b];
-        w.P = P < a.rows - a.L ? P : a.rows - a.L;
+        w.P = P < 0 ? -1 : P < a.rows - a.L ? P : a.rows - a.L;
     }
     return w;
 }
@@ -418,9 +420,16 @@ template <class T, int DH> __device__ __forceinline__ void nothing(const Args& a
 }
 
 // ---- few queries: the wavefronts of a workgroup have the same ones, and steps in turn; joined in LDS --------------------
-// Blocks of 16 rows that a wavefront goes over at a time: a tile, or half of one where the codes would take more registers than there are.
+// Bound by the cache where there are many sequences (32 of 4224 rows, 32 heads of 128, 4 bits, 575 MB: 104 us, 5.5 TB/s; 16 with a window
+// of 2048 rows in 8 bits, 304 MB: 54 us, 5.6 TB/s), by a wavefront's own chain of a step (1 to 1.5 us: loads, scores, maximum, exponentials,
+// products) where there are few: the plan spreads those over wavefronts and shares.  The next step's codes are on their way while a step is
+// computed (three wavefronts of a SIMD with 4 bits); a second step on its way gained nothing (28.3 us against 29.4, 29.8 against 30.5).
+// Against the running maximum of the keys as each step has it, a reference that moves once it is outgrown by 2^8 leaves out the products
+// with alpha of nearly every step.
+// Blocks of 16 rows that a wavefront goes over at a time: a tile, or half of one where the codes would take more registers than there are
+// (8 bits, heads of 128, two blocks of queries).
 constexpr int blocks_of_step(int fmt, int esz, int dh, int nq) { return esz == 2 && fmt == FP8 && dh == 128 && nq > 1 ? 2 : 4; }
-constexpr int waves_per_simd(int fmt, int esz, int dh, int nq) { return esz == 4 && dh == 128 ? (nq == 1 ? 2 : 1) : nq == 1 && fmt == FP4 ? 3 : 2; }
+constexpr int waves_per_simd(int fmt, int esz, int dh, int nq) { return nq == 1 && fmt == FP4 && (esz == 2 || dh == 64) ? 3 : 2; }      // without spills
 
 template <int FMT, class T, int DH, int NQ, int W>
 __global__ __launch_bounds__(64 * W, W == 8 ? 2 : waves_per_simd(FMT, sizeof(T), DH, NQ)) void k_packed_few(const Args a) {
@@ -474,7 +483,7 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 2 : waves_per_simd(FMT, sizeof(T),
 #pragma unroll
             for (int x = 0; x < NX; ++x)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) values.clear(x, e, sees<NX>(16 * x + e, last, first, head));
+                for (int e = 0; e < 4; ++e) values.clear(x, e, sees(16 * x + e, last, first, head));
         }
         refer(s, a.scale_log2, m_run, l_run, o);
         static_for<NX / 2>([&](auto hc) {
@@ -551,10 +560,17 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 2 : waves_per_simd(FMT, sizeof(T),
 
 // ---- many queries: the wavefronts have queries of their own and share a tile's values ------------------------------------
 // Every wavefront unpacks a quarter of a tile's values into LDS, where all of them read the second product's operand: with values unpacked by
-// every wavefront for itself they were a third of the vector instructions.  Two buffers, one barrier a tile.
-template <int FMT, class T, int DH, int NQ>
-__global__ __launch_bounds__(64 * NW, sizeof(T) == 4 && DH == 128 ? 1 : 2) void k_packed_block(const Args a) {
-    constexpr int U = DH / 16, NT = sizeof(T) == 2 ? 1 : 3;
+// every wavefront for itself they were a third of the vector instructions (4 x 1024 queries behind 3200 rows, 32 heads of 128: 288 us in 4
+// bits, 388 in 8, against 229 and 278 here).  Two buffers, one barrier a tile.
+// Bound by instructions: of those 229 us the matrix instructions are busy for two fifths of the cycles and the vector ones (exponentials,
+// maxima, unpacking) for nearly all of the others; 1.15 PFLOP/s, a library product in bf16 of 8192^3 reaches 1.21.  Unpacking costs 32 us,
+// the barrier 9.  Eight wavefronts to a tile's values took 254 us, scores of the next tile beside the exponentials 236 to 308 (registers), a
+// third wavefront of a SIMD spills.  float32's three terms take three times the products: its blocks stay with k_packed_few.
+constexpr int BLOCK_NQ = 2;
+template <int FMT, int DH>
+__global__ __launch_bounds__(64 * NW, 2) void k_packed_block(const Args a) {
+    using T = __bf16;
+    constexpr int U = DH / 16, NQ = BLOCK_NQ;
     // bf16 operands of either half of a tile: [half][channel of a lane][lane], 8 keys, 4 of each of the half's blocks
     __shared__ u32x2 lds[2][2][U][64][2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c16 = lane & 15, lg = lane >> 4;
@@ -585,7 +601,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 && DH == 128 ? 1 : 2) void 
         if (cut(a, k0, PACKED_TILE, g_min, g_max)) {
             const int off = k0 + 16 * wave + 4 * lg, last = g_max - off, first = a.window ? g_min - a.window - off : -1 - PACKED_TILE, head = a.sinks - off;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) values.clear(0, e, sees<4>(e, last, first, head));
+            for (int e = 0; e < 4; ++e) values.clear(0, e, sees(e, last, first, head));
         }
     };
     // channels 2 PR and 2 PR + 1 of this wavefront's block of 16 rows, in two steps
@@ -638,7 +654,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 && DH == 128 ? 1 : 2) void 
         // of the second, beside the second half's the unpacking of the next tile (behind the last one: the old values once more, which
         // nobody reads).
         constexpr int AHEAD = 2;
-        bf16x8 pf[2][NQ][NT], vf[AHEAD];
+        bf16x8 pf[2][NQ][1], vf[AHEAD];
         auto fragment = [&](int half, int m) { return *reinterpret_cast<const bf16x8*>(&lds[i & 1][half][m][lane][0]); };
 #pragma unroll
         for (int x = 0; x < AHEAD; ++x) vf[x] = fragment(0, x);
@@ -650,9 +666,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 && DH == 128 ? 1 : 2) void 
             const bf16x8 v = vf[m % AHEAD];
             if constexpr (half == 0 || m + AHEAD < U) vf[m % AHEAD] = m + AHEAD < U ? fragment(half, m + AHEAD) : fragment(1, m + AHEAD - U);
 #pragma unroll
-            for (int q = 0; q < NQ; ++q)
-#pragma unroll
-                for (int y = 0; y < NT; ++y) o[m][q] = mma(v, pf[half][q][y], o[m][q]);
+            for (int q = 0; q < NQ; ++q) o[m][q] = mma(v, pf[half][q][0], o[m][q]);
             if constexpr (half == 0) {
 #pragma unroll
                 for (int e = m * 8 / U; e < (m + 1) * 8 / U; ++e) exponential<true>(pf[1], s, 1, e, a.scale_log2, m_run, l_run);
@@ -672,21 +686,20 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 && DH == 128 ? 1 : 2) void 
         l_run[q] += __shfl_xor(l_run[q], 16);
         l_run[q] += __shfl_xor(l_run[q], 32);
         const int r = first + q * 16 + c16, hg = a.by_L.of(r);
-        const Result y{a, w.b, w.kvh * a.group + hg, r - hg * a.L, w.split};
         if (r >= a.n) continue;
         const float inv = l_run[q] > 0.f ? 1.0f / l_run[q] : 0.f;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
-            for (int k4 = 0; k4 < U / 4; ++k4) y.put<T, DH>((4 * lg + e) * U + 4 * k4, f32x4{o[4 * k4][q][e], o[4 * k4 + 1][q][e], o[4 * k4 + 2][q][e], o[4 * k4 + 3][q][e]}, inv);
-        if (lg == 0) y.put_ml(m_run[q], l_run[q]);
+            for (int k4 = 0; k4 < U / 4; ++k4) store4<T>(a, w.b, w.kvh * a.group + hg, r - hg * a.L, (4 * lg + e) * U + 4 * k4, inv * f32x4{o[4 * k4][q][e], o[4 * k4 + 1][q][e], o[4 * k4 + 2][q][e], o[4 * k4 + 3][q][e]});
     }
 }
 
 int clamp_int(int64_t v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : (int)v; }
 
 // What a call costs in microseconds, fitted to the times in make_plan's comment: a round of workgroups has START; a wavefront's step of
-// 64 rows takes LATENCY by itself, and a SIMD gets through one in WORK; the cache comes in at READ bytes a microsecond, into a CU at INTO_CU.
+// 64 rows takes LATENCY by itself, and a SIMD gets through one in WORK; the cache comes in at READ bytes a microsecond, into a CU at INTO_CU;
+// JOIN, and JOIN_SHARE and their bytes a share, when there are shares.
 struct Cost { double start, latency, work; };
 constexpr double READ = 5.9e6, INTO_CU = 45e3, JOIN = 4.5, JOIN_SHARE = 0.08, JOIN_BYTES = 5e6;
 Cost cost_few(int esz, int dh, int nq) {
@@ -707,6 +720,24 @@ void tiles_seen(const PackedAttn& a, int64_t n, int64_t rows, double& most, doub
     mean = mean / PACKED_TILE + (a.window ? 1 : 0.5);
 }
 
+// Four or eight wavefronts of k_packed_few with 16 queries, four with 32, shares of the keys, or k_packed_block: the one with the least time
+// by the estimate.  Measured, in us (bf16, 32 heads of 128, 4 bits where nothing else is said; "4/1" four wavefronts with 16 queries, "x 8" in
+// shares):
+//   1 x 1 query, 500 rows             4/1 6.5     8/1 7.1     4/1 x 2 9.6
+//   1 x 1, 4000                       4/1 22      8/1 17.3    4/1 x 8 11.4     8/1 x 8 12.5
+//   4 x 1, 4000                       4/1 27      8/1 20.4    4/1 x 4 19.5
+//   12 x 1, 4000                      4/1 43      8/1 47      8/1 x 2 47
+//   32 x 1, 4223                      4/1 104     8/1 103
+//   2 x 1, 60000, 8 key heads         8/1 x 16 30.5           4/1 x 37 35
+//   16 x 1, 4000, 16 heads of 64      4/1 22.6    8/1 16.9
+//   16 x 16, 4000, 8 key heads        4/1 38.6    4/2 36.2    8/1 39.3
+//   4 x 256, 3000                     4/1 88      4/2 72      block 79
+//   4 x 256, 832, 16 heads of 64, 8 bits          4/2 13.3    block 22.3
+//   16 x 64, 0                        4/1 17.4    4/2 17.7    block 10.6
+//   1 x 1024, 0                       4/2 28.0    block 27.2
+//   4 x 1024, 3200                    4/2 288     block 229     (8 bits 388, 278)
+//   8 x 1024, 0, 16 heads of 64       4/2 52      block 36
+//   float32, 6 x 5, 800, 16 heads of 64, 8 bits   4/1 9.5     8/1 8.8;   4 x 256   4/1 22.3   4/2 20.4
 // part_floats: the scratch there is (packed_attention_floats asks with as much as can be wanted)
 Plan make_plan(const PackedAttn& a, int64_t part_floats) {
     const int64_t n = (int64_t)(a.nh / a.nkv) * a.L, pairs = (int64_t)a.B * a.nkv, slot_floats = (int64_t)a.B * a.nh * a.L * (a.dh + 2);
@@ -728,13 +759,17 @@ Plan make_plan(const PackedAttn& a, int64_t part_floats) {
         const double bytes = pairs * most * tile_bytes;
         for (int waves = NW; waves <= (nq == 1 ? 2 * NW : NW); waves += NW) {
             const int places = cus * (waves > NW ? 1 : esz == 2 && nq == 1 && a.fmt == FP4 ? 3 : 2);
-            for (int split = 1; split <= slots && (split == 1 || split * waves <= most + waves); split += 1 + split / 4) {
+            auto with = [&](int split) {
+                if (split > slots || (split > 1 && split * waves > most + waves)) return;
                 const int64_t rounds = (base * split + places - 1) / places;
                 const int steps = (int)(most / (split * waves)) + 1;
                 const double alone = rounds * steps * c.latency, work = base * split * (mean / split) / (4.0 * cus) * c.work, most_of = alone > work ? alone : work;
                 const double into_cu = rounds * (most / split) * tile_bytes / INTO_CU, read = bytes / READ > into_cu ? bytes / READ : into_cu;
                 offer({nq, waves, (int)tiles, split}, rounds * c.start + sqrt(most_of * most_of + read * read) + (split > 1 ? JOIN + split * (JOIN_SHARE + slot_floats * 8.0 / JOIN_BYTES) : 0.0));
-            }
+            };
+            for (int split = 1; split <= slots; split += 1 + split / 4) with(split);
+            for (int64_t full = 1; full <= 2; ++full)      // as many as fill the chip once and twice
+                if (full * places / base > 1) with(clamp_int(full * places / base, 1, MAX_SHARES));
         }
     }
     if (esz == 2) {
@@ -742,10 +777,10 @@ Plan make_plan(const PackedAttn& a, int64_t part_floats) {
         // again; the last round is as long as its longest
         const double alone[3] = {a.dh == 128 ? 1.5 : 1.0, a.dh == 128 ? 2.0 : 1.25, 1.7}, codes = a.fmt == FP8 && a.dh == 128 ? 1.15 : 1.0, start = 6.0;
         const int per_cu = a.dh == 128 ? 2 : 3;
-        const int64_t rows = 32 * NW, tiles = (n + rows - 1) / rows, wgs = pairs * tiles, places = (int64_t)per_cu * cus, rounds = (wgs + places - 1) / places;
+        const int64_t rows = 16 * BLOCK_NQ * NW, tiles = (n + rows - 1) / rows, wgs = pairs * tiles, places = (int64_t)per_cu * cus, rounds = (wgs + places - 1) / places;
         const int64_t beside = (wgs - (rounds - 1) * places + cus - 1) / cus;
         tiles_seen(a, n, rows, most, mean);
-        offer({2, 0, (int)tiles, 1}, rounds * start + codes * ((rounds - 1) * mean * alone[per_cu - 1] + (rounds > 1 ? mean : most) * alone[beside - 1]));
+        offer({BLOCK_NQ, 0, (int)tiles, 1}, rounds * start + codes * ((rounds - 1) * mean * alone[per_cu - 1] + (rounds > 1 ? mean : most) * alone[beside - 1]));
     }
     return best;
 }
@@ -757,7 +792,7 @@ void run_cfg(Args a, hipStream_t st) {
     a.shares = a.tiles * a.nkv * a.B;
     a.by_nkv = Div(a.nkv); a.by_L = Div(a.L); a.round = a.tiles < 64 ? 64 / a.tiles : 1; a.by_round = Div(a.round * a.tiles); a.by_in_round = Div(a.round); a.by_shares = Div(a.shares);
     a.ml = a.part ? a.part + (int64_t)a.split * a.B * a.nh * a.L * DH : nullptr;
-    if constexpr (W == 0) hipLaunchKernelGGL((k_packed_block<FMT, T, DH, NQ>), dim3((unsigned)((int64_t)a.shares * a.split)), dim3(64 * NW), 0, st, a);
+    if constexpr (W == 0) hipLaunchKernelGGL((k_packed_block<FMT, DH>), dim3((unsigned)((int64_t)a.shares * a.split)), dim3(64 * NW), 0, st, a);
     else hipLaunchKernelGGL((k_packed_few<FMT, T, DH, NQ, W>), dim3((unsigned)((int64_t)a.shares * a.split)), dim3(64 * W), 0, st, a);
 }
 template <int FMT, class T, int DH>
