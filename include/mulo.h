@@ -492,7 +492,8 @@ MULO_API mulo_status mulo_check_packed_rows(const mulo_packed_kv *kv, const mulo
 /* Both run on the current HIP device and allocate nothing.
  * mulo_pack_rows writes rows of numbers into the cache and leaves its other rows as they are; mulo_unpack_rows writes rows of the
  * cache as numbers, exactly (-0 comes back as -0).  Memory that a call writes must not overlap what it reads.
- * Errors: (sequence, head)s of the cache, or rows of numbers that are written, on top of each other -> MULO_ERR_SHAPE. */
+ * Errors: (sequence, head)s of the cache, their keys and values, or rows of numbers that are written, on top of each other ->
+ * MULO_ERR_SHAPE. */
 MULO_API mulo_status mulo_pack_rows(void *hip_stream, const mulo_packed_kv *kv, const mulo_kv_rows *r);
 MULO_API mulo_status mulo_unpack_rows(void *hip_stream, const mulo_packed_kv *kv, const mulo_kv_rows *r);
 

@@ -700,7 +700,9 @@ mulo_status check_packed_rows(const mulo_packed_kv* c, const mulo_kv_rows* r, in
     }
     if (writes == 1) {
         const Dim d[] = {{c->B, c->batch}, {c->n_kv_heads, c->head}};
-        if (!apart(d, 2, c->rows / PACKED_TILE * packed_tile_bytes(c->format, c->head_dim))) return MULO_ERR_SHAPE;
+        const int64_t extent = c->rows / PACKED_TILE * packed_tile_bytes(c->format, c->head_dim);
+        const uintptr_t k = (uintptr_t)c->k, v = (uintptr_t)c->v;
+        if (!apart(d, 2, extent) || (r->k && r->v && (k < v ? v - k : k - v) < (uintptr_t)extent)) return MULO_ERR_SHAPE;
     }
     const int64_t pairs = (int64_t)c->B * c->n_kv_heads;      // fewer than 2^32 threads a launch: 16 a row, 256 for 64 rows or fewer of a pair
     if (pairs > (1 << 22) || pairs * r->L > (1 << 26)) return MULO_ERR_UNSUPPORTED;

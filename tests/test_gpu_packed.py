@@ -631,3 +631,97 @@ def test_a_contexts_cache_packed_attended_and_restored(fmt):
     torch.cuda.synchronize()
     assert torch.isfinite(logits[0]).all() and torch.equal(logits[0], logits[1])
     say("  logits of the next token, %s cache against bf16: relative 2-norm of the difference %.3g" % (fmt, ((logits[0] - logits[2]).norm() / logits[2].norm()).item()))
+
+
+# ---- calls that a careless program makes -------------------------------------------------------------------------------
+@pytest.mark.parametrize("fmt, dtype, B, L, nh, nkv, dh, P", [
+    ("fp4", "bf16", 2, 1, 8, 2, 128, 300), ("fp8", "bf16", 2, 1, 4, 1, 64, 2500), ("fp4", "bf16", 8, 128, 32, 32, 128, 0), ("fp8", "bf16", 2, 70, 4, 4, 64, 90),
+    ("fp4", "f32", 2, 5, 8, 4, 128, 200), ("fp8", "f32", 2, 40, 4, 4, 64, 100)])
+def test_a_query_that_is_not_finite_spoils_its_own_output(fmt, dtype, B, L, nh, nkv, dh, P):
+    c = make(fmt, dtype, B, L, nh, nkv, dh, P)
+    want = torch.full_like(c["q"], NAN, device=DEV)
+    plan = plan_of(c, want)
+    mulo.mulo_packed_attention(plan, workspace(plan))
+    b, h, j = B - 1, nh // 2, L // 2
+    keep = torch.ones(B, nh, L, dtype=torch.bool, device=DEV)
+    keep[b, h, j] = False
+    for bad in (NAN, float("inf"), float("-inf")):
+        for channel in (0, dh - 1):
+            q = c["q"].clone()
+            q[b, h, j, channel] = bad
+            out = torch.full_like(want, 7.0)
+            plan = plan_of(c, out, q=q.to(DEV))
+            mulo.mulo_packed_attention(plan, workspace(plan))
+            torch.cuda.synchronize()
+            assert torch.equal(out[keep], want[keep]), (bad, channel)
+
+
+@pytest.mark.parametrize("fmt, dtype, L", [("fp4", "bf16", 1), ("fp8", "f32", 7), ("fp4", "bf16", 140)])
+def test_the_lowest_and_the_highest_starts(fmt, dtype, L):
+    """Starts at either end of the type: absent, and the last rows that there are."""
+    B, nkv, dh, rows = 4, 2, 64, 192
+    low, high = -2 ** 31, 2 ** 31 - 1
+    starts = torch.tensor([low, high, 0, low], dtype=torch.int32, device=DEV)
+    g = torch.Generator().manual_seed(6)
+    tiles = [torch.full((B, nkv, rows // 64, OP.tile_bytes(fmt, dh)), 0x2A, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    before = tiles[0].clone()
+    x = [torch.randn(B, nkv, L, dh, generator=g).to(DT[dtype]).to(DEV) for _ in range(2)]
+    packed = packed_of(*tiles, fmt, dh)
+    mulo.mulo_pack_rows(packed, mulo.make_kv_rows(*x, rows - L, starts))
+    back = [torch.full_like(y, 5.0) for y in x]
+    mulo.mulo_unpack_rows(packed, mulo.make_kv_rows(*back, rows - L, starts))
+    torch.cuda.synchronize()
+    for t in tiles:
+        assert torch.equal(t[[0, 3]], before[[0, 3]])
+    for y, z in zip(x, back):
+        want = torch.tensor(OP.decode(*OP.encode(y.double().cpu().numpy(), fmt), fmt)).to(DT[dtype])
+        assert torch.equal(z[[1, 2]].cpu(), want[[1, 2]]) and (z[[0, 3]] == 5).all()
+    q = torch.randn(B, 4, L, dh, generator=g).to(DT[dtype]).to(DEV)
+    clamped = torch.tensor([-1, rows - L, 0, -1], dtype=torch.int32, device=DEV)
+    for window in (0, 30):
+        outs = []
+        for s in (starts, clamped):
+            out = torch.full_like(q, NAN)
+            plan = mulo.make_packed_attention(packed, q, out, rows - L, P_seq=s, window=window, sinks=3)
+            mulo.mulo_packed_attention(plan, workspace(plan))
+            outs.append(out)
+        torch.cuda.synchronize()
+        assert torch.isfinite(outs[0]).all() and torch.equal(*outs) and (outs[0][[0, 3]] == 0).all()
+
+
+def test_two_graphs_on_two_streams():
+    """Two recorded calls, each with scratch of its own, replayed beside each other and beside eager calls."""
+    cs = [make(fmt, "bf16", 2, 1, 8, 8, 128, P) for fmt, P in (("fp4", 3000), ("fp8", 2500))]
+    wants, outs, plans, spaces, graphs, sides = [], [], [], [], [], []
+    for c in cs:
+        want = torch.full_like(c["q"], NAN, device=DEV)
+        plan = plan_of(c, want)
+        mulo.mulo_packed_attention(plan, workspace(plan))
+        wants.append(want)
+        out = torch.full_like(want, NAN)
+        plan = plan_of(c, out)
+        plans.append(plan)
+        spaces.append(workspace(plan))
+        outs.append(out)
+        sides.append(torch.cuda.Stream())
+    torch.cuda.synchronize()
+    assert all(mulo.mulo_packed_attention_workspace_bytes(p) for p in plans)
+    for plan, ws, side in zip(plans, spaces, sides):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            mulo.mulo_packed_attention(plan, ws)
+        graphs.append(graph)
+    for rep in range(4):
+        for out in outs:
+            out.fill_(NAN)
+        torch.cuda.synchronize()
+        for graph, side in zip(graphs, sides):
+            with torch.cuda.stream(side):
+                for _ in range(3):
+                    graph.replay()
+        eager = torch.full_like(wants[0], NAN)
+        plan = plan_of(cs[0], eager)
+        mulo.mulo_packed_attention(plan, workspace(plan))
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], wants[0]) and torch.equal(outs[1], wants[1]) and torch.equal(eager, wants[0]), rep
+    del graphs

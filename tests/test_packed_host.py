@@ -201,3 +201,15 @@ def test_binding_refuses_tensors_that_do_not_fit():
         mulo.make_kv_rows(None, None, 0)
     with pytest.raises(ValueError):
         mulo.make_kv_rows(torch.zeros(1, 1, 1, 64), torch.zeros(1, 1, 2, 64), 0)
+
+
+@pytest.mark.parametrize("apart", [-HEAD + 16, -16, 16, HEAD - 16])
+def test_keys_and_values_on_top_of_each_other_are_not_written(lib, apart):
+    kv, r = split(dict(pv=(1 << 20) + apart))
+    assert lib.mulo_pack_rows(None, C.byref(kv), C.byref(r)) == SHAPE
+    for there in ("k", "v"):      # the one that the call leaves alone may lie anywhere
+        kv, r = split({there: None, "pv": (1 << 20) + apart})
+        assert lib.mulo_check_packed_rows(C.byref(kv), C.byref(r)) == 0
+    # keys and values of a head in turn
+    kv, r = split(dict(pv=(1 << 20) + HEAD, head=2 * HEAD, batch=4 * HEAD))
+    assert lib.mulo_check_packed_rows(C.byref(kv), C.byref(r)) == 0
