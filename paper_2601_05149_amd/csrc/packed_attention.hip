@@ -150,6 +150,13 @@ template <int FMT, int DH, int NX> struct Values {
         }
     }
 };
+// A query's first term is rounded, and rounded up from the last of float32's numbers it would be 2^128, an infinity: the first term of those is
+// the largest there is of its form (15 16 2^120 in four bits, which leaves 15 2^120 of bf16's largest, (2^8 - 1) 2^120 in bf16), and the other
+// terms hold the rest as exactly as of all others.
+template <class T> __device__ __forceinline__ float within(float x) {
+    constexpr float TOP = sizeof(T) == 2 ? 0x1.Ep127f : 0x1.FEp127f;
+    return __builtin_amdgcn_fmed3f(x, -TOP, TOP);
+}
 // 16 queries, one a lane: the terms of its channels
 template <class T, int DH> struct Query {
     static constexpr int NC = DH / 32;      // float32: chunks of 8 channels of a lane
@@ -187,8 +194,8 @@ template <class T, int DH> struct Query {
 #pragma unroll
                     for (int f = 0; f < 4; ++f) v[f] = (float)x[y][e >> 1][(e & 1) * 4 + f];
                     i16x2 w = {0, 0}, z = {0, 0};
-                    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, v[0], v[1], s_hi, false);
-                    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, v[2], v[3], s_hi, true);
+                    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, within<T>(v[0]), within<T>(v[1]), s_hi, false);
+                    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, within<T>(v[2]), within<T>(v[3]), s_hi, true);
                     const uint32_t h = __builtin_bit_cast(uint32_t, w);
                     const f32x2 d0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(h, s_hi, false), d1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(h, s_hi, true);
                     z = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(z, v[0] - d0.x, v[1] - d0.y, s_lo, false);
@@ -220,7 +227,7 @@ template <class T, int DH> struct Query {
                     float x = e < 4 ? x0[e & 3] : x1[e & 3];
 #pragma unroll
                     for (int y = 0; y < 3; ++y) {
-                        term[y][c][e] = (__bf16)x;
+                        term[y][c][e] = (__bf16)(y == 0 ? within<T>(x) : x);
                         x -= (float)term[y][c][e];
                     }
                 }

@@ -443,6 +443,35 @@ def test_very_large_and_very_small_numbers(fmt, dtype, size):
     check(c, out, "numbers of %g" % size, plain(c))
 
 
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+@pytest.mark.parametrize("dtype, B, L, nh, nkv, dh, P", [
+    ("bf16", 3, 1, 4, 2, 128, 100), ("bf16", 2, 20, 4, 4, 64, 90), ("bf16", 2, 1, 4, 2, 64, 3000), ("bf16", 8, 128, 32, 32, 128, 0), ("bf16", 16, 128, 32, 32, 64, 70),
+    ("f32", 3, 1, 4, 2, 128, 100), ("f32", 2, 20, 4, 4, 64, 90), ("f32", 2, 1, 4, 2, 64, 3000)])
+def test_queries_at_the_end_of_their_type(fmt, dtype, B, L, nh, nkv, dh, P):
+    """The largest numbers a query can hold against the smallest keys of a cache, so that the scores are ordinary numbers (the queries'
+    2^128, the keys' 2^-117 and a scale of 2^-14).  Whole queries from 0.9 of the largest number up, and queries with the largest one
+    beside ordinary numbers."""
+    c = make(fmt, dtype, B, L, nh, nkv, dh, P)
+    code, scale = OP.from_tiles(c["tk"].numpy(), fmt, dh, True)
+    scale = np.where(scale == 255, 255, 10).astype(np.uint8)
+    if fmt == "fp8":      # up to 7.5
+        code = np.where((code & 127) < 0x50, code, code & 0x80 | code & 7 | 0x48).astype(np.uint8)
+        code[scale.repeat(32, -1) == 255] = 255
+    c["tk"], c["k"] = torch.tensor(OP.to_tiles(code, scale, fmt, True)), torch.tensor(OP.decode(code, scale, fmt))
+    top = torch.finfo(DT[dtype]).max
+    g = torch.Generator().manual_seed(7)
+    q = ((0.9 + 0.1 * torch.rand(c["q"].shape, generator=g, dtype=torch.float64)) * top * (1 - 2 * torch.randint(0, 2, c["q"].shape, generator=g))).clamp(-top, top)
+    q[0, ::2] = torch.randn(q[0, ::2].shape, generator=g, dtype=torch.float64)
+    q[0, ::2, :, 0], q[0, ::2, :, dh - 1] = top, -top
+    c["q"] = q.to(DT[dtype])
+    assert torch.isfinite(c["q"]).all() and (c["q"].abs() == top).any()
+    out = torch.full_like(c["q"], NAN, device=DEV)
+    plan = plan_of(c, out, scale=2.0 ** -14)
+    mulo.mulo_packed_attention(plan, workspace(plan))
+    torch.cuda.synchronize()
+    check(c, out, "queries up to %g" % top, plain(c, 2.0 ** -14))
+
+
 @pytest.mark.parametrize("L", [1, 20, 150])
 def test_strides(L):
     """Token-major queries and output inside a wider row, a cache whose heads lie in front of its sequences and inside a larger one; what
