@@ -505,8 +505,9 @@ MULO_API mulo_status mulo_unpack_rows(void *hip_stream, const mulo_packed_kv *kv
  *   dtype        mulo_dtype of q and out
  *   q, out       element (b, h, j, c) at q_batch b + q_head h + q_row j + c, n_heads heads (head h reads n_kv_heads * h / n_heads)
  *   P, P_seq, sinks, window, scale  as mulo_attention_args; rows P_b .. P_b + L-1 hold the block's own keys and values
- * Rows that no query of the call sees may hold anything; what some query sees has to be finite.  q and out must not overlap.
- * batch and head of the cache may be 0 (sequences or heads that share theirs).
+ * Rows that no query of the call sees may hold anything; what some query sees has to be finite.  A query with an infinity or a NaN gets NaN
+ * in all channels, an absent sequence zeros whatever its queries hold.  q and out must not overlap.  batch and head of the cache may
+ * be 0 (sequences or heads that share theirs).
  * Limits: those of mulo_packed_kv; q, out and their strides of 16 bytes; n_heads a multiple of n_kv_heads; B * n_heads <= 2^22,
  * B * n_heads * L < 2^26. */
 typedef struct {

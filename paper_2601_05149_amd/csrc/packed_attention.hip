@@ -561,7 +561,7 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 2 : waves_per_simd(FMT, sizeof(T),
             for (int x = 0; x < W; ++x) sum += f[x] * acc[x][row * (DH / 4) + (c4 ^ row)];
             y.put<T, DH>(c4 * 4, sum, inv);
         }
-        if ((tid & 15) == 0) y.put_ml(M, den);
+        if ((tid & 15) == 0) y.put_ml(den >= 0.f ? M : den, den);      // a query with NaN or an infinity has no maximum, and its share is not an empty one
     }
 }
 

@@ -685,6 +685,27 @@ def test_a_query_that_is_not_finite_spoils_its_own_output(fmt, dtype, B, L, nh, 
             assert torch.equal(out[keep], want[keep]), (bad, channel)
 
 
+@pytest.mark.parametrize("fmt, dtype, B, L, nh, nkv, dh, P, shares", [
+    ("fp4", "bf16", 2, 1, 8, 2, 128, 300, False), ("fp4", "bf16", 8, 128, 32, 32, 128, 0, False), ("fp8", "bf16", 2, 70, 4, 4, 64, 90, False),
+    ("fp4", "f32", 2, 5, 8, 4, 128, 200, False), ("fp8", "f32", 2, 40, 4, 4, 64, 100, False),
+    ("fp8", "bf16", 2, 1, 4, 1, 64, 2500, True), ("fp4", "bf16", 2, 3, 8, 2, 128, 4000, True), ("fp4", "f32", 2, 3, 4, 2, 128, 2500, True), ("fp8", "f32", 2, 2, 8, 8, 64, 3000, True)])
+def test_a_query_that_is_not_finite_is_answered_with_nan(fmt, dtype, B, L, nh, nkv, dh, P, shares):
+    """All of its channels, also where its keys are dealt to several workgroups."""
+    c = make(fmt, dtype, B, L, nh, nkv, dh, P)
+    b, h, j = B - 1, nh // 2, L // 2
+    for bad in (NAN, float("inf"), float("-inf")):
+        q = c["q"].clone()
+        q[b, h, j, 1] = bad
+        out = torch.full_like(q, 7.0, device=DEV)
+        plan = plan_of(c, out, q=q.to(DEV))
+        assert (mulo.mulo_packed_attention_workspace_bytes(plan) > 0) == shares
+        for ws in (workspace(plan, 0), None):
+            mulo.mulo_packed_attention(plan, ws)
+            torch.cuda.synchronize()
+            nans = torch.isnan(out).sum(-1).tolist()
+            assert nans[b][h][j] == dh and np.sum(nans) == dh, bad
+
+
 @pytest.mark.parametrize("fmt, dtype, L", [("fp4", "bf16", 1), ("fp8", "f32", 7), ("fp4", "bf16", 140)])
 def test_the_lowest_and_the_highest_starts(fmt, dtype, L):
     """Starts at either end of the type: absent, and the last rows that there are."""
