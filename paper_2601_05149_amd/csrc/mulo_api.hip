@@ -527,9 +527,12 @@ bool context_sizes_ok(const mulo_ctx* ctx, int rows) {
            ctx->cfg.max_seq % (int)(16 / ctx->esz) == 0 && rows <= (1 << 24) && ctx->cfg.max_seq <= (1 << 24);
 }
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-// Are the places of an array apart?  Every dimension has to step over what lies inside it (runs of `extent` innermost), in one order or another.
+// Are the places of an array apart?  Every dimension has to step over what lies inside it (runs of `run` innermost), in one order or another.
+// (2^26 steps of 2^40 pass 64 bits.)
+typedef __int128 wide;
 struct Dim { int64_t n, step; };
-bool apart(const Dim* dims, int n_dims, int64_t extent) {
+bool apart(const Dim* dims, int n_dims, int64_t run) {
+    wide extent = run;
     Dim d[4];
     for (int i = 0; i < n_dims; ++i) d[i] = dims[i];
     for (int i = 0; i < n_dims; ++i)      // innermost first
@@ -538,7 +541,7 @@ bool apart(const Dim* dims, int n_dims, int64_t extent) {
     for (int i = 0; i < n_dims; ++i) {
         if (d[i].n == 1) continue;
         if (d[i].step < extent) return false;
-        extent += (d[i].n - 1) * d[i].step;
+        extent += (wide)(d[i].n - 1) * d[i].step;
     }
     return true;
 }

@@ -213,3 +213,18 @@ def test_keys_and_values_on_top_of_each_other_are_not_written(lib, apart):
     # keys and values of a head in turn
     kv, r = split(dict(pv=(1 << 20) + HEAD, head=2 * HEAD, batch=4 * HEAD))
     assert lib.mulo_check_packed_rows(C.byref(kv), C.byref(r)) == 0
+
+
+FAR = (1 << 40) - 8      # 2^24 rows of such a stride span 2^64 numbers
+
+
+@pytest.mark.parametrize("changes", [dict(k_row=FAR, k_batch=1 << 40, v=None, pv=None), dict(v_row=FAR, v_batch=1 << 40, k=None, pk=None)], ids=["k", "v"])
+def test_rows_on_top_of_each_other_whose_span_passes_64_bits(lib, changes):
+    kv, r = split(dict(changes, rows=1 << 24, L=1 << 24, P=0, B=2, n_kv_heads=1, batch=1 << 30))
+    assert lib.mulo_check_packed_rows(C.byref(kv), C.byref(r)) == 0
+    assert lib.mulo_unpack_rows(None, C.byref(kv), C.byref(r)) == SHAPE
+
+
+def test_outputs_on_top_of_each_other_whose_span_passes_64_bits(lib):
+    a = attention_args(rows=1 << 24, L=1 << 24, P=0, B=2, n_kv_heads=1, n_heads=1, out_row=FAR, out_batch=1 << 40)
+    assert lib.mulo_check_packed_attention(C.byref(a)) == SHAPE
