@@ -486,14 +486,16 @@ typedef struct {
     const int32_t *P_seq;
 } mulo_kv_rows;
 
-/* Host-side check of the arguments (no GPU needed), also run by the two calls below. */
+/* Host-side check of the arguments (no GPU needed), also run by the two calls below: of everything that holds for both.  Either call refuses
+ * besides what it would write on top of itself. */
 MULO_API mulo_status mulo_check_packed_rows(const mulo_packed_kv *kv, const mulo_kv_rows *r);
 
 /* Both run on the current HIP device and allocate nothing.
  * mulo_pack_rows writes rows of numbers into the cache and leaves its other rows as they are; mulo_unpack_rows writes rows of the
  * cache as numbers, exactly (-0 comes back as -0).  Memory that a call writes must not overlap what it reads.
- * Errors: (sequence, head)s of the cache, their keys and values, or rows of numbers that are written, on top of each other ->
- * MULO_ERR_SHAPE. */
+ * Errors: what a call writes on top of each other -> MULO_ERR_SHAPE: (sequence, head)s of the cache, all of their rows, keys and values
+ * alike; rows of numbers, keys and values alike, which may lie in each other's gaps.  MULO_ERR_UNSUPPORTED: keys and values of
+ * unlike strides in each other's gaps, more than 2^16 of them. */
 MULO_API mulo_status mulo_pack_rows(void *hip_stream, const mulo_packed_kv *kv, const mulo_kv_rows *r);
 MULO_API mulo_status mulo_unpack_rows(void *hip_stream, const mulo_packed_kv *kv, const mulo_kv_rows *r);
 

@@ -545,6 +545,57 @@ bool apart(const Dim* dims, int n_dims, int64_t run) {
     }
     return true;
 }
+// The places of an array whose dimensions are apart, innermost first, those that make a longer run folded into it.
+struct Places {
+    Dim d[4];
+    wide extent[5];      // of the first 0, 1, .. dimensions; extent[0]: a run
+    int n = 0;
+    Places(const Dim* dims, int n_dims, int64_t run) {
+        for (int i = 0; i < n_dims; ++i) {
+            if (dims[i].n == 1) continue;
+            int at = n++;
+            for (; at > 0 && d[at - 1].step > dims[i].step; --at) d[at] = d[at - 1];
+            d[at] = dims[i];
+        }
+        extent[0] = run;
+        int folded = 0;
+        while (folded < n && d[folded].step == extent[0]) extent[0] *= d[folded++].n;
+        n -= folded;
+        for (int i = 0; i < n; ++i) {
+            d[i] = d[i + folded];
+            extent[i + 1] = extent[i] + (wide)(d[i].n - 1) * d[i].step;
+        }
+    }
+};
+wide down(wide a, wide b) { return a >= 0 ? a / b : -((b - 1 - a) / b); }      // a / b rounded down
+enum class Meet { no, yes, unknown };
+// Is some place of a (its first na dimensions) one of b, which begins `off` behind it?  Blocks of the outermost dimension whose spans meet are looked
+// into: where both have the same step at most three differences of their numbers, else every such block of the array with the larger one.
+// left: how many blocks may still be looked into.
+Meet meet(const Places& a, int na, const Places& b, int nb, wide off, int& left) {
+    if (off >= a.extent[na] || off + b.extent[nb] <= 0) return Meet::no;
+    if (!na && !nb) return Meet::yes;
+    if (--left < 0) return Meet::unknown;
+    const int64_t sa = na ? a.d[na - 1].step : 0, sb = nb ? b.d[nb - 1].step : 0, step = sa > sb ? sa : sb;
+    const bool in_a = sa == step, in_b = sb == step;
+    const wide ea = a.extent[na - in_a], eb = b.extent[nb - in_b];
+    // off + m step, of block j of b (of all of it: 0) against block i of a, m = j - i
+    wide first = down(-eb - off, step) + 1, last = down(ea - off - 1, step);
+    const wide least = in_a ? 1 - a.d[na - 1].n : 0, most = in_b ? b.d[nb - 1].n - 1 : 0;
+    if (first < least) first = least;
+    if (last > most) last = most;
+    for (wide m = first; m <= last; ++m) {
+        const Meet x = meet(a, na - in_a, b, nb - in_b, off + m * step, left);
+        if (x != Meet::no) return x;
+    }
+    return Meet::no;
+}
+// Is a place of one array a place of the other (`off` units behind it)?  Unlike steps that interleave in more than 2^16 blocks are not gone through.
+mulo_status separate(const Places& a, const Places& b, int64_t off) {
+    int left = 1 << 16;
+    const Meet x = meet(a, a.n, b, b.n, off, left);
+    return x == Meet::no ? MULO_OK : x == Meet::yes ? MULO_ERR_SHAPE : MULO_ERR_UNSUPPORTED;
+}
 }  // namespace
 
 mulo_status mulo_attach_prefix(mulo_ctx* ctx, const mulo_prefix* p) {
@@ -675,6 +726,8 @@ mulo_status check_packed_rows(const mulo_packed_kv* c, const mulo_kv_rows* r, in
     if (s != MULO_OK) return s;
     if ((int64_t)r->P + r->L > c->rows) return MULO_ERR_SHAPE;
     const int unit = r->dtype == MULO_BF16 ? 8 : 4;      // elements of 16 bytes
+    const Dim k_dims[] = {{c->B, r->k_batch}, {c->n_kv_heads, r->k_head}, {r->L, r->k_row}};
+    const Dim v_dims[] = {{c->B, r->v_batch}, {c->n_kv_heads, r->v_head}, {r->L, r->v_row}, {c->head_dim, r->v_chan}};
     if (r->k) {
         const int64_t strides[] = {r->k_batch, r->k_head, r->k_row};
         for (const int64_t x : strides)
@@ -682,8 +735,7 @@ mulo_status check_packed_rows(const mulo_packed_kv* c, const mulo_kv_rows* r, in
         for (const int64_t x : strides)
             if (x % unit) return MULO_ERR_UNSUPPORTED;
         if (!aligned16(r->k)) return MULO_ERR_UNSUPPORTED;
-        const Dim d[] = {{c->B, r->k_batch}, {c->n_kv_heads, r->k_head}, {r->L, r->k_row}};
-        if (writes == 2 && !apart(d, 3, c->head_dim)) return MULO_ERR_SHAPE;
+        if (writes == 2 && !apart(k_dims, 3, c->head_dim)) return MULO_ERR_SHAPE;
     }
     if (r->v) {
         const int64_t strides[] = {r->v_batch, r->v_head, r->v_row, r->v_chan};
@@ -697,19 +749,20 @@ mulo_status check_packed_rows(const mulo_packed_kv* c, const mulo_kv_rows* r, in
         } else if ((uintptr_t)r->v % (r->dtype == MULO_BF16 ? 2 : 4)) {
             return MULO_ERR_UNSUPPORTED;
         }
-        const Dim d[] = {{c->B, r->v_batch}, {c->n_kv_heads, r->v_head}, {r->L, r->v_row}, {c->head_dim, r->v_chan}};
-        if (writes == 2 && !apart(d, 4, 1)) return MULO_ERR_SHAPE;
-        if (writes == 2 && r->k == r->v) return MULO_ERR_SHAPE;
+        if (writes == 2 && !apart(v_dims, 4, 1)) return MULO_ERR_SHAPE;
     }
-    if (writes == 1) {
-        const Dim d[] = {{c->B, c->batch}, {c->n_kv_heads, c->head}};
-        const int64_t extent = c->rows / PACKED_TILE * packed_tile_bytes(c->format, c->head_dim);
-        const uintptr_t k = (uintptr_t)c->k, v = (uintptr_t)c->v;
-        if (!apart(d, 2, extent) || (r->k && r->v && (k < v ? v - k : k - v) < (uintptr_t)extent)) return MULO_ERR_SHAPE;
-    }
+    const Dim heads[] = {{c->B, c->batch}, {c->n_kv_heads, c->head}};
+    const int64_t head_bytes = c->rows / PACKED_TILE * packed_tile_bytes(c->format, c->head_dim);
+    if (writes == 1 && !apart(heads, 2, head_bytes)) return MULO_ERR_SHAPE;
     const int64_t pairs = (int64_t)c->B * c->n_kv_heads;      // fewer than 2^32 threads a launch: 16 a row, 256 for 64 rows or fewer of a pair
     if (pairs > (1 << 22) || pairs * r->L > (1 << 26)) return MULO_ERR_UNSUPPORTED;
-    return MULO_OK;
+    if (!r->k || !r->v || !writes) return MULO_OK;
+    // keys and values of a call are written at once
+    if (writes == 1) {
+        const Places of(heads, 2, head_bytes);
+        return separate(of, of, (int64_t)((uintptr_t)c->v - (uintptr_t)c->k));
+    }
+    return separate(Places(k_dims, 3, c->head_dim), Places(v_dims, 4, 1), (int64_t)((uintptr_t)r->v - (uintptr_t)r->k) / (16 / unit));
 }
 PackedRows packed_rows(const mulo_packed_kv* c, const mulo_kv_rows* r) {
     PackedRows a{};
@@ -724,6 +777,9 @@ PackedRows packed_rows(const mulo_packed_kv* c, const mulo_kv_rows* r) {
 }  // namespace
 
 mulo_status mulo_check_packed_rows(const mulo_packed_kv* kv, const mulo_kv_rows* r) { return check_packed_rows(kv, r, 0); }
+
+// For the tests of what the two calls below refuse, and not part of the interface (mulo.h does not declare it): their checks alone.
+MULO_API mulo_status mulo_internal_check_rows(const mulo_packed_kv* kv, const mulo_kv_rows* r, int32_t writes) { return check_packed_rows(kv, r, writes); }
 
 mulo_status mulo_pack_rows(void* hip_stream, const mulo_packed_kv* kv, const mulo_kv_rows* r) {
     const mulo_status s = check_packed_rows(kv, r, 1);

@@ -706,6 +706,35 @@ def test_a_query_that_is_not_finite_is_answered_with_nan(fmt, dtype, B, L, nh, n
             assert nans[b][h][j] == dh and np.sum(nans) == dh, bad
 
 
+def test_keys_and_values_out_of_one_tensor():
+    """Heads of one cache, and of one tensor of rows: next to each other and in turn they are written, on top of each other they are not."""
+    B, nkv, L, dh, rows = 2, 2, 5, 64, 64
+    g = torch.Generator().manual_seed(2)
+    x = [torch.randn(B, nkv, L, dh, generator=g).bfloat16() for _ in range(2)]
+    size = OP.tile_bytes("fp4", dh)
+    both = lambda t, how: (t[:, :nkv], t[:, nkv:2 * nkv]) if how == "next" else (t[:, 0:2 * nkv:2], t[:, 1:2 * nkv:2]) if how == "in turn" else (t[:, :nkv], t[:, 1:nkv + 1])
+    row_in = mulo.make_kv_rows(*(t.to(DEV) for t in x), 3)
+    want = [torch.tensor(OP.decode(*OP.encode(t.double().numpy(), "fp4"), "fp4")) for t in x]
+    for cache_how in ("next", "in turn"):
+        tiles = torch.zeros(B, 2 * nkv, rows // 64, size, dtype=torch.uint8, device=DEV)
+        packed = packed_of(*both(tiles, cache_how), "fp4", dh)
+        mulo.mulo_pack_rows(packed, row_in)
+        for how in ("next", "in turn"):
+            big = torch.full((B, 2 * nkv, L, dh), NAN, dtype=torch.bfloat16, device=DEV)
+            out = both(big, how)
+            mulo.mulo_unpack_rows(packed, mulo.make_kv_rows(*out, 3))
+            torch.cuda.synchronize()
+            assert all(torch.equal(o.double().cpu(), w) for o, w in zip(out, want)), (cache_how, how)
+        before = big.clone()
+        with pytest.raises(mulo.MuloError):
+            mulo.mulo_unpack_rows(packed, mulo.make_kv_rows(*both(big, "shifted"), 3))
+        assert torch.equal(big, before)
+    before = tiles.clone()
+    with pytest.raises(mulo.MuloError):
+        mulo.mulo_pack_rows(packed_of(*both(tiles, "shifted"), "fp4", dh), row_in)
+    assert torch.equal(tiles, before)
+
+
 @pytest.mark.parametrize("fmt, dtype, L", [("fp4", "bf16", 1), ("fp8", "f32", 7), ("fp4", "bf16", 140)])
 def test_the_lowest_and_the_highest_starts(fmt, dtype, L):
     """Starts at either end of the type: absent, and the last rows that there are."""

@@ -228,3 +228,115 @@ def test_rows_on_top_of_each_other_whose_span_passes_64_bits(lib, changes):
 def test_outputs_on_top_of_each_other_whose_span_passes_64_bits(lib):
     a = attention_args(rows=1 << 24, L=1 << 24, P=0, B=2, n_kv_heads=1, n_heads=1, out_row=FAR, out_batch=1 << 40)
     assert lib.mulo_check_packed_attention(C.byref(a)) == SHAPE
+
+
+# ---- keys and values on top of each other ----------------------------------------------------------------------------
+PACK, UNPACK = 1, 2
+
+
+def refusal(lib, writes, **changes):
+    kv, r = split(changes)
+    return lib.mulo_internal_check_rows(C.byref(kv), C.byref(r), writes)
+
+
+@pytest.mark.parametrize("status, apart, changes", [
+    (SHAPE, HEAD, {}), (SHAPE, -HEAD, {}), (SHAPE, 2 * HEAD, {}), (SHAPE, 7 * HEAD, {}), (SHAPE, -7 * HEAD + 16, {}), (SHAPE, 8 * HEAD - 16, {}), (0, 8 * HEAD, {}), (0, -8 * HEAD, {}),
+    # a head, or a sequence, in turn
+    (0, HEAD, dict(head=2 * HEAD, batch=4 * HEAD)), (SHAPE, 2 * HEAD, dict(head=2 * HEAD, batch=4 * HEAD)), (0, 3 * HEAD, dict(head=2 * HEAD, batch=4 * HEAD)),
+    (0, 2 * HEAD, dict(batch=4 * HEAD)), (SHAPE, 3 * HEAD, dict(batch=4 * HEAD)), (0, 6 * HEAD, dict(batch=4 * HEAD)), (SHAPE, 12 * HEAD, dict(batch=4 * HEAD)), (0, 14 * HEAD, dict(batch=4 * HEAD)),
+    # gaps of exactly a head
+    (0, HEAD, dict(head=3 * HEAD, batch=6 * HEAD)), (0, 2 * HEAD, dict(head=3 * HEAD, batch=6 * HEAD)), (SHAPE, 2 * HEAD + 16, dict(head=3 * HEAD, batch=6 * HEAD)),
+    # heads outside of sequences
+    (SHAPE, 4 * HEAD, dict(batch=HEAD, head=4 * HEAD)), (0, 8 * HEAD, dict(batch=HEAD, head=4 * HEAD)),
+], ids=str)
+def test_keys_on_values_of_another_head_are_not_written(lib, status, apart, changes):
+    assert refusal(lib, PACK, pv=(1 << 20) + apart, **changes) == status
+    if status:
+        kv, r = split(dict(changes, pv=(1 << 20) + apart))
+        assert lib.mulo_pack_rows(None, C.byref(kv), C.byref(r)) == status
+    assert refusal(lib, UNPACK, pv=(1 << 20) + apart, v=1 << 18, **changes) == 0       # read only
+
+
+# rows of numbers, bytes from the keys to the values: 3 rows of 64 bf16 numbers of 2 heads of 4 sequences are 3072 bytes
+TOKENS = dict(k_row=128, k_head=64, k_batch=384, v_row=128, v_head=64, v_batch=384)
+FUSED = dict(k_row=256, k_head=64, k_batch=768, v_row=256, v_head=64, v_batch=768)      # a token's keys, then its values
+
+
+@pytest.mark.parametrize("status, apart, changes", [
+    (SHAPE, 16, {}), (SHAPE, -16, {}), (SHAPE, 768, {}), (SHAPE, 3056, {}), (0, 3072, {}), (0, -3072, {}), (SHAPE, 3072, dict(dtype=0)), (0, 6144, dict(dtype=0)),
+    (SHAPE, 256, TOKENS), (SHAPE, 128, TOKENS), (0, 3072, TOKENS),
+    (0, 256, FUSED), (0, -256, FUSED), (SHAPE, 128, FUSED), (SHAPE, 240, FUSED), (0, 512 + 256, FUSED), (SHAPE, 512, FUSED), (0, 1536 + 256, FUSED),
+    # heads of keys and, behind them, channels of rows; of other steps inside a head
+    (0, 384, dict(ACROSS, k_head=384, v_head=384, k_batch=768, v_batch=768)), (SHAPE, 382, dict(ACROSS, k_head=384, v_head=384, k_batch=768, v_batch=768)),
+    (SHAPE, 384, dict(ACROSS, v_chan=4, k_head=384, v_head=384, k_batch=768, v_batch=768)),
+    # values in the gaps of every second row of the keys, and on one of their rows
+    (0, 128, dict(k_row=128, k_head=1024, k_batch=4096, v_row=256, v_head=1024, v_batch=4096)), (SHAPE, 128 + 64, dict(k_row=128, k_head=1024, k_batch=4096, v_row=192, v_head=1024, v_batch=4096)),
+    # batches of other steps far apart
+    (0, 1 << 30, dict(v_batch=1 << 20)),
+], ids=str)
+def test_rows_on_top_of_each_other_are_not_written(lib, status, apart, changes):
+    assert refusal(lib, UNPACK, k=1 << 20, v=(1 << 20) + apart, pv=1 << 25, **changes) == status
+    if status:
+        kv, r = split(dict(changes, k=1 << 20, v=(1 << 20) + apart))
+        assert lib.mulo_unpack_rows(None, C.byref(kv), C.byref(r)) == status
+    assert refusal(lib, PACK, k=1 << 20, v=(1 << 20) + apart, pv=1 << 25, **changes) == 0       # read only
+
+
+def test_steps_that_interleave_without_end(lib):
+    """Keys every 128 numbers, values of unlike steps in their gaps: gone through up to a limit."""
+    far = dict(B=1, n_kv_heads=1, rows=1 << 20, P=0, k=1 << 20, v=(1 << 20) + 128, pv=1 << 40, k_row=128, v_row=256, batch=0, head=0)
+    assert refusal(lib, UNPACK, L=1000, **far) == 0
+    assert refusal(lib, UNPACK, L=1 << 18, **far) == UNSUPPORTED
+
+
+def test_random_layouts_against_sets_of_places(lib):
+    rng = np.random.default_rng(5)
+
+    def places(dims, run):
+        at = np.arange(run)
+        for n, step in dims:
+            at = (at[None] + (np.arange(n) * step).reshape(-1, *[1] * at.ndim)).reshape(-1)
+        return at
+
+    def nested(dims, unit, tight):
+        """Steps that step over what lies inside, the dimensions in a random order of nesting."""
+        steps, extent = [0] * len(dims), unit[1]
+        for i in rng.permutation(len(dims)):
+            steps[i] = -(-extent // unit[0]) * unit[0] + unit[0] * int(rng.integers(0, 1 if tight else 20))
+            extent += (dims[i] - 1) * steps[i]
+        return steps
+
+    found = {0: 0, SHAPE: 0}
+    for trial in range(1500):
+        B, nkv, L = (int(x) for x in rng.integers(1, 4, 3))
+        across, alike = trial % 3 == 0, trial % 2
+        ks = nested([B, nkv, L], (8, 64), rng.random() < 0.3)
+        if across:
+            extent = L + int(rng.integers(1, 9))      # (1: rows of channels)
+            outer = nested([B, nkv], (1, 63 * extent + L), rng.random() < 0.3)
+            if alike:      # steps that step over the keys and the values of a head
+                inside = max(63 * extent + L, 64 + (L - 1) * ks[2]) + 64 * int(rng.integers(0, 60))
+                outer = nested([B, nkv], (8, inside), True)
+                ks[:2] = outer
+            vs, chan = outer + [1], extent
+        else:
+            vs, chan = list(ks) if alike else nested([B, nkv, L], (8, 64), rng.random() < 0.3), 1
+        kp, vp = places(list(zip((B, nkv, L), ks)), 64), places(list(zip((B, nkv, L, 64), vs + [chan])), 1)
+        if len(set(kp)) < len(kp) or len(set(vp)) < len(vp):
+            continue
+        off = int(rng.integers(-(vp.max() + 20), kp.max() + 20)) if rng.random() < 0.5 else int(rng.choice(ks)) + 64 * int(rng.integers(-2, 3))
+        if not across or chan == 1:
+            off = off // 8 * 8
+        want = SHAPE if np.intersect1d(kp, vp + off).size else 0
+        got = refusal(lib, UNPACK, B=B, n_kv_heads=nkv, L=L, P=0, k=1 << 20, v=(1 << 20) + 2 * off, batch=1 << 20, head=1 << 16, pv=1 << 30,
+                      k_batch=ks[0], k_head=ks[1], k_row=ks[2], v_batch=vs[0], v_head=vs[1], v_row=vs[2], v_chan=chan)
+        assert got == want, (B, nkv, L, ks, vs, chan, off)
+        found[want] += 1
+        # a cache of the same arrangement, in tiles
+        hs = nested([B, nkv], (16, HEAD), rng.random() < 0.3)
+        cp = places(list(zip((B, nkv), hs)), HEAD)
+        off = int(rng.integers(-(cp.max() + 64), cp.max() + 64)) // 16 * 16 if rng.random() < 0.5 else HEAD * int(rng.integers(1, 9)) + 16 * int(rng.integers(-1, 2))
+        want = SHAPE if np.intersect1d(cp[::16], cp[::16] + off).size else 0
+        assert refusal(lib, PACK, B=B, n_kv_heads=nkv, batch=hs[0], head=hs[1], pk=1 << 25, pv=(1 << 25) + off) == want, (B, nkv, hs, off)
+        found[want] += 1
+    assert min(found.values()) > 300, found
