@@ -117,6 +117,45 @@ def test_rows_in_and_out(case):
             assert torch.isnan(torch.as_strided(o, (o.storage_offset(),), (1,), 0).float()).all()
 
 
+def inside(shape, how, dtype, device):
+    """A buffer of sevens and a view [B, nkv, L, dh] into it that has some of them on every side: rows of channels, or channels of rows, from a
+    place of 16 bytes on and whole pieces of them apart, or from an odd place on."""
+    B, n, L, dh = shape
+    if how == "rows":
+        w = torch.full((n, B, L + 2, 3 * dh), 7.0, dtype=dtype, device=device)
+        return w, w[:, :, 1:1 + L, dh:2 * dh].transpose(0, 1)
+    first, wide = (8, (L + 23) // 8 * 8) if how == "whole" else (5, L + 13)
+    w = torch.full((B, n, dh + 2, wide), 7.0, dtype=dtype, device=device)
+    return w, w[:, :, 1:1 + dh, first:first + L].transpose(2, 3)
+
+
+def outside_is_seven(w, view):
+    own = torch.zeros(w.numel(), dtype=torch.bool, device=w.device)
+    own.as_strided(view.shape, view.stride(), view.storage_offset()).fill_(True)
+    return bool((w.flatten()[~own] == 7).all())
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+@pytest.mark.parametrize("dtype, dh", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("how", ["rows", "whole", "odd"])
+def test_nothing_around_the_rows_is_written(fmt, dtype, dh, how):
+    """Rows read back into the middle of a buffer, at lengths that end inside a piece of 16 bytes, inside a tile and behind one; one of the
+    sequences is absent."""
+    B, nkv, rows = 3, 2, 320
+    for L in (1, 2, 3, 7, 8, 9, 33, 63, 64, 65, 71, 127, 130):
+        x = [numbers(B, nkv, L, dh, dtype, i) for i in (1, 2)]
+        packed = mulo.alloc_packed_kv(B, nkv, rows, dh, FMT[fmt], DEV)
+        starts = torch.tensor([rows - L, -1, 61], dtype=torch.int32, device=DEV)
+        mulo.mulo_pack_rows(packed, mulo.make_kv_rows(*(t.to(DEV) for t in x), rows - L, starts))
+        (wk, k), (wv, v) = inside(x[0].shape, "rows", DT[dtype], DEV), inside(x[1].shape, how, DT[dtype], DEV)
+        mulo.mulo_unpack_rows(packed, mulo.make_kv_rows(k, v, rows - L, starts))
+        torch.cuda.synchronize()
+        for t, w, out in zip(x, (wk, wv), (k, v)):
+            assert outside_is_seven(w, out) and (out[1] == 7).all(), L
+            want = torch.tensor(OP.decode(*OP.encode(t.double().numpy(), fmt), fmt))
+            assert torch.equal(torch.nan_to_num(out[::2].double().cpu(), nan=5.5), torch.nan_to_num(want[::2], nan=5.5)), L
+
+
 @pytest.mark.parametrize("fmt", ["fp4", "fp8"])
 def test_keys_or_values_alone(fmt):
     x = numbers(2, 2, 5, 64, "bf16", 9)

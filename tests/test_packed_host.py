@@ -340,3 +340,19 @@ def test_random_layouts_against_sets_of_places(lib):
         assert refusal(lib, PACK, B=B, n_kv_heads=nkv, batch=hs[0], head=hs[1], pk=1 << 25, pv=(1 << 25) + off) == want, (B, nkv, hs, off)
         found[want] += 1
     assert min(found.values()) > 300, found
+
+
+@pytest.mark.parametrize("how", ["rows", "whole", "odd"])
+@pytest.mark.parametrize("L", [1, 3, 8])
+def test_a_number_written_beside_the_rows_is_noticed(how, L):
+    """The check that the tests on the card use: every place of the buffer but the rows' own."""
+    from tests.test_gpu_packed import inside, outside_is_seven
+    w, view = inside((2, 2, L, 4), how, torch.float32, "cpu")
+    view.fill_(1.0)
+    flat, own = w.view(-1), (w == 1).view(-1).clone()
+    assert own.sum() == view.numel() and not own[0] and not own[-1] and outside_is_seven(w, view)
+    for i in range(w.numel()):
+        if not own[i]:
+            flat[i] = 1.0
+            assert not outside_is_seven(w, view), i
+            flat[i] = 7.0
