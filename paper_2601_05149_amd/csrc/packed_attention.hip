@@ -367,12 +367,12 @@ __device__ __forceinline__ void span(const Args& a, int P, int r0, int n, int& p
     p_min = P + (ha == hb ? r0 - ha * a.L : 0);
     p_max = P + (ha == hb ? rb - hb * a.L : a.L - 1);
 }
-// The steps of ROWS rows that queries at p_min .. p_max see: the head [0, head) of the sinks and from `from` on the window; of them a share
+// The steps of ROWS rows that queries at p_min .. p_max see: the head [0, head) of the sinks and from `from` on the window
 struct Steps {
     int head, from, begin, end;
     __device__ __forceinline__ int of(int i) const { return i < head ? i : from + i - head; }
 };
-template <int ROWS> __device__ __forceinline__ Steps steps(const Args& a, int P, int p_min, int p_max, int split) {
+template <int ROWS> __device__ __forceinline__ Steps steps(const Args& a, int P, int p_min, int p_max) {
     Steps w;
     int lo = 0;
     w.head = 0;
@@ -381,8 +381,14 @@ template <int ROWS> __device__ __forceinline__ Steps steps(const Args& a, int P,
         w.head = ((a.sinks < lo ? a.sinks : lo) + ROWS - 1) / ROWS;
     }
     w.from = lo / ROWS > w.head ? lo / ROWS : w.head;
-    const int more = p_max / ROWS + 1 - w.from, n = P < 0 ? 0 : w.head + (more > 0 ? more : 0), per = (n + a.split - 1) / a.split;
-    w.begin = split * per;
+    const int more = p_max / ROWS + 1 - w.from;
+    w.begin = 0;
+    w.end = P < 0 ? 0 : w.head + (more > 0 ? more : 0);
+    return w;
+}
+__device__ __forceinline__ Steps share_of(Steps w, int split, int i) {      // share i of them
+    const int n = w.end, per = (n + split - 1) / split;
+    w.begin = i * per;
     w.end = w.begin + per < n ? w.begin + per : n;
     return w;
 }
@@ -414,15 +420,20 @@ struct Result {
         if (a.split > 1) *reinterpret_cast<float2*>(a.ml + 2 * row()) = make_float2(m, l);
     }
 };
-// Queries r0 .. r0 + n - 1 see nothing: zeros, or an empty share
-template <class T, int DH> __device__ __forceinline__ void nothing(const Args& a, const Place& w, int r0, int n, int tid, int threads) {
+// Queries r0 .. r0 + n - 1 see nothing: zeros
+template <class T, int DH> __device__ __forceinline__ void zeros(const Args& a, const Place& w, int r0, int n, int tid, int threads) {
     for (int x = tid; x < n * (DH / 4); x += threads) {
-        const int r = r0 + x / (DH / 4), c = x % (DH / 4) * 4;
+        const int r = r0 + x / (DH / 4);
         if (r >= a.n) return;
         const int hg = a.by_L.of(r);
-        const Result y{a, w.b, w.kvh * a.group + hg, r - hg * a.L, w.split};
-        if (a.split == 1) store4<T>(a, w.b, y.h, y.j, c, f32x4{0.f, 0.f, 0.f, 0.f});
-        else if (c == 0) y.put_ml(MINUS_INF, 0.f);
+        store4<T>(a, w.b, w.kvh * a.group + hg, r - hg * a.L, x % (DH / 4) * 4, f32x4{0.f, 0.f, 0.f, 0.f});
+    }
+}
+// ... of this share
+__device__ __forceinline__ void empty_share(const Args& a, const Place& w, int r0, int n, int tid, int threads) {
+    for (int r = r0 + tid; r < r0 + n && r < a.n; r += threads) {
+        const int hg = a.by_L.of(r);
+        Result{a, w.b, w.kvh * a.group + hg, r - hg * a.L, w.split}.put_ml(MINUS_INF, 0.f);
     }
 }
 
@@ -447,8 +458,8 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 2 : waves_per_simd(FMT, sizeof(T),
     const int r0 = w.qt * (16 * NQ);
     int p_min, p_max;
     span(a, w.P, r0, 16 * NQ, p_min, p_max);
-    const Steps st = steps<ROWS>(a, w.P, p_min, p_max, w.split);
-    if (st.begin >= st.end) return nothing<T, DH>(a, w, r0, 16 * NQ, tid, 64 * W);
+    const Steps st = share_of(steps<ROWS>(a, w.P, p_min, p_max), a.split, w.split);
+    if (st.begin >= st.end) return a.split > 1 ? empty_share(a, w, r0, 16 * NQ, tid, 64 * W) : zeros<T, DH>(a, w, r0, 16 * NQ, tid, 64 * W);
 
     const uint8_t* const kb = a.k + w.b * a.batch + w.kvh * a.head;
     const uint8_t* const vb = a.v + w.b * a.batch + w.kvh * a.head;
@@ -586,15 +597,15 @@ __global__ __launch_bounds__(64 * NW, 2) void k_packed_block(const Args a) {
     int g_min, g_max, p_min = 0, p_max = -1;      // of the workgroup, of the wavefront
     span(a, w.P, g0, NW * 16 * NQ, g_min, g_max);
     if (r0 < a.n) span(a, w.P, r0, 16 * NQ, p_min, p_max);
-    const Steps st = steps<PACKED_TILE>(a, w.P, g_min, g_max, w.split);
-    if (st.begin >= st.end) return nothing<T, DH>(a, w, g0, NW * 16 * NQ, tid, 64 * NW);
+    const Steps st = steps<PACKED_TILE>(a, w.P, g_min, g_max);      // (of a query's keys there is one share)
+    if (st.end == 0) return zeros<T, DH>(a, w, g0, NW * 16 * NQ, tid, 64 * NW);
 
     const uint8_t* const kb = a.k + w.b * a.batch + w.kvh * a.head;
     const uint8_t* const vb = a.v + w.b * a.batch + w.kvh * a.head;
     Keys<FMT, T, DH, 4> keys;
     Values<FMT, DH, 1> values;
-    values.load_block(vb, st.of(st.begin), wave, c16, lg);
-    keys.load(kb, st.of(st.begin), c16, lg);
+    values.load_block(vb, st.of(0), wave, c16, lg);
+    keys.load(kb, st.of(0), c16, lg);
     Query<T, DH> query[NQ];
     int at[NQ];
 #pragma unroll
@@ -631,9 +642,9 @@ __global__ __launch_bounds__(64 * NW, 2) void k_packed_block(const Args a) {
             unpack(pc, i, true);
         });
     };
-    clear(st.begin);
-    unpack_all(st.begin);
-    if (st.begin + 1 < st.end) values.load_block(vb, st.of(st.begin + 1), wave, c16, lg);
+    clear(0);
+    unpack_all(0);
+    if (1 < st.end) values.load_block(vb, st.of(1), wave, c16, lg);
     f32x4 o[U][NQ];
     float m_run[NQ], l_run[NQ];
 #pragma unroll
@@ -643,7 +654,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_packed_block(const Args a) {
 #pragma unroll
         for (int m = 0; m < U; ++m) o[m][q] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    for (int i = st.begin; i < st.end; ++i) {
+    for (int i = 0; i < st.end; ++i) {
         const int k0 = st.of(i) * PACKED_TILE;
         const bool next = i + 1 < st.end;
         // the buffer is full, and everybody has read the other one
