@@ -13,10 +13,13 @@ SOURCES = ["mulo_api.hip", "decide.hip", "elementwise.hip", "gemm.hip", "attenti
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument"]
 
-# The compiler's pass that folds a shift of a byte into an instruction (SDWA) has read that byte behind another instruction's overwriting
-# of its register here (a word whose four bytes become four scales): these sources are built without it.
+# The compiler's pass that folds a shift into an instruction that reads a byte (SDWA) has read the byte too late here: of the four scales of a
+# word, scale_of(word, 3) became v_lshlrev_b32_sdwa .. BYTE_3 of a register that v_lshlrev_b32 .., 7 and v_and_b32 for scale_of(word, 2) had
+# overwritten by then (AMD clang 22, roc-7.2.0, on an earlier form of the float32 kernel for heads of 64 and 32 queries a wavefront, which
+# test_attention covers).  As the source is now it compiles to the same numbers either way and runs as fast, but nothing in it rules the
+# pattern out.
 NO_SDWA = ["-mllvm", "-amdgpu-sdwa-peephole=0"]
-MORE_FLAGS = {"packed.hip": NO_SDWA, "packed_attention.hip": NO_SDWA}
+MORE_FLAGS = {"packed_attention.hip": NO_SDWA}
 
 
 def _compile(src):

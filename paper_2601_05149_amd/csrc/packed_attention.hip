@@ -271,8 +271,8 @@ __device__ __forceinline__ void scores(f32x4 (&s)[NX][NQ], const Keys<FMT, T, DH
         }
     });
 }
-// The compiler may move these instructions to where their results are used, also behind a branch that not all lanes take; all lanes' operands
-// are needed.
+// The products end here, in front of the loads and the softmax that follow them in the source.  Without this the compiler spreads them
+// among those: the same numbers, and 4 x 1024 queries behind 3200 rows take 214 us instead of 203.
 template <int N, int NQ> __device__ __forceinline__ void stay(f32x4 (&s)[N][NQ]) {
 #pragma unroll
     for (int x = 0; x < N; ++x)
