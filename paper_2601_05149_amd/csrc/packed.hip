@@ -85,9 +85,10 @@ template <int X> __device__ __forceinline__ uint32_t quad_swap(uint32_t v) {    
 // ---- rows in, rows out ----------------------------------------------------------------------------------------------
 // A thread has eight channels of a row, four threads a group: 16 bytes of bf16 in, 4 or 8 bytes of codes out, or the other way round.
 // Values that come as channels of rows go through LDS, 64 rows a workgroup: in pieces of 16 bytes 4 x 1024 rows of 32 heads of 128 pack in
-// 18 us (86 MB, 4.7 TB/s) and come back in 15; number by number the two took 92 us.
+// 18 us (85 MB, 4.7 TB/s; 8 bits 22) and come back in 15 (16.5); float32 32 and 28; number by number the first two took 92 us.
 // Bound by the numbers' bytes; 4 x 4224 rows back, 350 MB, in 50 us, 7 TB/s: written past the caches, which hold the codes that are read, against
-// 72 us through them.  A token's rows of 32 sequences take 3 us, a launch's time.
+// 72 us through them (8 bits 70 us; float32 141, 4.4 TB/s, and as rows of channels, whose lines are written in halves, 4 x 1024 rows in 47).  A token's
+// rows of 32 sequences take 3 us, a launch's time.
 constexpr int ROWS_THREADS = 256;
 struct __attribute__((packed, aligned(2))) Piece { u32x4 v; };
 struct RowsArgs : PackedRows {
@@ -152,7 +153,8 @@ __device__ __forceinline__ int first_row(const PackedRows& a, int b) {
     return P < a.rows - a.L ? P : a.rows - a.L;
 }
 
-// Rows of a thread.  us, one / two (through the caches), 4 x 4224 rows of 32 heads of 128 read back 76 / 72; float32, 4 x 1024 40.6 / 42.9.
+// Rows of a thread.  us, one / two, rows of 32 heads of 128 in 4 bits: 4 x 4224 packed 77 / 67, read back 61 / 56; float32, 4 x 1024 33.4 / 32.8 and
+// 46.6 / 57.4.
 constexpr int rows_each(int esz) { return esz == 2 ? 2 : 1; }
 
 template <int FMT, class T, int DH, bool PACK>

@@ -438,8 +438,8 @@ __device__ __forceinline__ void empty_share(const Args& a, const Place& w, int r
 }
 
 // ---- few queries: the wavefronts of a workgroup have the same ones, and steps in turn; joined in LDS --------------------
-// Bound by the cache where there are many sequences (32 of 4224 rows, 32 heads of 128, 4 bits, 575 MB: 104 us, 5.5 TB/s; 16 with a window
-// of 2048 rows in 8 bits, 304 MB: 54 us, 5.6 TB/s), by a wavefront's own chain of a step (1 to 1.5 us: loads, scores, maximum, exponentials,
+// Bound by the cache where there are many sequences (32 of 4224 rows, 32 heads of 128, 4 bits, 588 MB: 104 us, 5.7 TB/s; 16 with a window
+// of 2048 rows and 128 sinks in 8 bits, 303 MB of whole tiles: 54 us, 5.6 TB/s), by a wavefront's own chain of a step (1 to 1.5 us: loads, scores, maximum, exponentials,
 // products) where there are few: the plan spreads those over wavefronts and shares.  The next step's codes are on their way while a step is
 // computed (three wavefronts of a SIMD with 4 bits); a second step on its way gained nothing (28.3 us against 29.4, 29.8 against 30.5).
 // Against the running maximum of the keys as each step has it, a reference that moves once it is outgrown by 2^8 leaves out the products
@@ -578,12 +578,14 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 2 : waves_per_simd(FMT, sizeof(T),
 
 // ---- many queries: the wavefronts have queries of their own and share a tile's values ------------------------------------
 // Every wavefront unpacks a quarter of a tile's values into LDS, where all of them read the second product's operand: with values unpacked by
-// every wavefront for itself they were a third of the vector instructions (4 x 1024 queries behind 3200 rows, 32 heads of 128: 288 us in 4
-// bits, 388 in 8, against 229 and 278 here).  Two buffers, one barrier a tile.
-// Bound by instructions: of those 229 us the matrix instructions are busy for two fifths of the cycles and the vector ones (exponentials,
-// maxima, unpacking) for nearly all of the others; 1.15 PFLOP/s, a library product in bf16 of 8192^3 reaches 1.21.  Unpacking costs 32 us,
-// the barrier 9.  Eight wavefronts to a tile's values took 254 us, scores of the next tile beside the exponentials 236 to 308 (registers), a
-// third wavefront of a SIMD spills.  float32's three terms take three times the products: its blocks stay with k_packed_few.
+// every wavefront for itself they were a third of the vector instructions (4 x 1024 queries behind 3200 rows, 32 heads of 128: 278 us in 4
+// bits, 388 in 8, against 217 and 268 here).  Two buffers, one barrier a tile.
+// Bound by instructions: 249 GFLOP in those 217 us are 1.15 PFLOP/s, a library product in bf16 of 8192^3 reaches 1.21.  Of the cycles the
+// matrix instructions are busy for 51 %, the vector ones (exponentials, maxima, unpacking) for 62 %, so that little is left in which
+// neither is.  When the kernel took 241 us, unpacking was 32 of them and the barrier 9, eight wavefronts to a tile's values took 254, scores
+// of the next tile beside the exponentials 236 to 308 (registers); a third wavefront of a SIMD spills.  float32's three terms take three times
+// the products: its blocks stay with k_packed_few.  A query's keys are one workgroup's, so blocks of few workgroups wait for their longest
+// (make_plan's comment: 1 x 1024, 4 x 256).
 constexpr int BLOCK_NQ = 2;
 template <int FMT, int DH>
 __global__ __launch_bounds__(64 * NW, 2) void k_packed_block(const Args a) {
@@ -740,22 +742,26 @@ void tiles_seen(const PackedAttn& a, int64_t n, int64_t rows, double& most, doub
 
 // Four or eight wavefronts of k_packed_few with 16 queries, four with 32, shares of the keys, or k_packed_block: the one with the least time
 // by the estimate.  Measured, in us (bf16, 32 heads of 128, 4 bits where nothing else is said; "4/1" four wavefronts with 16 queries, "x 8" in
-// shares):
-//   1 x 1 query, 500 rows             4/1 6.5     8/1 7.1     4/1 x 2 9.6
-//   1 x 1, 4000                       4/1 22      8/1 17.3    4/1 x 8 11.4     8/1 x 8 12.5
-//   4 x 1, 4000                       4/1 27      8/1 20.4    4/1 x 4 19.5
-//   12 x 1, 4000                      4/1 43      8/1 47      8/1 x 2 47
-//   32 x 1, 4223                      4/1 104     8/1 103
-//   2 x 1, 60000, 8 key heads         8/1 x 16 30.5           4/1 x 37 35
-//   16 x 1, 4000, 16 heads of 64      4/1 22.6    8/1 16.9
-//   16 x 16, 4000, 8 key heads        4/1 38.6    4/2 36.2    8/1 39.3
-//   4 x 256, 3000                     4/1 88      4/2 72      block 79
-//   4 x 256, 832, 16 heads of 64, 8 bits          4/2 13.3    block 22.3
-//   16 x 64, 0                        4/1 17.4    4/2 17.7    block 10.6
-//   1 x 1024, 0                       4/2 28.0    block 27.2
-//   4 x 1024, 3200                    4/2 288     block 229     (8 bits 388, 278)
-//   8 x 1024, 0, 16 heads of 64       4/2 52      block 36
-//   float32, 6 x 5, 800, 16 heads of 64, 8 bits   4/1 9.5     8/1 8.8;   4 x 256   4/1 22.3   4/2 20.4
+// shares; * what the estimate takes):
+//   1 x 1 query, 500 rows             4/1 6.4     8/1 7.2 *   4/1 x 2 8.8
+//   1 x 1, 4000                       4/1 22      8/1 17.6    4/1 x 8 11.5     8/1 x 8 12.1 *
+//   4 x 1, 4000                       4/1 27      8/1 20.4 *  4/1 x 4 19.8
+//   12 x 1, 4000                      4/1 41 *    8/1 45      8/1 x 2 47
+//   32 x 1, 4223                      4/1 104 *   8/1 101
+//   2 x 1, 60000, 8 key heads         8/1 x 16 31 *           4/1 x 37 36
+//   16 x 1, 4000, 16 heads of 64      4/1 22.4    8/1 17.1 *
+//   16 x 16, 4000, 8 key heads        4/1 32 *    4/2 34.5    8/1 36.5
+//   4 x 256, 3000                     4/1 79      4/2 68 *    block 80
+//   4 x 256, 832, 16 heads of 64, 8 bits          4/2 13.5 *  block 22.5
+//   16 x 64, 0                        4/1 17.6    4/2 18.1    block 11.5 *
+//   1 x 1024, 0                       4/2 28 *    block 28
+//   4 x 1024, 3200                    4/2 278     block 217 * (8 bits 388, 268 *)
+//   8 x 1024, 0                       4/2 188     block 101 *
+//   8 x 1024, 0, 16 heads of 64       4/2 52      block 35 *
+//   float32, 6 x 5, 800, 16 heads of 64, 8 bits   4/1 9.6     8/1 9.0 *; 4 x 256   4/1 22.3   4/2 20.1 *
+// It takes the slower side of four of these rows, by 3 to 12 %.  Over 46 other calls, spread over all sizes, it was 4 % behind the best of up
+// to 22 plans in the mean, more than 10 % behind for five of them, 38 % at most (four single float32 queries over 2000 rows: 8/1 11.7, 4/1 x 8
+// 8.5): eight wavefronts have the START of four, and float32's shares look dearer than they are.
 // part_floats: the scratch there is (packed_attention_floats asks with as much as can be wanted)
 Plan make_plan(const PackedAttn& a, int64_t part_floats) {
     const int64_t n = (int64_t)(a.nh / a.nkv) * a.L, pairs = (int64_t)a.B * a.nkv, slot_floats = (int64_t)a.B * a.nh * a.L * (a.dh + 2);
