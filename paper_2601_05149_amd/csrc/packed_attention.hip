@@ -272,7 +272,7 @@ __device__ __forceinline__ void scores(f32x4 (&s)[NX][NQ], const Keys<FMT, T, DH
     });
 }
 // The products end here, in front of the loads and the softmax that follow them in the source.  Without this the compiler spreads them
-// among those: the same numbers, and 4 x 1024 queries behind 3200 rows take 214 us instead of 203.
+// among those: the same numbers, and 4 x 1024 queries behind 3200 rows take 214 us instead of 203 (the same call over and over).
 template <int N, int NQ> __device__ __forceinline__ void stay(f32x4 (&s)[N][NQ]) {
 #pragma unroll
     for (int x = 0; x < N; ++x)
@@ -439,9 +439,10 @@ __device__ __forceinline__ void empty_share(const Args& a, const Place& w, int r
 
 // ---- few queries: the wavefronts of a workgroup have the same ones, and steps in turn; joined in LDS --------------------
 // Bound by the cache where there are many sequences (32 of 4224 rows, 32 heads of 128, 4 bits, 588 MB: 104 us, 5.7 TB/s; 16 with a window
-// of 2048 rows and 128 sinks in 8 bits, 303 MB of whole tiles: 54 us, 5.6 TB/s), by a wavefront's own chain of a step (1 to 1.5 us: loads, scores, maximum, exponentials,
-// products) where there are few: the plan spreads those over wavefronts and shares.  The next step's codes are on their way while a step is
-// computed (three wavefronts of a SIMD with 4 bits); a second step on its way gained nothing (28.3 us against 29.4, 29.8 against 30.5).
+// of 2048 rows and 128 sinks in 8 bits, 303 MB of whole tiles: 54 us, 5.6 TB/s), by a wavefront's own chain of a step (1 to 1.5 us: loads,
+// scores, maximum, exponentials, products) where there are few: the plan spreads those over wavefronts and shares.  The next step's codes
+// are on their way while a step is computed (three wavefronts of a SIMD with 4 bits); a second step on its way gained nothing (28.3 us
+// against 29.4, 29.8 against 30.5).
 // Against the running maximum of the keys as each step has it, a reference that moves once it is outgrown by 2^8 leaves out the products
 // with alpha of nearly every step.
 // Blocks of 16 rows that a wavefront goes over at a time: a tile, or half of one where the codes would take more registers than there are
